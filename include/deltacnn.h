@@ -45,7 +45,8 @@ typedef enum {
     DCNN_EUNSUPPORTED = 7
 } dcnn_status;
 
-typedef enum { DCNN_F32 = 0, DCNN_F16 = 1 } dcnn_dtype;
+/* DCNN_BF16 and DCNN_I8 exist for the row operators (dcnn_rows_*) only; layers and networks refuse them. */
+typedef enum { DCNN_F32 = 0, DCNN_F16 = 1, DCNN_BF16 = 2, DCNN_I8 = 3 } dcnn_dtype;
 
 typedef enum {
     DCNN_DELTAGEN = 0,      /* input layer: dense frame -> (delta, mask)            Fig. 2; Section 4   */
@@ -274,6 +275,96 @@ int32_t     dcnn_net_num_layers(const dcnn_net* net);
 dcnn_status dcnn_net_layer(const dcnn_net* net, int32_t i, dcnn_layer** layer, int32_t* node_id);
 /* Per-layer counters of the last step, stats_host[dcnn_net_num_layers]; synchronises. */
 dcnn_status dcnn_net_stats(dcnn_net* net, dcnn_stats* stats_host);
+
+/* ---- rows: per-token operators ---------------------------------------------------------------- */
+/* A row is the channel vector of one token: one pixel of an NHWC map seen as [map_rows, c], or one row of a plain
+ * matrix.  Blocks that treat every pixel by itself (norm, expansion, projection, gated residual) give the same values
+ * whether they run on the whole map or on the flagged pixels alone, so each operator takes a list as layers hand it out:
+ *   idx_dev    NULL: row r of the operator is row r of the maps.  Else entry r names the map row (dcnn_delta.idx).
+ *              An entry outside 0 .. map_rows-1 is a row without a token: nothing of a map is read or written for it,
+ *              its compact outputs are zero.  Entries that are written through (y) must be distinct.
+ *   count_dev  NULL: `rows` rows.  Else the number of rows is min(*count_dev, rows), read on the GPU.
+ * Maps (x, y) are addressed through idx, compact matrices (h, z, q, outputs of products) by r; compact rows at and
+ * beyond the number of rows are neither read nor written.  Leading dimensions (ld*) count elements; rows of maps and
+ * matrices need no alignment beyond their element's, except 8-bit rows (below).  Arithmetic is fp32 (products: exact
+ * 32-bit integers), with one rounding to the storage type at each store.  No call needs a workspace of the context. */
+typedef struct {
+    int64_t        rows;        /* rows at most (0: nothing is launched)             */
+    int64_t        map_rows;    /* rows of the maps; without idx_dev at least `rows`  */
+    const int32_t* idx_dev;
+    const int32_t* count_dev;
+} dcnn_row_list;
+
+typedef enum { DCNN_NORM_NONE = 0, DCNN_NORM_RMS = 1, DCNN_NORM_LAYER = 2 } dcnn_norm_kind;
+
+/* RMS: v / sqrt(mean(v^2) + eps) * w + b.  LAYER: (v - mean(v)) / sqrt(var(v) + eps) * w + b (var over c, not c-1). */
+typedef struct {
+    int32_t     kind;           /* dcnn_norm_kind; NONE: v itself, w and b are not read */
+    float       eps;
+    const void* w_dev;          /* [c] of the call's dtype, NULL: ones                 */
+    const void* b_dev;          /* [c], NULL: zeros                                    */
+} dcnn_row_norm;
+
+/* The end of one residual block and the start of the next in one pass:
+ *   y[i] = x[i] + scale * gate[i / gate_rows] * post(h[r]),   z[r] = pre(y[i]),   i = idx[r].
+ * x NULL: 0; h NULL: y is x (and y_dev must be NULL); gate NULL: 1.  z is formed from y before y is rounded.
+ * q / q_scale: z in 8 bits, q[r] = round_half_even(z[r] * (127 / max|z[r]|)) with q_scale[r] = max|z[r]| / 127.  A row
+ * whose largest magnitude is below 1e-36 becomes zeros with scale 0, a row that holds a NaN or an infinity zeros with
+ * scale NaN (products of it are NaN).  At least one of y, z, q is wanted; y_dev may equal x_dev (in place), outputs
+ * overlap nothing else.  c <= 32768. */
+typedef struct {
+    dcnn_row_list list;
+    int32_t       dtype;        /* of x, h, gate, y, z and the norms' w and b: F32, F16, BF16 */
+    int32_t       c;
+    const void*   x_dev;        /* map                                                 */
+    const void*   h_dev;        /* compact                                             */
+    const void*   gate_dev;     /* [ceil(map_rows / gate_rows), c]                      */
+    void*         y_dev;        /* map                                                 */
+    void*         z_dev;        /* compact                                             */
+    int8_t*       q_dev;        /* compact; 16-byte aligned, ldq a multiple of 16.  Bytes c .. of a row's last 16 may be overwritten */
+    float*        q_scale_dev;  /* [rows]                                              */
+    int64_t       ldx, ldh, ldg, ldy, ldz, ldq;
+    int64_t       gate_rows;    /* map rows that share a row of gate; 0: all of them    */
+    float         scale;
+    dcnn_row_norm post, pre;
+} dcnn_rows_norm_args;
+dcnn_status dcnn_rows_norm(dcnn_ctx* ctx, const dcnn_rows_norm_args* args);
+
+/* Weights of a product in 8 bits with a scale per output channel, laid out once for the matrix cores.  w_dev is [k][n]
+ * (a 1x1 convolution's [cin][cout]) with leading dimension ldw.  F32 / F16 / BF16 weights are quantised here (scale
+ * max|w[:, n]| / 127, rounded half to even); I8 weights come with scale_dev [n].  packed_dev: dcnn_rows_weights_bytes(k, n)
+ * bytes (0 where k or n is out of range), 256-byte aligned; w_dev and scale_dev may be freed after dcnn_ctx_sync.
+ * k <= 65536: the sums of 8-bit products then stay exact in 32 bits. */
+size_t      dcnn_rows_weights_bytes(int64_t k, int64_t n);
+dcnn_status dcnn_rows_pack(dcnn_ctx* ctx, int32_t dtype, int64_t k, int64_t n, const void* w_dev, int64_t ldw,
+                           const float* scale_dev, void* packed_dev, size_t packed_bytes);
+
+/* y[r][j] = act( (sum_k q[r][k] * w[k][j]) * (q_scale[r] * w_scale[j]) + bias[j] ).
+ * dcnn_rows_matmul takes rows that are 8-bit integers already; dcnn_rows_linear takes the rows of a map in the type of
+ * y, norms them with `pre` (or not: NONE) and quantises them as dcnn_rows_norm does: two of a block's steps in one call.
+ * scratch_dev: dcnn_rows_scratch_bytes(rows, k, n) bytes (may be 0), 256-byte aligned, zero-filled before its first use
+ * and left alone by the caller between calls; calls that share it must not overlap. */
+typedef struct {
+    dcnn_row_list list;         /* matmul: rows and count_dev only                      */
+    int32_t       dtype;        /* of y, bias and x: F32, F16, BF16                     */
+    int32_t       act;          /* dcnn_act                                            */
+    int64_t       k, n;
+    const void*   packed_dev;   /* of dcnn_rows_pack with the same k and n              */
+    const void*   bias_dev;     /* [n] or NULL                                         */
+    void*         y_dev;        /* [rows, n] compact                                   */
+    int64_t       ldy;
+    const int8_t* q_dev;        /* matmul: [rows, k], 16-byte aligned, ldq a multiple of 16 (the bytes behind k may hold anything) */
+    const float*  q_scale_dev;  /* matmul: [rows]                                      */
+    int64_t       ldq;
+    const void*   x_dev;        /* linear: map [map_rows, k]; k <= 32768                */
+    int64_t       ldx;
+    dcnn_row_norm pre;          /* linear                                              */
+    void*         scratch_dev;
+    size_t        scratch_bytes;
+} dcnn_rows_matmul_args;
+size_t      dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n);
+dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
+dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
 
 #ifdef __cplusplus
 }

@@ -6,5 +6,5 @@ The work is done by hand-written HIP kernels for gfx950 in `lib/libdeltacnn.so` 
 """
 from .binding import (  # noqa: F401
     ACCUM, ACT, CONCAT, GAVGPOOL, UPSAMPLE_BILINEAR, ACT_CODES, ACT_NONE, ACT_RELU, ACT_RELU6, CONV, DELTAGEN, DWCONV, F16, F32, MAXPOOL, UPSAMPLE,
-    Context, DcnnError, Delta, Layer, Net, EXPORTS, LIB_PATH, load_library, make_desc,
+    BF16, I8, Context, DcnnError, Delta, Layer, Net, RowNorm, RowWeights, EXPORTS, LIB_PATH, load_library, make_desc,
 )

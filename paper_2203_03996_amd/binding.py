@@ -17,11 +17,13 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libdeltacnn.so")
 
-F32, F16 = 0, 1
+F32, F16, BF16, I8 = range(4)          # (BF16 and I8: row operators only)
 DELTAGEN, CONV, DWCONV, ACT, MAXPOOL, UPSAMPLE, ACCUM, CONCAT, UPSAMPLE_BILINEAR, GAVGPOOL = range(10)
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
 ACT_CODES = {"none": ACT_NONE, None: ACT_NONE, "relu": ACT_RELU, "relu6": ACT_RELU6}
 TORCH_DTYPE = {F32: torch.float32, F16: torch.float16}
+ROW_DTYPE_CODE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+NORM_CODES = {"none": 0, None: 0, "rms": 1, "layer": 2}
 DTYPE_CODE = {"f32": F32, "f16": F16}
 STATUS_NAMES = ["OK", "EINVAL", "ESHAPE", "EDTYPE", "ESTATE", "ENOMEM", "EHIP", "EUNSUPPORTED"]
 
@@ -32,6 +34,8 @@ EXPORTS = [
     "dcnn_layer_stats", "dcnn_layer_set_eps", "dcnn_layer_set_timing", "dcnn_layer_set_counting", "dcnn_layer_timing", "dcnn_net_create", "dcnn_net_destroy", "dcnn_net_add", "dcnn_net_finalize",
     "dcnn_net_bind", "dcnn_net_init", "dcnn_net_step", "dcnn_net_reset", "dcnn_net_output",
     "dcnn_net_num_layers", "dcnn_net_layer", "dcnn_net_stats",
+    "dcnn_rows_norm", "dcnn_rows_weights_bytes", "dcnn_rows_pack", "dcnn_rows_scratch_bytes", "dcnn_rows_matmul",
+    "dcnn_rows_linear",
 ]
 
 
@@ -64,6 +68,29 @@ class Stats(C.Structure):
 
     def as_dict(self) -> dict:
         return {name: getattr(self, name) for name, _ in self._fields_ if name != "reserved"}
+
+
+class RowList(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("map_rows", C.c_int64), ("idx", C.c_void_p), ("count", C.c_void_p)]
+
+
+class RowNormStruct(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("w", C.c_void_p), ("b", C.c_void_p)]
+
+
+class RowsNormArgs(C.Structure):
+    _fields_ = [("list", RowList), ("dtype", C.c_int32), ("c", C.c_int32), ("x", C.c_void_p), ("h", C.c_void_p),
+                ("gate", C.c_void_p), ("y", C.c_void_p), ("z", C.c_void_p), ("q", C.c_void_p), ("q_scale", C.c_void_p),
+                ("ldx", C.c_int64), ("ldh", C.c_int64), ("ldg", C.c_int64), ("ldy", C.c_int64), ("ldz", C.c_int64),
+                ("ldq", C.c_int64), ("gate_rows", C.c_int64), ("scale", C.c_float), ("post", RowNormStruct),
+                ("pre", RowNormStruct)]
+
+
+class RowsMatmulArgs(C.Structure):
+    _fields_ = [("list", RowList), ("dtype", C.c_int32), ("act", C.c_int32), ("k", C.c_int64), ("n", C.c_int64),
+                ("packed", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("q", C.c_void_p),
+                ("q_scale", C.c_void_p), ("ldq", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("pre", RowNormStruct), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
 
 
 class DcnnError(RuntimeError):
@@ -126,6 +153,14 @@ def load_library() -> C.CDLL:
     lib.dcnn_net_num_layers.restype = i32
     lib.dcnn_net_layer.argtypes = [vp, i32, P(vp), P(i32)]
     lib.dcnn_net_stats.argtypes = [vp, P(Stats)]
+    lib.dcnn_rows_norm.argtypes = [vp, P(RowsNormArgs)]
+    lib.dcnn_rows_weights_bytes.argtypes = [C.c_int64, C.c_int64]
+    lib.dcnn_rows_weights_bytes.restype = sz
+    lib.dcnn_rows_pack.argtypes = [vp, i32, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp, sz]
+    lib.dcnn_rows_scratch_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+    lib.dcnn_rows_scratch_bytes.restype = sz
+    lib.dcnn_rows_matmul.argtypes = [vp, P(RowsMatmulArgs)]
+    lib.dcnn_rows_linear.argtypes = [vp, P(RowsMatmulArgs)]
     _lib = lib
     return lib
 
@@ -214,6 +249,77 @@ class Context:
         n, h, w = mask_in.shape
         self.check(self.lib.dcnn_mask_compact_static(self.handle, _ptr(mask_in), n, h, w, k, stride, pad, _ptr(mask_b),
                                                      _ptr(mask_out), _ptr(idx), _ptr(count)))
+
+    def empty(self, shape, dtype):
+        """An uninitialised device tensor that belongs to the context's stream, whichever stream torch is on."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def rows_norm(self, x=None, h=None, *, post=None, gate=None, gate_rows=0, scale=1.0, pre=None, idx=None, count=None,
+                  y=None, z=None, q=None, q_scale=None):
+        """dcnn_rows_norm: y = x + scale * gate * post(h) and z = pre(y), z also in 8 bits (q with q_scale).
+
+        x and y are maps (last dimension c), the rest is [rows, c].  y, z, q: a tensor to write, True for a new one, or
+        None where it is not wanted (q_scale: a tensor [rows], or None for a new one).  post, pre: RowNorm or None.
+        Returns (y, z, q, q_scale)."""
+        t = x if x is not None else h
+        if t is None:
+            raise ValueError("rows_norm: neither x nor h")
+        c = t.shape[-1]
+        dt = t.dtype
+        a = RowsNormArgs()
+        a.dtype, a.c, a.scale, a.gate_rows = _row_dtype(dt), c, scale, gate_rows
+        rows = idx.numel() if idx is not None else None
+        if x is not None:
+            x, a.ldx, n = _as_rows(x, "x", c, dt, self.device)
+            a.x, a.list.map_rows = x.data_ptr(), n
+            rows = n if rows is None else rows
+        if h is not None:
+            h, a.ldh, n = _as_rows(h, "h", c, dt, self.device)
+            a.h = h.data_ptr()
+            rows = n if rows is None or (idx is not None and n < rows) else rows
+            if n < rows:
+                raise ValueError(f"rows_norm: h has {n} rows, {rows} are wanted")
+        if y is True:
+            y = self.empty(x.shape if x is not None else (rows, c), dt)
+        if y is not None:
+            yr, a.ldy, n = _as_rows(y, "y", c, dt, self.device)
+            if x is not None and n != a.list.map_rows:
+                raise ValueError(f"rows_norm: x has {a.list.map_rows} rows, y {n}")
+            a.y, a.list.map_rows = yr.data_ptr(), n
+        elif x is None:
+            a.list.map_rows = rows if idx is None else 0x7fffffff
+        if gate is not None:
+            gate, a.ldg, n = _as_rows(gate if gate.dim() > 1 else gate[None], "gate", c, dt, self.device)
+            if n < (-(-a.list.map_rows // gate_rows) if gate_rows > 0 else 1):
+                raise ValueError(f"rows_norm: {n} rows of gate for {a.list.map_rows} map rows, {gate_rows} to each")
+            a.gate = gate.data_ptr()
+        if z is True:
+            z = self.empty((rows, c), dt)
+        if z is not None:
+            z, a.ldz, n = _as_rows(z, "z", c, dt, self.device)
+            rows = min(rows, n)
+            a.z = z.data_ptr()
+        if q is True:
+            q = self.empty((rows, -(-c // 16) * 16), torch.int8)[:, :c]
+        if q is not None:
+            q_scale = self.empty(rows, torch.float32) if q_scale is None else q_scale
+            a.ldq = _check_q(q, q_scale, c, self.device)
+            rows = min(rows, q.shape[0])
+            a.q, a.q_scale = q.data_ptr(), q_scale.data_ptr()
+        if post is not None:
+            post.fill(a.post, c, dt, self.device)
+        if pre is not None:
+            pre.fill(a.pre, c, dt, self.device)
+        a.list.rows, a.list.idx, a.list.count = rows, _int32(idx, "idx", self.device), _int32(count, "count", self.device)
+        self.check(self.lib.dcnn_rows_norm(self.handle, C.byref(a)))
+        return y, z, q, q_scale
+
+    def rows_quantize(self, x, *, pre=None, idx=None, count=None):
+        """Rows of x (normed with `pre`, or as they are) in 8 bits: (q [rows, c], q_scale [rows])."""
+        return self.rows_norm(x, pre=pre, idx=idx, count=count, q=True)[2:]
 
     def __del__(self):
         try:
@@ -314,6 +420,130 @@ class Layer:
                 self.handle = None
         except Exception:
             pass
+
+
+def _row_dtype(dt) -> int:
+    code = ROW_DTYPE_CODE.get(dt)
+    if code is None:
+        raise ValueError(f"row operators take float32, float16 and bfloat16, got {dt}")
+    return code
+
+
+def _as_rows(t, name, c, dt, device):
+    """(t as a matrix of c columns, its leading dimension, its rows); the ABI takes bare pointers, so shapes are checked here."""
+    if t.dim() != 2:
+        t = t.view(-1, t.shape[-1])
+    if t.shape[1] != c or t.dtype != dt or t.device.type != device.type or (c > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must hold rows of {c} {dt} side by side on {device}, got {tuple(t.shape)} {t.dtype} strides {t.stride()} "
+                         f"on {t.device}")
+    n = t.shape[0]
+    ld = t.stride(0)
+    if n > 1 and ld < c:
+        raise ValueError(f"{name}: rows overlap (stride {ld}, {c} columns)")
+    return t, (ld if n > 1 else c), n
+
+
+def _check_q(q, q_scale, c, device):
+    """Leading dimension of 8-bit rows."""
+    if q.dim() != 2 or q.shape[1] != c or q.dtype != torch.int8 or q.device.type != device.type or (c > 1 and q.stride(1) != 1):
+        raise ValueError(f"q must be an int8 device matrix of {c} columns, got {tuple(q.shape)} {q.dtype} strides {q.stride()}")
+    if q_scale.dtype != torch.float32 or q_scale.numel() < q.shape[0] or not q_scale.is_contiguous() or q_scale.device.type != device.type:
+        raise ValueError(f"q_scale must hold {q.shape[0]} float32 numbers on the device")
+    n, padded = q.shape[0], -(-c // 16) * 16
+    ld = q.stride(0) if n > 1 else padded
+    if n and q.storage_offset() + (n - 1) * ld + padded > q.untyped_storage().nbytes():
+        raise ValueError("the last row of q does not fill its multiple of 16 bytes")
+    return ld
+
+
+def _int32(t, name, device):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device.type != device.type or (name == "count" and t.numel() != 1):
+        raise ValueError(f"{name} must be a contiguous int32 device tensor")
+    return t.data_ptr()
+
+
+class RowNorm:
+    """Parameters of a norm over a row's channels: kind "rms" or "layer", weight and bias [c] (None: ones, zeros)."""
+
+    def __init__(self, kind: str, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5):
+        self.kind, self.weight, self.bias, self.eps = NORM_CODES[kind], weight, bias, float(eps)
+
+    def fill(self, s: RowNormStruct, c: int, dt, device):
+        s.kind, s.eps = self.kind, self.eps
+        for name, t in (("w", self.weight), ("b", self.bias)):
+            if t is None:
+                setattr(s, name, None)
+                continue
+            if t.shape != (c,) or t.dtype != dt or t.device.type != device.type or not t.is_contiguous():
+                raise ValueError(f"a norm's parameters must be contiguous [{c}] {dt} on the device, got {tuple(t.shape)} {t.dtype}")
+            setattr(s, name, t.data_ptr())
+
+
+class RowWeights:
+    """Weights [k, n] of a product, in 8 bits with a scale per output channel, laid out once for the matrix cores (dcnn_rows_pack).
+
+    weights: floating point (quantised here), or int8 with `scale` [n].  bias: [n] of the outputs' type, or None."""
+
+    def __init__(self, ctx: Context, weights: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None, act="none"):
+        self.ctx, lib = ctx, ctx.lib
+        if weights.dim() != 2 or weights.stride(1) != 1 or not weights.is_cuda:
+            raise ValueError("weights must be a device matrix [k, n] with its rows side by side")
+        k, n = weights.shape
+        code = I8 if weights.dtype == torch.int8 else _row_dtype(weights.dtype)
+        if (scale is not None) != (code == I8) or (scale is not None and (scale.shape != (n,) or scale.dtype != torch.float32 or
+                                                                          not scale.is_contiguous() or not scale.is_cuda)):
+            raise ValueError(f"8-bit weights come with a float32 scale [{n}] on the device, others without one")
+        self.k, self.n, self.bias, self.scale = k, n, bias, scale
+        nbytes = lib.dcnn_rows_weights_bytes(k, n)
+        if nbytes == 0:
+            raise ValueError(f"weights [{k}, {n}] are out of range")
+        self.packed = ctx.empty(nbytes, torch.uint8)
+        ctx.check(lib.dcnn_rows_pack(ctx.handle, code, k, n, weights.data_ptr(), weights.stride(0) if k > 1 else n, _ptr(scale),
+                                     self.packed.data_ptr(), nbytes))
+        self._source = weights                                    # until the stream has read it
+        self._scratch = None
+        self._args = a = RowsMatmulArgs()
+        a.k, a.n, a.act, a.packed = k, n, ACT_CODES[act], self.packed.data_ptr()
+        if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
+            raise ValueError(f"bias must be a contiguous device tensor [{n}]")
+        a.bias = _ptr(bias)
+
+    def _call(self, call, rows, dt, count, out):
+        ctx, a = self.ctx, self._args
+        if self.bias is not None and self.bias.dtype != dt:
+            raise ValueError(f"the bias is {self.bias.dtype}, the output {dt}")
+        a.dtype = _row_dtype(dt)
+        if out is None:
+            out = ctx.empty((rows, self.n), dt)
+        o, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.device)
+        a.list.rows, a.list.count, a.y = min(rows, n), _int32(count, "count", ctx.device), o.data_ptr()
+        need = ctx.lib.dcnn_rows_scratch_bytes(a.list.rows, self.k, self.n)
+        if self._scratch is None or self._scratch.numel() < need:
+            with torch.cuda.stream(ctx.stream):
+                self._scratch = torch.zeros(max(need, 256), dtype=torch.uint8, device=ctx.device)
+        a.scratch, a.scratch_bytes = self._scratch.data_ptr(), self._scratch.numel()
+        ctx.check(call(ctx.handle, C.byref(a)))
+        return out
+
+    def matmul(self, q, q_scale, *, dtype=torch.float16, count=None, out=None):
+        """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`."""
+        a = self._args
+        a.ldq = _check_q(q, q_scale, self.k, self.ctx.device)
+        a.q, a.q_scale, a.x, a.list.idx, a.list.map_rows = q.data_ptr(), q_scale.data_ptr(), None, None, 0
+        return self._call(self.ctx.lib.dcnn_rows_matmul, q.shape[0], dtype, count, out)
+
+    def linear(self, x, *, pre=None, idx=None, count=None, out=None):
+        """dcnn_rows_linear: rows of the map x (those that idx names), normed with `pre`, quantised and multiplied; [rows, n]."""
+        a = self._args
+        x, a.ldx, n = _as_rows(x, "x", self.k, x.dtype, self.ctx.device)
+        a.q, a.q_scale, a.x, a.list.map_rows, a.list.idx = None, None, x.data_ptr(), n, _int32(idx, "idx", self.ctx.device)
+        if pre is not None:
+            pre.fill(a.pre, self.k, x.dtype, self.ctx.device)
+        else:
+            a.pre.kind = 0
+        return self._call(self.ctx.lib.dcnn_rows_linear, n if idx is None else idx.numel(), x.dtype, count, out)
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

@@ -1,0 +1,95 @@
+// Device-side helpers of the row operators: element types, 16-byte vectors at any element address, reductions over a row's lanes.
+#pragma once
+
+#include "device_utils.h"
+#include "rows.h"
+
+namespace dcnn {
+
+typedef __bf16 bf16;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+
+// 16 bytes of a row.  Rows start at any multiple of the element's size (odd widths, views), and the memory path takes vectors
+// at such addresses: the alignment is the element's.
+template <typename T> struct RowVec;
+template <> struct RowVec<float> { static constexpr int E = 4; typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct RowVec<f16> { static constexpr int E = 8; typedef f16 type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct RowVec<bf16> { static constexpr int E = 8; typedef bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
+// Four consecutive outputs.
+template <typename T> struct RowQuad { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
+
+// Rows of this call, read on the GPU where a list's length is.
+__device__ __forceinline__ int row_count(const int32_t* count, int rows) {
+    if (count == nullptr) return rows;
+    const int n = *count;
+    return n < 0 ? 0 : (n < rows ? n : rows);
+}
+
+struct SumOp {
+    typedef float type;
+    static __device__ __forceinline__ float op(float a, float b) { return a + b; }
+};
+struct MaxOp {                   // bit patterns of magnitudes: NaN above infinity above every number
+    typedef uint32_t type;
+    static __device__ __forceinline__ uint32_t op(uint32_t a, uint32_t b) { return a > b ? a : b; }
+};
+template <typename Op, int CTRL> __device__ __forceinline__ typename Op::type dpp_step(typename Op::type u) {
+    const int v = __builtin_bit_cast(int, u);
+    return Op::op(u, __builtin_bit_cast(typename Op::type, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, true)));
+}
+// Over aligned groups of L lanes of a wave, delivered to all of them; every step adds the same two numbers on both sides, so
+// the lanes of a group hold the same bits.  (Within 16 lanes by lane permutations, see group_max.)
+template <typename Op, int L> __device__ __forceinline__ typename Op::type wave_reduce(typename Op::type u) {
+    if constexpr (L >= 2) u = dpp_step<Op, 0xB1>(u);
+    if constexpr (L >= 4) u = dpp_step<Op, 0x4E>(u);
+    if constexpr (L >= 8) u = dpp_step<Op, 0x141>(u);
+    if constexpr (L >= 16) u = dpp_step<Op, 0x140>(u);
+    if constexpr (L >= 32) u = Op::op(u, __shfl_xor(u, 16, kWave));
+    if constexpr (L >= 64) u = Op::op(u, __shfl_xor(u, 32, kWave));
+    return u;
+}
+// Over the L lanes of a row: a part of a wave, or the whole workgroup.  `red` is 2 * waves words of LDS, `turn` alternates: a
+// reduction's words are overwritten two reductions later, behind the barrier of the one between.
+template <typename Op, int L> __device__ __forceinline__ typename Op::type row_reduce(typename Op::type u, uint32_t* red, int& turn) {
+    u = wave_reduce<Op, (L < kWave ? L : kWave)>(u);
+    if constexpr (L > kWave) {
+        constexpr int W = L / kWave;
+        uint32_t* s = red + turn * W;
+        turn ^= 1;
+        if (threadIdx.x % kWave == 0) s[threadIdx.x / kWave] = __builtin_bit_cast(uint32_t, u);
+        __syncthreads();
+        u = __builtin_bit_cast(typename Op::type, s[0]);
+#pragma unroll
+        for (int i = 1; i < W; ++i) u = Op::op(u, __builtin_bit_cast(typename Op::type, s[i]));
+    }
+    return u;
+}
+
+// Activation of a product's output.  A NaN (of a row that held one) stays one.
+__device__ __forceinline__ float act_keep_nan(float v, float hi) { return v != v ? v : act_clamp(v, hi); }
+
+// v -> round_half_even(v * inv) as the low byte of the result.  |v * inv| <= 127.5: adding 1.5 * 2^23 leaves the integer in the
+// low bits, rounded half to even.  The product is rounded by itself first (no fused multiply-add): that is the definition.
+__device__ __forceinline__ uint32_t quantize_bits(float v, float inv) {
+#pragma clang fp contract(off)
+    const float p = v * inv;
+    return __builtin_bit_cast(uint32_t, p + 12582912.0f);
+}
+// low bytes of four words
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
+    return lo | hi << 16;
+}
+constexpr float kQuantMin = 1e-36f;            // below it 127 / max|v| overflows: such a row is zeros
+// The scale of a row and what its values are multiplied with; bits: max|v| as bits
+__device__ __forceinline__ float quantize_scale(uint32_t bits, float* inv) {
+    const float amax = __builtin_bit_cast(float, bits);
+    *inv = 0.0f;
+    if (bits >= 0x7f800000u) return __builtin_nanf("");
+    if (amax < kQuantMin) return 0.0f;
+    *inv = 127.0f / amax;
+    return amax / 127.0f;
+}
+
+}  // namespace dcnn

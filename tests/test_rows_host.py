@@ -1,0 +1,42 @@
+"""Row operators: what can be checked without a GPU."""
+import ctypes as C
+
+import pytest
+
+import paper_2203_03996_amd as pkg
+from paper_2203_03996_amd.binding import RowsMatmulArgs, RowsNormArgs
+
+
+def test_sizes_of_packed_weights_and_scratch():
+    lib = pkg.load_library()
+    size = lib.dcnn_rows_weights_bytes
+    for k, n in ((1, 1), (64, 33), (128, 32), (129, 32), (4096, 4096), (65536, 100)):
+        need = -(-k // 128) * 128 * (-(-n // 32) * 32) + -(-n // 32) * 32 * 4      # 8-bit weights in whole blocks, a scale per channel
+        assert need <= size(k, n) < need + 256 and size(k, n) % 256 == 0
+    for k, n in ((0, 4), (4, 0), (-1, 4), (65537, 4), (4, (1 << 24) + 1)):
+        assert size(k, n) == 0 and lib.dcnn_rows_scratch_bytes(4, k, n) == 0
+    for rows, k in ((0, 64), (1, 1), (7, 65), (1000, 4096)):
+        assert lib.dcnn_rows_scratch_bytes(rows, k, 64) >= rows * (k + 4)
+    assert lib.dcnn_rows_scratch_bytes(-1, 64, 64) == 0
+
+
+def test_calls_without_a_context_are_refused():
+    lib = pkg.load_library()
+    assert lib.dcnn_rows_norm(None, C.byref(RowsNormArgs())) == 1
+    assert lib.dcnn_rows_matmul(None, C.byref(RowsMatmulArgs())) == 1 and lib.dcnn_rows_linear(None, C.byref(RowsMatmulArgs())) == 1
+    assert lib.dcnn_rows_pack(None, 0, 4, 4, None, 4, None, None, 0) == 1
+
+
+def test_layers_and_networks_keep_to_their_types():
+    """The types that only row operators take."""
+    from paper_2203_03996_amd.binding import LayerSizes
+    lib = pkg.load_library()
+    for dtype in (pkg.BF16, pkg.I8):
+        desc = pkg.make_desc(pkg.ACT, dtype, 2, 16, 16, 64, act=pkg.ACT_RELU)
+        assert lib.dcnn_layer_query(C.byref(desc), C.byref(LayerSizes())) == 3
+
+
+def test_norm_kinds():
+    assert pkg.RowNorm("rms").kind == 1 and pkg.RowNorm("layer").kind == 2 and pkg.RowNorm("none").kind == 0
+    with pytest.raises(KeyError):
+        pkg.RowNorm("batch")
