@@ -70,27 +70,28 @@ class Stats(C.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_ if name != "reserved"}
 
 
-class RowList(C.Structure):
-    _fields_ = [("rows", C.c_int64), ("map_rows", C.c_int64), ("idx", C.c_void_p), ("count", C.c_void_p)]
+# (nested members -- dcnn_row_list, dcnn_row_norm -- are spelled out: an attribute of a nested structure costs an object)
+_ROW_LIST = [("rows", C.c_int64), ("map_rows", C.c_int64), ("idx", C.c_void_p), ("count", C.c_void_p)]
 
 
-class RowNormStruct(C.Structure):
-    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("w", C.c_void_p), ("b", C.c_void_p)]
+def _row_norm(name):
+    return [(name + "_kind", C.c_int32), (name + "_eps", C.c_float), (name + "_w", C.c_void_p), (name + "_b", C.c_void_p)]
 
 
 class RowsNormArgs(C.Structure):
-    _fields_ = [("list", RowList), ("dtype", C.c_int32), ("c", C.c_int32), ("x", C.c_void_p), ("h", C.c_void_p),
-                ("gate", C.c_void_p), ("y", C.c_void_p), ("z", C.c_void_p), ("q", C.c_void_p), ("q_scale", C.c_void_p),
-                ("ldx", C.c_int64), ("ldh", C.c_int64), ("ldg", C.c_int64), ("ldy", C.c_int64), ("ldz", C.c_int64),
-                ("ldq", C.c_int64), ("gate_rows", C.c_int64), ("scale", C.c_float), ("post", RowNormStruct),
-                ("pre", RowNormStruct)]
+    _fields_ = _ROW_LIST + [
+        ("dtype", C.c_int32), ("c", C.c_int32), ("x", C.c_void_p), ("h", C.c_void_p), ("gate", C.c_void_p),
+        ("y", C.c_void_p), ("z", C.c_void_p), ("q", C.c_void_p), ("q_scale", C.c_void_p), ("ldx", C.c_int64),
+        ("ldh", C.c_int64), ("ldg", C.c_int64), ("ldy", C.c_int64), ("ldz", C.c_int64), ("ldq", C.c_int64),
+        ("gate_rows", C.c_int64), ("scale", C.c_float), ("_pad", C.c_int32)] + _row_norm("post") + _row_norm("pre")
 
 
 class RowsMatmulArgs(C.Structure):
-    _fields_ = [("list", RowList), ("dtype", C.c_int32), ("act", C.c_int32), ("k", C.c_int64), ("n", C.c_int64),
-                ("packed", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("q", C.c_void_p),
-                ("q_scale", C.c_void_p), ("ldq", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
-                ("pre", RowNormStruct), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+    _fields_ = _ROW_LIST + [
+        ("dtype", C.c_int32), ("act", C.c_int32), ("k", C.c_int64), ("n", C.c_int64), ("packed", C.c_void_p),
+        ("bias", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("q", C.c_void_p), ("q_scale", C.c_void_p),
+        ("ldq", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64)] + _row_norm("pre") + [
+        ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
 
 
 class DcnnError(RuntimeError):
@@ -195,6 +196,7 @@ class Context:
         nbytes = self.lib.dcnn_workspace_bytes(int(max_pixels)) if max_pixels > 0 else 0
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
         self.stream = torch.cuda.current_stream(self.device)
+        self.index, self._raw_stream = self.stream.device_index, self.stream.cuda_stream
         h = C.c_void_p()
         st = self.lib.dcnn_ctx_create(C.c_void_p(self.stream.cuda_stream), C.c_void_p(_ptr(self.workspace)),
                                       nbytes, C.byref(h))
@@ -252,7 +254,8 @@ class Context:
 
     def empty(self, shape, dtype):
         """An uninitialised device tensor that belongs to the context's stream, whichever stream torch is on."""
-        if torch.cuda.current_stream(self.device) == self.stream:
+        # (torch.cuda.current_stream builds an object, 3 us; the calls that allocate their outputs take 8 in all)
+        if torch._C._cuda_getCurrentRawStream(self.index) == self._raw_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
@@ -264,57 +267,63 @@ class Context:
         x and y are maps (last dimension c), the rest is [rows, c].  y, z, q: a tensor to write, True for a new one, or
         None where it is not wanted (q_scale: a tensor [rows], or None for a new one).  post, pre: RowNorm or None.
         Returns (y, z, q, q_scale)."""
-        t = x if x is not None else h
+        t = h if x is None else x
         if t is None:
             raise ValueError("rows_norm: neither x nor h")
-        c = t.shape[-1]
-        dt = t.dtype
+        c, dt, dev = t.shape[-1], t.dtype, self.index
         a = RowsNormArgs()
-        a.dtype, a.c, a.scale, a.gate_rows = _row_dtype(dt), c, scale, gate_rows
-        rows = idx.numel() if idx is not None else None
+        a.dtype, a.c, a.scale = _row_dtype(dt), c, scale
+        rows = map_rows = None
+        if idx is not None:
+            a.idx, rows = _int32(idx, "idx", dev), idx.numel()
+        if count is not None:
+            a.count = _int32(count, "count", dev)
         if x is not None:
-            x, a.ldx, n = _as_rows(x, "x", c, dt, self.device)
-            a.x, a.list.map_rows = x.data_ptr(), n
-            rows = n if rows is None else rows
+            a.x, a.ldx, map_rows = _as_rows(x, "x", c, dt, dev)
+            if rows is None:
+                rows = map_rows
         if h is not None:
-            h, a.ldh, n = _as_rows(h, "h", c, dt, self.device)
-            a.h = h.data_ptr()
-            rows = n if rows is None or (idx is not None and n < rows) else rows
-            if n < rows:
+            a.h, a.ldh, n = _as_rows(h, "h", c, dt, dev)
+            if rows is None or (n < rows and idx is not None):
+                rows = n
+            elif n < rows:
                 raise ValueError(f"rows_norm: h has {n} rows, {rows} are wanted")
-        if y is True:
-            y = self.empty(x.shape if x is not None else (rows, c), dt)
         if y is not None:
-            yr, a.ldy, n = _as_rows(y, "y", c, dt, self.device)
-            if x is not None and n != a.list.map_rows:
-                raise ValueError(f"rows_norm: x has {a.list.map_rows} rows, y {n}")
-            a.y, a.list.map_rows = yr.data_ptr(), n
+            if y is True:
+                y = self.empty((rows, c) if x is None else x.shape, dt)
+            a.y, a.ldy, n = _as_rows(y, "y", c, dt, dev)
+            if map_rows is not None and n != map_rows:
+                raise ValueError(f"rows_norm: x has {map_rows} rows, y {n}")
+            map_rows = n
         elif x is None:
-            a.list.map_rows = rows if idx is None else 0x7fffffff
+            map_rows = rows if idx is None else 0x7fffffff
         if gate is not None:
-            gate, a.ldg, n = _as_rows(gate if gate.dim() > 1 else gate[None], "gate", c, dt, self.device)
-            if n < (-(-a.list.map_rows // gate_rows) if gate_rows > 0 else 1):
-                raise ValueError(f"rows_norm: {n} rows of gate for {a.list.map_rows} map rows, {gate_rows} to each")
-            a.gate = gate.data_ptr()
-        if z is True:
-            z = self.empty((rows, c), dt)
+            a.gate, a.ldg, n = _as_rows(gate if gate.dim() > 1 else gate[None], "gate", c, dt, dev)
+            a.gate_rows = gate_rows
+            if n < (-(-map_rows // gate_rows) if gate_rows > 0 else 1):
+                raise ValueError(f"rows_norm: {n} rows of gate for {map_rows} map rows, {gate_rows} to each")
         if z is not None:
-            z, a.ldz, n = _as_rows(z, "z", c, dt, self.device)
-            rows = min(rows, n)
-            a.z = z.data_ptr()
-        if q is True:
-            q = self.empty((rows, -(-c // 16) * 16), torch.int8)[:, :c]
+            if z is True:
+                z = self.empty((rows, c), dt)
+                a.z, a.ldz = z.data_ptr(), c
+            else:
+                a.z, a.ldz, n = _as_rows(z, "z", c, dt, dev)
+                rows = min(rows, n)
         if q is not None:
-            q_scale = self.empty(rows, torch.float32) if q_scale is None else q_scale
-            a.ldq = _check_q(q, q_scale, c, self.device)
+            if q is True:
+                q = self.empty((rows, -(-c // 16) * 16), torch.int8)[:, :c]
+            if q_scale is None:
+                q_scale = self.empty(rows, torch.float32)
+            a.q, a.q_scale, a.ldq = _check_q(q, q_scale, c, dev)
             rows = min(rows, q.shape[0])
-            a.q, a.q_scale = q.data_ptr(), q_scale.data_ptr()
         if post is not None:
-            post.fill(a.post, c, dt, self.device)
+            a.post_kind, a.post_eps, a.post_w, a.post_b = post.pointers(c, dt, dev)
         if pre is not None:
-            pre.fill(a.pre, c, dt, self.device)
-        a.list.rows, a.list.idx, a.list.count = rows, _int32(idx, "idx", self.device), _int32(count, "count", self.device)
-        self.check(self.lib.dcnn_rows_norm(self.handle, C.byref(a)))
+            a.pre_kind, a.pre_eps, a.pre_w, a.pre_b = pre.pointers(c, dt, dev)
+        a.rows, a.map_rows = rows, map_rows
+        st = self.lib.dcnn_rows_norm(self.handle, a)
+        if st:
+            self.check(st)
         return y, z, q, q_scale
 
     def rows_quantize(self, x, *, pre=None, idx=None, count=None):
@@ -429,56 +438,57 @@ def _row_dtype(dt) -> int:
     return code
 
 
-def _as_rows(t, name, c, dt, device):
-    """(t as a matrix of c columns, its leading dimension, its rows); the ABI takes bare pointers, so shapes are checked here."""
+def _as_rows(t, name, c, dt, dev):
+    """(address, leading dimension, rows) of a tensor as a matrix of c columns; the ABI takes bare pointers, so shapes are checked here."""
     if t.dim() != 2:
         t = t.view(-1, t.shape[-1])
-    if t.shape[1] != c or t.dtype != dt or t.device.type != device.type or (c > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must hold rows of {c} {dt} side by side on {device}, got {tuple(t.shape)} {t.dtype} strides {t.stride()} "
+    n, cols = t.shape
+    ld, one = t.stride()
+    if cols != c or t.dtype != dt or t.get_device() != dev or (one != 1 and c > 1):
+        raise ValueError(f"{name} must hold rows of {c} {dt} side by side on GPU {dev}, got {tuple(t.shape)} {t.dtype} strides {t.stride()} "
                          f"on {t.device}")
-    n = t.shape[0]
-    ld = t.stride(0)
-    if n > 1 and ld < c:
+    if n <= 1:
+        ld = c
+    elif ld < c:
         raise ValueError(f"{name}: rows overlap (stride {ld}, {c} columns)")
-    return t, (ld if n > 1 else c), n
+    return t.data_ptr(), ld, n
 
 
-def _check_q(q, q_scale, c, device):
-    """Leading dimension of 8-bit rows."""
-    if q.dim() != 2 or q.shape[1] != c or q.dtype != torch.int8 or q.device.type != device.type or (c > 1 and q.stride(1) != 1):
+def _check_q(q, q_scale, c, dev):
+    """(address, address of the scales, leading dimension) of 8-bit rows."""
+    if q.dim() != 2 or q.shape[1] != c or q.dtype != torch.int8 or q.get_device() != dev or (c > 1 and q.stride(1) != 1):
         raise ValueError(f"q must be an int8 device matrix of {c} columns, got {tuple(q.shape)} {q.dtype} strides {q.stride()}")
-    if q_scale.dtype != torch.float32 or q_scale.numel() < q.shape[0] or not q_scale.is_contiguous() or q_scale.device.type != device.type:
-        raise ValueError(f"q_scale must hold {q.shape[0]} float32 numbers on the device")
     n, padded = q.shape[0], -(-c // 16) * 16
+    if q_scale.dtype != torch.float32 or q_scale.numel() < n or not q_scale.is_contiguous() or q_scale.get_device() != dev:
+        raise ValueError(f"q_scale must hold {n} float32 numbers on the device")
     ld = q.stride(0) if n > 1 else padded
-    if n and q.storage_offset() + (n - 1) * ld + padded > q.untyped_storage().nbytes():
+    if c != padded and n and q.storage_offset() + (n - 1) * ld + padded > q.untyped_storage().nbytes():
         raise ValueError("the last row of q does not fill its multiple of 16 bytes")
-    return ld
+    return q.data_ptr(), q_scale.data_ptr(), ld
 
 
-def _int32(t, name, device):
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device.type != device.type or (name == "count" and t.numel() != 1):
+def _int32(t, name, dev):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != dev or (name == "count" and t.numel() != 1):
         raise ValueError(f"{name} must be a contiguous int32 device tensor")
     return t.data_ptr()
 
 
 class RowNorm:
-    """Parameters of a norm over a row's channels: kind "rms" or "layer", weight and bias [c] (None: ones, zeros)."""
+    """A norm over a row's channels: kind "rms" or "layer", weight and bias [c] (None: ones, zeros), which it keeps."""
 
     def __init__(self, kind: str, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5):
         self.kind, self.weight, self.bias, self.eps = NORM_CODES[kind], weight, bias, float(eps)
+        self._fits = {(t.numel(), t.dtype, t.get_device()) for t in (weight, bias) if t is not None}
+        for t in (weight, bias):
+            if t is not None and (t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"a norm's parameters must be contiguous vectors, got {tuple(t.shape)} strides {t.stride()}")
+        self._pointers = (self.kind, self.eps, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr())
 
-    def fill(self, s: RowNormStruct, c: int, dt, device):
-        s.kind, s.eps = self.kind, self.eps
-        for name, t in (("w", self.weight), ("b", self.bias)):
-            if t is None:
-                setattr(s, name, None)
-                continue
-            if t.shape != (c,) or t.dtype != dt or t.device.type != device.type or not t.is_contiguous():
-                raise ValueError(f"a norm's parameters must be contiguous [{c}] {dt} on the device, got {tuple(t.shape)} {t.dtype}")
-            setattr(s, name, t.data_ptr())
+    def pointers(self, c: int, dt, dev):
+        """(kind, eps, address of the weight, address of the bias) for rows of c channels."""
+        if not self._fits <= {(c, dt, dev)}:
+            raise ValueError(f"a norm's parameters must be [{c}] {dt} on GPU {dev}, got {self._fits}")
+        return self._pointers
 
 
 class RowWeights:
@@ -503,47 +513,56 @@ class RowWeights:
         ctx.check(lib.dcnn_rows_pack(ctx.handle, code, k, n, weights.data_ptr(), weights.stride(0) if k > 1 else n, _ptr(scale),
                                      self.packed.data_ptr(), nbytes))
         self._source = weights                                    # until the stream has read it
-        self._scratch = None
-        self._args = a = RowsMatmulArgs()
-        a.k, a.n, a.act, a.packed = k, n, ACT_CODES[act], self.packed.data_ptr()
         if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
             raise ValueError(f"bias must be a contiguous device tensor [{n}]")
-        a.bias = _ptr(bias)
+        self.act, self._bias = ACT_CODES[act], _ptr(bias) or None
+        self._scratch, self._scratch_bytes, self._scratch_rows = None, 0, -1
 
-    def _call(self, call, rows, dt, count, out):
-        ctx, a = self.ctx, self._args
+    def _call(self, call, a, rows, dt, count, out):
+        ctx = self.ctx
         if self.bias is not None and self.bias.dtype != dt:
             raise ValueError(f"the bias is {self.bias.dtype}, the output {dt}")
-        a.dtype = _row_dtype(dt)
+        a.dtype, a.k, a.n, a.act, a.packed, a.bias = _row_dtype(dt), self.k, self.n, self.act, self.packed.data_ptr(), self._bias
+        if count is not None:
+            a.count = _int32(count, "count", ctx.index)
         if out is None:
             out = ctx.empty((rows, self.n), dt)
-        o, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.device)
-        a.list.rows, a.list.count, a.y = min(rows, n), _int32(count, "count", ctx.device), o.data_ptr()
-        need = ctx.lib.dcnn_rows_scratch_bytes(a.list.rows, self.k, self.n)
-        if self._scratch is None or self._scratch.numel() < need:
-            with torch.cuda.stream(ctx.stream):
-                self._scratch = torch.zeros(max(need, 256), dtype=torch.uint8, device=ctx.device)
-        a.scratch, a.scratch_bytes = self._scratch.data_ptr(), self._scratch.numel()
-        ctx.check(call(ctx.handle, C.byref(a)))
+            a.y, a.ldy = out.data_ptr(), self.n
+        else:
+            a.y, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.index)
+            rows = min(rows, n)
+        a.rows = rows
+        if rows > self._scratch_rows:
+            self._grow(rows)
+        a.scratch, a.scratch_bytes = self._scratch.data_ptr(), self._scratch_bytes
+        st = call(ctx.handle, a)
+        if st:
+            ctx.check(st)
         return out
+
+    def _grow(self, rows):
+        """Scratch for up to this many rows."""
+        self._scratch_bytes = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n)
+        with torch.cuda.stream(self.ctx.stream):
+            self._scratch = torch.zeros(self._scratch_bytes, dtype=torch.uint8, device=self.ctx.device)
+        self._scratch_rows = rows
 
     def matmul(self, q, q_scale, *, dtype=torch.float16, count=None, out=None):
         """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`."""
-        a = self._args
-        a.ldq = _check_q(q, q_scale, self.k, self.ctx.device)
-        a.q, a.q_scale, a.x, a.list.idx, a.list.map_rows = q.data_ptr(), q_scale.data_ptr(), None, None, 0
-        return self._call(self.ctx.lib.dcnn_rows_matmul, q.shape[0], dtype, count, out)
+        a = RowsMatmulArgs()
+        a.q, a.q_scale, a.ldq = _check_q(q, q_scale, self.k, self.ctx.index)
+        return self._call(self.ctx.lib.dcnn_rows_matmul, a, q.shape[0], dtype, count, out)
 
     def linear(self, x, *, pre=None, idx=None, count=None, out=None):
         """dcnn_rows_linear: rows of the map x (those that idx names), normed with `pre`, quantised and multiplied; [rows, n]."""
-        a = self._args
-        x, a.ldx, n = _as_rows(x, "x", self.k, x.dtype, self.ctx.device)
-        a.q, a.q_scale, a.x, a.list.map_rows, a.list.idx = None, None, x.data_ptr(), n, _int32(idx, "idx", self.ctx.device)
+        a, dt, dev = RowsMatmulArgs(), x.dtype, self.ctx.index
+        a.x, a.ldx, rows = _as_rows(x, "x", self.k, dt, dev)
+        a.map_rows = rows
+        if idx is not None:
+            a.idx, rows = _int32(idx, "idx", dev), idx.numel()
         if pre is not None:
-            pre.fill(a.pre, self.k, x.dtype, self.ctx.device)
-        else:
-            a.pre.kind = 0
-        return self._call(self.ctx.lib.dcnn_rows_linear, n if idx is None else idx.numel(), x.dtype, count, out)
+            a.pre_kind, a.pre_eps, a.pre_w, a.pre_b = pre.pointers(self.k, dt, dev)
+        return self._call(self.ctx.lib.dcnn_rows_linear, a, rows, dt, count, out)
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

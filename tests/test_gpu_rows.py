@@ -619,9 +619,9 @@ def test_c_refusals(ctx):
 
     def norm(**kw):
         a = RowsNormArgs(c=64, x=p, z=o, ldx=64, ldz=64, scale=1.0)
-        a.list.rows = a.list.map_rows = 4
+        a.rows = a.map_rows = 4
         for k, v in kw.items():
-            setattr(a.list if k in ("rows", "map_rows", "idx", "count") else a, k, v)
+            setattr(a, k, v)
         return lib.dcnn_rows_norm(ctx.handle, C.byref(a))
     assert norm(dtype=3) == 3 and norm(dtype=-1) == 3 and norm(dtype=9) == 3
     assert norm(c=0) == 1 and norm(c=32769) == 7 and norm(rows=-1) == 1 and norm(rows=1 << 31) == 1 and norm(rows=5) == 2 and norm(map_rows=-1) == 1
@@ -648,13 +648,13 @@ def test_c_refusals(ctx):
 
     def product(linear, **kw):
         a = RowsMatmulArgs(k=64, n=64, packed=packed, y=o, ldy=64, scratch=scratch.data_ptr(), scratch_bytes=scratch.numel())
-        a.list.rows = a.list.map_rows = 4
+        a.rows = a.map_rows = 4
         if linear:
             a.x, a.ldx = p, 64
         else:
             a.q, a.q_scale, a.ldq = q.data_ptr(), ws.data_ptr(), 64
         for k, v in kw.items():
-            setattr(a.list if k in ("rows", "map_rows", "idx", "count") else a, k, v)
+            setattr(a, k, v)
         return (lib.dcnn_rows_linear if linear else lib.dcnn_rows_matmul)(ctx.handle, C.byref(a))
     for linear in (False, True):
         assert product(linear, dtype=3) == 3 and product(linear, act=3) == 1 and product(linear, k=0) == 1 and product(linear, n=0) == 1 and product(linear, n=1 << 25) == 1

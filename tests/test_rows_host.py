@@ -40,3 +40,37 @@ def test_norm_kinds():
     assert pkg.RowNorm("rms").kind == 1 and pkg.RowNorm("layer").kind == 2 and pkg.RowNorm("none").kind == 0
     with pytest.raises(KeyError):
         pkg.RowNorm("batch")
+
+
+def test_argument_blocks_have_the_layout_of_the_header(tmp_path):
+    """The binding spells nested members out: sizes and offsets against a C compiler's."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = {RowsNormArgs: "dcnn_rows_norm_args", RowsMatmulArgs: "dcnn_rows_matmul_args"}
+    plain = {"post": "post.", "pre": "pre."}
+    lines, want = [], []
+    for cls, name in names.items():
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        want.append(C.sizeof(cls))
+        for field, _ in cls._fields_:
+            if field == "_pad":
+                continue
+            first = field.split("_")[0]
+            member = field
+            if field in ("rows", "map_rows"):
+                member = "list." + field
+            elif field in ("idx", "count"):
+                member = f"list.{field}_dev"
+            elif first in plain and field != first:
+                rest = field[len(first) + 1:]
+                member = plain[first] + (rest + "_dev" if rest in ("w", "b") else rest)
+            elif getattr(cls, field).size == 8 and field in ("x", "h", "gate", "y", "z", "q", "q_scale", "packed", "bias", "scratch"):
+                member = field + "_dev"
+            lines.append(f'printf("%zu\\n", offsetof({name}, {member}));')
+            want.append(getattr(cls, field).offset)
+    src = tmp_path / "layout.c"
+    src.write_text(f'#include <stdio.h>\n#include "{root}/include/deltacnn.h"\nint main(void) {{ {" ".join(lines)} return 0; }}\n')
+    subprocess.run(["gcc", str(src), "-o", str(tmp_path / "layout")], check=True)
+    got = subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True, check=True).stdout.split()
+    assert [int(v) for v in got] == want
