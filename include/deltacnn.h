@@ -321,7 +321,7 @@ typedef struct {
     const void*   gate_dev;     /* [ceil(map_rows / gate_rows), c]                      */
     void*         y_dev;        /* map                                                 */
     void*         z_dev;        /* compact                                             */
-    int8_t*       q_dev;        /* compact; 16-byte aligned, ldq a multiple of 16.  Bytes c .. of a row's last 16 may be overwritten */
+    int8_t*       q_dev;        /* compact; 16-byte aligned, ldq a multiple of 16 and at most 2^22.  Bytes c .. of a row's last 16 may be overwritten */
     float*        q_scale_dev;  /* [rows]                                              */
     int64_t       ldx, ldh, ldg, ldy, ldz, ldq;
     int64_t       gate_rows;    /* map rows that share a row of gate; 0: all of them    */
@@ -353,7 +353,7 @@ typedef struct {
     const void*   bias_dev;     /* [n] or NULL                                         */
     void*         y_dev;        /* [rows, n] compact                                   */
     int64_t       ldy;
-    const int8_t* q_dev;        /* matmul: [rows, k], 16-byte aligned, ldq a multiple of 16 (the bytes behind k may hold anything) */
+    const int8_t* q_dev;        /* matmul: [rows, k], aligned and spaced as in dcnn_rows_norm_args (the bytes behind k may hold anything) */
     const float*  q_scale_dev;  /* matmul: [rows]                                      */
     int64_t       ldq;
     const void*   x_dev;        /* linear: map [map_rows, k]; k <= 32768                */

@@ -5,6 +5,8 @@ using namespace dcnn;
 
 namespace {
 
+constexpr int64_t kLdqMax = 1 << 22;       // 8-bit rows of a tile are addressed in 32 bits
+
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 dcnn_status check_list(dcnn_ctx* ctx, const char* what, const dcnn_row_list& l) {
@@ -29,6 +31,7 @@ dcnn_status check_ld(dcnn_ctx* ctx, const char* what, const char* name, const vo
 dcnn_status check_q(dcnn_ctx* ctx, const char* what, const void* q, const void* scale, int64_t ld, int64_t c) {
     if (q == nullptr || scale == nullptr) return fail(ctx, DCNN_EINVAL, "%s: 8-bit rows need q and q_scale", what);
     if (!aligned(q, 16) || ld % 16 != 0) return fail(ctx, DCNN_EINVAL, "%s: 8-bit rows must start at multiples of 16 bytes (ldq %lld)", what, (long long)ld);
+    if (ld > kLdqMax) return fail(ctx, DCNN_EUNSUPPORTED, "%s: 8-bit rows %lld bytes apart", what, (long long)ld);
     if (!aligned(scale, 4)) return fail(ctx, DCNN_EINVAL, "%s: q_scale not 4-byte aligned", what);
     return check_ld(ctx, what, "q", q, ld, c, 1);
 }
@@ -184,6 +187,7 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     a.q_scale = reinterpret_cast<float*>(scratch);
     a.q = reinterpret_cast<int8_t*>(scratch + scratch_rows_offset(p->list.rows)), a.ldq = (int)scratch_ldq(p->k);
     set_norm(p->pre, &a.pre, &a.pre_eps, &a.pre_w, &a.pre_b);
+    if (rows_linear_fuses(p->dtype, p->list.rows, p->k)) return launch_rows_linear_few(ctx, p->dtype, a, m);
     st = launch_rows_norm(ctx, p->dtype, a);
     if (st != DCNN_OK) return st;
     m.q = a.q, m.q_scale = a.q_scale, m.ldq = a.ldq;

@@ -19,6 +19,10 @@ template <> struct RowVec<bf16> { static constexpr int E = 8; typedef bf16 type 
 // Four consecutive outputs.
 template <typename T> struct RowQuad { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 
+// The same in LDS, where they are aligned.
+template <typename T> using AlignedVec = T __attribute__((ext_vector_type(16 / sizeof(T))));
+template <typename T> using AlignedQuad = T __attribute__((ext_vector_type(4)));
+
 // Rows of this call, read on the GPU where a list's length is.
 __device__ __forceinline__ int row_count(const int32_t* count, int rows) {
     if (count == nullptr) return rows;
@@ -66,8 +70,32 @@ template <typename Op, int L> __device__ __forceinline__ typename Op::type row_r
     return u;
 }
 
-// Activation of a product's output.  A NaN (of a row that held one) stays one.
-__device__ __forceinline__ float act_keep_nan(float v, float hi) { return v != v ? v : act_clamp(v, hi); }
+// Activation of a product's outputs.  A NaN (of a row that held one) stays one: no comparison with it holds.
+__device__ __forceinline__ void act_keep_nan(float (&v)[4], int act, float hi) {
+    if (act == DCNN_ACT_NONE) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = v[e] < 0.0f ? 0.0f : v[e];
+        v[e] = v[e] > hi ? hi : v[e];
+    }
+}
+
+// Four channels of a bias, zero where there is none.
+template <typename T> __device__ __forceinline__ f32x4 load_bias(const void* bias, int ch, int n) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    const T* b = static_cast<const T*>(bias);
+    if (b == nullptr || ch >= n) return v;
+    if (ch + 4 <= n) {
+        const typename RowQuad<T>::type q = *reinterpret_cast<const typename RowQuad<T>::type*>(b + ch);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)q[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < n) v[e] = (float)b[ch + e];
+    }
+    return v;
+}
 
 // v -> round_half_even(v * inv) as the low byte of the result.  |v * inv| <= 127.5: adding 1.5 * 2^23 leaves the integer in the
 // low bits, rounded half to even.  The product is rounded by itself first (no fused multiply-add): that is the definition.
@@ -90,6 +118,93 @@ __device__ __forceinline__ float quantize_scale(uint32_t bits, float* inv) {
     if (amax < kQuantMin) return 0.0f;
     *inv = 127.0f / amax;
     return amax / 127.0f;
+}
+
+// ---- rows in registers ----------------------------------------------------------------------------------------------
+// 16 bytes of a row of c elements from element `base` on; what lies behind the row is zero.
+template <typename T> __device__ __forceinline__ typename RowVec<T>::type row_load(const T* row, int base, int c) {
+    constexpr int E = RowVec<T>::E;
+    typename RowVec<T>::type v;
+    if (base + E <= c) return *reinterpret_cast<const typename RowVec<T>::type*>(row + base);
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = base + e < c ? row[base + e] : (T)0.0f;
+    return v;
+}
+template <typename T> __device__ __forceinline__ void row_store(T* row, int base, int c, const float* o) {
+    constexpr int E = RowVec<T>::E;
+    typename RowVec<T>::type v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = (T)o[e];
+    if (base + E <= c) {
+        *reinterpret_cast<typename RowVec<T>::type*>(row + base) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (base + e < c) row[base + e] = v[e];
+    }
+}
+
+// v <- norm(v); elements behind the row's end are zero before and after.
+template <typename T, int L, int NV>
+__device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const T* w, const T* b, int lane, int c, float inv_c,
+                                         uint32_t* red, int& turn) {
+    constexpr int E = RowVec<T>::E;
+    typename RowVec<T>::type wv[NV], bv[NV];
+    if (w != nullptr) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) wv[j] = row_load<T>(w, (j * L + lane) * E, c);
+    }
+    if (b != nullptr) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) bv[j] = row_load<T>(b, (j * L + lane) * E, c);
+    }
+    float mean = 0.0f;
+    if (kind == DCNN_NORM_LAYER) {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += v[j][e];
+        mean = row_reduce<SumOp, L>(s, red, turn) * inv_c;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int left = c - (j * L + lane) * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[j][e] = e < left ? v[j][e] - mean : 0.0f;
+            s += v[j][e] * v[j][e];
+        }
+    }
+    const float r = 1.0f / sqrtf(row_reduce<SumOp, L>(s, red, turn) * inv_c + eps);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[j][e] *= r;
+            if (w != nullptr) v[j][e] *= (float)wv[j][e];
+            if (b != nullptr) v[j][e] += (float)bv[j][e];
+        }
+}
+
+// A row's largest magnitude, as bits, over its lanes.
+template <int L, int NV, int E> __device__ __forceinline__ uint32_t row_amax(const float (&v)[NV][E], uint32_t* red, int& turn) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu);
+    return row_reduce<MaxOp, L>(m, red, turn);
+}
+// E values in 8 bits at p.
+template <int E> __device__ __forceinline__ void store_quantized(int8_t* p, const float (&v)[E], float inv) {
+    uint32_t word[E / 4];
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+        word[e / 4] = inv == 0.0f ? 0u : pack_bytes(quantize_bits(v[e], inv), quantize_bits(v[e + 1], inv), quantize_bits(v[e + 2], inv), quantize_bits(v[e + 3], inv));
+    if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(word[0], word[1]);
+    else *reinterpret_cast<uint32_t*>(p) = word[0];
 }
 
 }  // namespace dcnn

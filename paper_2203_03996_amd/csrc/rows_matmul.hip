@@ -66,143 +66,465 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------
-// A workgroup of TW x CW waves computes TW*FT*32 rows by CW*FC*32 channels, K-tiles of 128 at a time.  A K-tile of both operands is
-// staged through registers into one of two LDS buffers while the other is multiplied.  Weights lie in LDS as they are packed
-// (an operand load of a wave is 1 KB in a row); a row's eight chunks of 16 k are exchanged by the low bits of its number, so
-// that the lanes of an operand load, 32 rows at one k, start on different banks.  The channels are the matrix cores' rows and
-// the tokens their columns: a lane ends with four consecutive channels of one token.
-template <typename T, int TW, int CW, int FT, int FC> struct TileShape {
-    static constexpr int threads = TW * CW * kWave, tokens = TW * FT * 32, channels = CW * FC * 32;
-    static constexpr int stage = (tokens + channels) * kPackK;
+// A workgroup of TW x CW waves computes TW*FT*32 rows by CW*FC*32 channels over K-tiles of 128.  The channels are the matrix cores' rows
+// and the tokens their columns: a lane ends with four consecutive channels of one token.
+//
+// K-tiles go from memory straight into one of NB LDS buffers, NB - 1 K-tiles ahead of their use, the first ones of the workgroup's next
+// tile behind the last ones of this; the operands of a step of 32 k are read from LDS one step ahead, the first ones of the next K-tile
+// behind the one barrier, which stands a step before the tile's end.  So the matrix cores wait neither for memory nor for LDS.
+// Weights lie in LDS as they are packed (an operand load of a wave is 1 KB in a row).  A row's eight chunks of 16 k are exchanged by bits
+// of its number: the 16 lanes of a quarter of an operand load, 16 rows at one k, then cover all 64 banks.
+//
+// The sums leave through LDS, a wave's 32 tokens by 128 bytes at a time: pieces of rows, 16 bytes a lane, where the matrix cores' order
+// would store 16 bytes from 32 rows.
+constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
+template <typename T, int TW, int CW, int FT, int FC, int NB> struct TileShape {
+    static constexpr int waves = TW * CW, threads = waves * kWave, tokens = TW * FT * 32, channels = CW * FC * 32;
+    static constexpr int row = FC * 32 * (int)sizeof(T) < 128 ? FC * 32 * (int)sizeof(T) : 128;      // bytes of a token on their way out
+    static constexpr int stage = (tokens + channels) * kPackK, unit = 32 * row, lds = NB * stage + waves * unit;
 };
+__device__ __forceinline__ int chunk_swizzle(int row) { return (row >> 1) & 7; }
 
-template <typename T, int TW, int CW, int FT, int FC>
-__global__ __launch_bounds__(TW * CW * kWave) void rows_matmul_kernel(MatmulArgs a) {
-    using S = TileShape<T, TW, CW, FT, FC>;
-    constexpr int CH = kPackK / 16;                            // chunks of a row of a K-tile
-    constexpr int QL = S::tokens * CH / S::threads, WL = S::channels * CH / S::threads;
-    extern __shared__ __align__(16) int8_t lds[];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+// Tiles in the order that workgroups take them: four rows of tiles side by side, so that the tiles in work on an XCD share what its L2 holds.
+struct TileAt { int t, c; };
+__device__ __forceinline__ TileAt tile_at(int tile, int tiles_t, int tiles_c) {
+    const int group = tile / (4 * tiles_c), first = group * 4, size = tiles_t - first < 4 ? tiles_t - first : 4;
+    const int r = tile - group * 4 * tiles_c;
+    return {first + r % size, r / size};
+}
+
+// 16 bytes a lane from memory to 1 KB of LDS, in the order of the lanes.
+__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, int offset, int uniform, int8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, uniform, 0, 0);
+}
+// at most N loads of this wave still on their way
+template <int N> __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70); }
+
+// All waves are here, and what they have read from LDS is in their registers.  (A fence would wait for the copies into LDS as well.)
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);                        // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int I> using Int = std::integral_constant<int, I>;
+template <int N, int I = 0, typename F> __device__ __forceinline__ void unrolled(F&& f) {
+    if constexpr (I < N) {
+        f(Int<I>{});
+        unrolled<N, I + 1>(f);
+    }
+}
+
+template <typename T, int TW, int CW, int FT, int FC, int NB>
+__global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a) {
+    using S = TileShape<T, TW, CW, FT, FC, NB>;
+    constexpr int QL = S::tokens / 8 / S::waves, WL = S::channels / 8 / S::waves;        // copies of 1 KB per K-tile and wave
+    static_assert(S::threads >= S::channels && S::threads >= S::tokens && (2 * S::channels + S::tokens) * 4 <= S::waves * S::unit, "a thread for each factor");
+    static_assert(QL * 8 * S::waves == S::tokens && WL * 8 * S::waves == S::channels, "whole rounds of copies");
+    // (an array each: what is read from one buffer does not wait for copies into the others)
+    __shared__ __align__(1024) int8_t buf0[S::stage], buf1[S::stage], buf2[NB > 2 ? S::stage : 16], buf3[NB > 3 ? S::stage : 16],
+        buf4[NB > 4 ? S::stage : 16], buf5[NB > 5 ? S::stage : 16], out_lds[S::waves * S::unit];
+    static_assert(NB >= 2 && NB <= 6, "an array for each buffer");
+    auto buffer = [&](auto i) -> int8_t* {
+        constexpr int I = decltype(i)::value % NB;
+        if constexpr (I == 0) return buf0;
+        else if constexpr (I == 1) return buf1;
+        else if constexpr (I == 2) return buf2;
+        else if constexpr (I == 3) return buf3;
+        else if constexpr (I == 4) return buf4;
+        else return buf5;
+    };
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int tw = wave / CW, cw = wave % CW;
-    const int count = row_count(a.count, a.rows);
+    const int count = row_count(a.count, a.rows), kts = a.kt;
     const int tiles_t = (count + S::tokens - 1) / S::tokens, tiles_c = (a.n + S::channels - 1) / S::channels;
     const int blocks_c = (a.n + kPackC - 1) / kPackC;
-    const int q_row = tid / CH, q_chunk = (tid % CH) ^ (q_row % CH);       // rows tid/8 + i*threads/8: the same low bits
-    const int w_ch = tid % kPackC, w_k = tid / kPackC % CH, w_block = tid / (kPackC * CH);
-    constexpr int w_step = S::threads / (kPackC * CH);
-    static_assert(S::threads % (kPackC * CH) == 0, "a round of loads is whole blocks of packed weights");
-    const int64_t w_block_bytes = (int64_t)a.kt * kPackK * kPackC;
+    const int w_block_bytes = kts * kPackK * kPackC;           // 2 MB at most
     const WgTileRange range = wg_tile_range((int64_t)tiles_t * tiles_c);
-    for (int64_t tile = range.begin; tile < range.end; tile += range.step) {
-        const int t0 = (int)(tile / tiles_c) * S::tokens, c0 = (int)(tile % tiles_c) * S::channels;
-        const int8_t* q_at[QL];
-        const int8_t* w_at[WL];
+    if (range.begin >= range.end) return;
+
+    // of the tile that is being copied: rows behind the last one read the last one, blocks behind the last one the last one
+    __amdgpu_buffer_rsrc_t q_tile, w_tile;
+    int q_at[QL], w_at[WL];
+    auto aim = [&](int64_t tile) {
+        const TileAt at = tile_at((int)tile, tiles_t, tiles_c);
+        const int t0 = at.t * S::tokens, b0 = at.c * (S::channels / kPackC);
+        q_tile = ws_rsrc(a.q + (int64_t)t0 * a.ldq, kWsMaxBytes);
+        w_tile = ws_rsrc(a.w + (int64_t)b0 * w_block_bytes, kWsMaxBytes);
 #pragma unroll
-        for (int i = 0; i < QL; ++i) {                         // rows behind the last one read the last one
-            const int row = t0 + q_row + i * (S::threads / CH);
-            q_at[i] = a.q + (int64_t)(row < count ? row : count - 1) * a.ldq;
+        for (int i = 0; i < QL; ++i) {
+            const int row = (i * S::waves + wave) * 8 + lane / 8;
+            q_at[i] = (row < count - t0 ? row : count - t0 - 1) * a.ldq;
         }
 #pragma unroll
         for (int i = 0; i < WL; ++i) {
-            const int block = c0 / kPackC + w_block + i * w_step;
-            w_at[i] = a.w + (block < blocks_c ? block : blocks_c - 1) * w_block_bytes + (w_k * kPackC + w_ch) * 16;
+            const int j = i * S::waves + wave, block = j / 4;
+            w_at[i] = (block < blocks_c - b0 ? block : blocks_c - b0 - 1) * w_block_bytes + j % 4 * 1024 + lane * 16;
         }
-        u32x4 qv[QL], wv[WL];
-        auto load = [&](int kt) {
-            const int chunk = kt * CH + q_chunk;               // chunks behind a row's last one: any, their weights are zero
-            const int at = (chunk < a.kc ? chunk : 0) * 16;
+    };
+    // (rows 8 on: their low bits are the same but for one)
+    const int q_chunk[2] = {lane % 8 ^ chunk_swizzle(lane / 8), lane % 8 ^ chunk_swizzle(lane / 8 + 8)};
+    auto copy = [&](int8_t* buf, int kt) {
+        int at[2];
 #pragma unroll
-            for (int i = 0; i < QL; ++i) qv[i] = *reinterpret_cast<const u32x4*>(q_at[i] + at);
+        for (int i = 0; i < 2; ++i) {                          // chunks behind a row's last one: any, their weights are zero
+            const int chunk = kt * kChunks + q_chunk[i];
+            at[i] = (chunk < a.kc ? chunk : 0) * 16;
+        }
 #pragma unroll
-            for (int i = 0; i < WL; ++i) wv[i] = *reinterpret_cast<const u32x4*>(w_at[i] + (int64_t)kt * (kPackK * kPackC));
-        };
-        auto stage = [&](int buf) {
-            int8_t* s = lds + buf * S::stage;
+        for (int i = 0; i < QL; ++i) {
+            const int rows = (i * S::waves + wave) * 8;
+            copy_to_lds(q_tile, q_at[i] + (S::waves % 2 == 0 ? (wave % 2 ? at[1] : at[0]) : (rows / 8 % 2 ? at[1] : at[0])), 0, buf + rows * kPackK);
+        }
 #pragma unroll
-            for (int i = 0; i < QL; ++i) *reinterpret_cast<u32x4*>(s + (tid + i * S::threads) * 16) = qv[i];
-            s += S::tokens * kPackK;
+        for (int i = 0; i < WL; ++i) copy_to_lds(w_tile, w_at[i], kt * (kPackK * kPackC), buf + S::tokens * kPackK + (i * S::waves + wave) * 1024);
+    };
+    i32x4 qf[2][FT], wf[2][FC];
+    // (32 rows on, the low bits that exchange chunks are the same)
+    const int q_lane = (tw * FT * 32 + lane % 32) * kPackK + (lane / 32 ^ chunk_swizzle(lane % 32)) * 16;
+    const int w_lane = S::tokens * kPackK + cw * FC * (kPackK * kPackC) + lane * 16;
+    auto operands = [&](int8_t* buf, int ks) {
 #pragma unroll
-            for (int i = 0; i < WL; ++i) *reinterpret_cast<u32x4*>(s + (tid + i * S::threads) * 16) = wv[i];
-        };
-        i32x16 acc[FT][FC] = {};
-        load(0);
-        stage(0);
-        __syncthreads();
-        for (int kt = 0; kt < a.kt; ++kt) {
-            if (kt + 1 < a.kt) load(kt + 1);
-            const int8_t* s = lds + (kt & 1) * S::stage;
+        for (int t = 0; t < FT; ++t) qf[ks % 2][t] = *reinterpret_cast<const i32x4*>(buf + (q_lane ^ ks * 32) + t * (32 * kPackK));
 #pragma unroll
-            for (int ks = 0; ks < kPackK / 32; ++ks) {
-                i32x4 qf[FT], wf[FC];
-                const int chunk = 2 * ks + lane / 32;
+        for (int f = 0; f < FC; ++f) wf[ks % 2][f] = *reinterpret_cast<const i32x4*>(buf + w_lane + f * (kPackK * kPackC) + ks * 1024);
+    };
+    i32x16 acc[FT][FC];
+    auto multiply = [&](int ks) {
 #pragma unroll
-                for (int t = 0; t < FT; ++t) {
-                    const int row = (tw * FT + t) * 32 + lane % 32;
-                    qf[t] = *reinterpret_cast<const i32x4*>(s + row * kPackK + (chunk ^ (row % CH)) * 16);
-                }
+        for (int t = 0; t < FT; ++t)
 #pragma unroll
-                for (int f = 0; f < FC; ++f)
-                    wf[f] = *reinterpret_cast<const i32x4*>(s + S::tokens * kPackK + ((cw * FC + f) * CH + chunk) * (kPackC * 16) + lane % 32 * 16);
+            for (int f = 0; f < FC; ++f) acc[t][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[ks % 2][f], qf[ks % 2][t], acc[t][f], 0, 0, 0);
+    };
+    int64_t ahead = range.begin;                               // the tile whose K-tiles are copied
+    auto wait_but = [&](int tiles) {                           // until all but the last so many copied K-tiles have arrived
+        unrolled<NB>([&](auto i) {
+            constexpr int J = NB - 1 - decltype(i)::value;
+            if (tiles == J) wait_loads<J * (QL + WL)>();
+        });
+    };
+    int arrived;                                               // of this workgroup's tile, before it began
+    // K-tile kt of this workgroup's tile lies in `buf`, kt + 1 in `next`.
+    auto k_tile = [&](int kt, int8_t* buf, int8_t* next) {
 #pragma unroll
-                for (int t = 0; t < FT; ++t)
-#pragma unroll
-                    for (int f = 0; f < FC; ++f) acc[t][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[f], qf[t], acc[t][f], 0, 0, 0);
+        for (int ks = 0; ks < kSteps - 1; ++ks) {
+            operands(buf, ks + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(ks);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kt + 1 >= arrived) {                               // K-tile kt + 1: those behind it may be on their way
+            const int behind = ahead < range.end ? NB - 2 : kts - 2 - kt;
+            if (behind >= NB - 2) wait_loads<(NB - 2) * (QL + WL)>();
+            else wait_but(behind > 0 ? behind : 0);
+        }
+        meet();
+        operands(next, 0);                                     // (behind a tile's last K-tile: anything, nobody uses it)
+        int from = kt + NB;
+        if (from >= kts) {                                     // the next tile's K-tile of this buffer
+            if (from == kts || (kts < NB && kt == 0)) {
+                ahead += range.step;
+                if (ahead < range.end) aim(ahead);
             }
-            if (kt + 1 < a.kt) stage((kt + 1) & 1);
-            __syncthreads();
+            from = kt % NB;
         }
-        const float hi = act_hi(a.act);
+        if (ahead < range.end) copy(buf, from);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(kSteps - 1);
+    };
+    aim(ahead);
+    unrolled<NB>([&](auto i) {
+        if (decltype(i)::value < kts) copy(buffer(i), decltype(i)::value);
+    });
+    wait_but((kts < NB ? kts : NB) - 1);
+    arrived = 1;
+    meet();
+    operands(buf0, 0);
+    const float hi = act_hi(a.act);
+    for (int64_t tile = range.begin; tile < range.end; tile += range.step) {
+        const TileAt at = tile_at((int)tile, tiles_t, tiles_c);
+        const int t0 = at.t * S::tokens, c0 = at.c * S::channels;
 #pragma unroll
-        for (int t = 0; t < FT; ++t) {
-            const int row = t0 + (tw * FT + t) * 32 + lane % 32;
-            if (row >= count) continue;
-            const float rs = a.q_scale[row];
-            T* y = static_cast<T*>(a.y) + (int64_t)row * a.ldy;
+        for (int t = 0; t < FT; ++t)
 #pragma unroll
-            for (int f = 0; f < FC; ++f)
+            for (int f = 0; f < FC; ++f) acc[t][f] = i32x16{};
+        // what the sums are scaled with: a channel's and a row's by each thread, dealt out when the sums are there
+        const int my_ch = c0 + (int)threadIdx.x, my_row = t0 + (int)threadIdx.x;
+        float my_ws = 0.0f, my_bias = 0.0f, my_rs = 0.0f;
+        if ((int)threadIdx.x < S::channels && my_ch < a.n) {
+            my_ws = a.w_scale[my_ch];
+            if (a.bias != nullptr) my_bias = (float)static_cast<const T*>(a.bias)[my_ch];
+        }
+        if ((int)threadIdx.x < S::tokens && my_row < count) my_rs = a.q_scale[my_row];
+        int kt = 0;
+#pragma clang loop unroll(disable)
+        for (; kt + NB <= kts; kt += NB)
+            unrolled<NB>([&](auto i) { k_tile(kt + decltype(i)::value, buffer(i), buffer(Int<decltype(i)::value + 1>{})); });
+        unrolled<NB - 1>([&](auto i) {
+            if (kt + decltype(i)::value < kts) k_tile(kt + decltype(i)::value, buffer(i), buffer(Int<decltype(i)::value + 1>{}));
+        });
+        arrived = NB;
+        wait_loads<0>();                                       // the next tile's first K-tiles have arrived, ...
+        float* const factors = reinterpret_cast<float*>(out_lds);
+        if ((int)threadIdx.x < S::channels) {
+            factors[threadIdx.x] = my_ws;
+            factors[S::channels + threadIdx.x] = my_bias;
+        }
+        if ((int)threadIdx.x < S::tokens) factors[2 * S::channels + threadIdx.x] = my_rs;
+        meet();                                                // ... everybody's
+        f32x4 ws[FC][4], bias[FC][4];
+        float rs[FT];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int ch = c0 + (cw * FC + f) * 32 + g * 8 + lane / 32 * 4;
-                    if (ch >= a.n) continue;
-                    // (the channel scales are padded to whole blocks)
-                    const f32x4 ws = *reinterpret_cast<const f32x4*>(a.w_scale + ch);
-                    typename RowQuad<T>::type out;
+        for (int t = 0; t < FT; ++t) rs[t] = factors[2 * S::channels + (tw * FT + t) * 32 + lane % 32];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = (float)acc[t][f][g * 4 + e] * (rs * ws[e]);
-                        if (a.bias != nullptr && ch + e < a.n) v += (float)static_cast<const T*>(a.bias)[ch + e];
-                        out[e] = (T)(a.act == DCNN_ACT_NONE ? v : act_keep_nan(v, hi));
+        for (int f = 0; f < FC; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int ch = (cw * FC + f) * 32 + g * 8 + lane / 32 * 4;
+                ws[f][g] = *reinterpret_cast<const f32x4*>(factors + ch);
+                bias[f][g] = *reinterpret_cast<const f32x4*>(factors + S::channels + ch);
+            }
+        meet();
+        int8_t* mine = out_lds + wave * S::unit;
+        constexpr int E = RowVec<T>::E, PW = S::row / 16, UF = PW * E / 32;
+#pragma unroll
+        for (int t = 0; t < FT; ++t)
+#pragma unroll
+            for (int u = 0; u < FC / UF; ++u) {
+                // PW places of 16 bytes to a token, exchanged by the token's low bits
+#pragma unroll
+                for (int fu = 0; fu < UF; ++fu)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int f = u * UF + fu, c = fu * 32 + g * 8 + lane / 32 * 4;
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = (float)acc[t][f][g * 4 + e] * (rs[t] * ws[f][g][e]) + bias[f][g][e];
+                        act_keep_nan(v, a.act, hi);
+                        AlignedQuad<T> out;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) out[e] = (T)v[e];
+                        *reinterpret_cast<AlignedQuad<T>*>(mine + ((lane % 32) * PW + (c / E ^ lane % PW)) * 16 + c % E * sizeof(T)) = out;
                     }
-                    if (ch + 4 <= a.n) {
-                        *reinterpret_cast<typename RowQuad<T>::type*>(y + ch) = out;
-                    } else {
+                lds_wave_sync();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (ch + e < a.n) y[ch + e] = out[e];
+                for (int i = 0; i < 32 * PW / kWave; ++i) {
+                    const int r = i * (kWave / PW) + lane / PW, p = lane % PW;
+                    const int row = t0 + (tw * FT + t) * 32 + r, ch = c0 + (cw * FC + u * UF) * 32 + p * E;
+                    const AlignedVec<T> v = *reinterpret_cast<const AlignedVec<T>*>(mine + (r * PW + (p ^ r % PW)) * 16);
+                    if (row >= count || ch >= a.n) continue;
+                    T* y = static_cast<T*>(a.y) + (int64_t)row * a.ldy + ch;
+                    if (ch + E <= a.n) {
+                        *reinterpret_cast<typename RowVec<T>::type*>(y) = v;
+                    } else {
+                        const T* from = reinterpret_cast<const T*>(mine + (r * PW + (p ^ r % PW)) * 16);
+#pragma clang loop unroll(disable)
+                        for (int e = 0; e < a.n - ch; ++e) y[e] = from[e];
                     }
                 }
-        }
+                lds_wave_sync();
+            }
+        operands(buf0, 0);                                     // (read here and not at the tile's begin: nothing is left to be waited for)
     }
 }
 
-template <typename T, int TW, int CW, int FT, int FC> static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a) {
-    using S = TileShape<T, TW, CW, FT, FC>;
-    auto kern = rows_matmul_kernel<T, TW, CW, FT, FC>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * S::stage);
-        if (err != hipSuccess) return check_hip(ctx, err, "hipFuncSetAttribute(rows_matmul_kernel)");
-        attr_set = true;
-    }
+template <typename T, int TW, int CW, int FT, int FC, int NB> static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a) {
+    using S = TileShape<T, TW, CW, FT, FC, NB>;
     const int64_t tiles = cdiv(a.rows, S::tokens) * cdiv(a.n, S::channels);
-    const int64_t most = (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / (2 * S::stage));
+    const int64_t most = (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
     const int64_t grid = cdiv(tiles < most ? tiles : most, kXcd) * kXcd;   // (tile_range deals out to whole rounds of XCDs)
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(S::threads), 2 * S::stage, ctx->stream, a);
+    hipLaunchKernelGGL((rows_matmul_kernel<T, TW, CW, FT, FC, NB>), dim3((unsigned)grid), dim3(S::threads), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "rows_matmul_kernel launch");
 }
 
+// ---- few rows -----------------------------------------------------------------------------------------------------
+// Up to G*16 tokens: the weights are all there is to read, once, and every workgroup reads its own: F*16 channels, whose k the workgroup's
+// waves deal out among themselves in steps of 64, with kAhead steps of a wave on their way at a time.  A step is one instruction of the
+// matrix cores (16 channels by 16 tokens) per F and G.  The waves' sums meet in LDS.
+//
+// NORM > 0: up to NORM tokens are normed and quantised on the spot, by every workgroup for itself (a row is 8 KB that the caches hold, a
+// launch of its own takes longer), while the first weights are on their way.
+constexpr int kFewWaves = 8, kAhead = 8;
+template <int G, int F> struct FewShape {
+    static constexpr int sums = kFewWaves * G * F * kWave * 16;
+};
+struct FewRows {                 // what NORM > 0 needs to know of the rows
+    const void *x, *w, *b;
+    const int32_t* idx;
+    int ldx, map_rows, c, kind;
+    float eps;
+};
+
+template <typename T, int G, int F, int NORM, int NV>
+__global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs a, FewRows n) {
+    constexpr int L = kFewWaves * kWave;
+    extern __shared__ __align__(16) int8_t lds[];              // sums, then (NORM) the 8-bit rows
+    __shared__ uint32_t red[2 * kFewWaves];
+    __shared__ float scales[NORM > 0 ? NORM : 1];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int count = row_count(a.count, a.rows);
+    const int steps = (a.kc + 3) / 4;                          // of 64 k
+    const int c0 = blockIdx.x * (F * 16);
+    if (count == 0) return;
+    // 16 channels of a block of 32, four chunks of 16 k to a step
+    const int w_block_bytes = a.kt * kPackK * kPackC;
+    const __amdgpu_buffer_rsrc_t w = ws_rsrc(a.w + (int64_t)(c0 / kPackC) * w_block_bytes, kWsMaxBytes);
+    const int w_lane = c0 % kPackC * 16 + lane / 16 * (kPackC * 16) + lane % 16 * 16;
+    auto weights = [&](int step, int f) {                      // (F = 2: both halves of a block)
+        const uint32_t at = step < steps ? (uint32_t)(w_lane + step * (64 * kPackC) + f * 256) : kOob;
+        return ws_load16<i32x4>(w, at);
+    };
+    i32x4 wv[kAhead][F];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int f = 0; f < F; ++f) wv[i][f] = weights(wave + i * kFewWaves, f);
+
+    // what this thread's four sums are scaled with at the end (G * F waves have some): lane: channels lane / 16 * 4 .. + 3 of token lane % 16
+    static_assert(G * F <= kFewWaves, "a wave for each 16 x 16 sums");
+    const int out_row = wave / F * 16 + lane % 16, out_ch = c0 + wave % F * 16 + lane / 16 * 4;
+    const bool out = wave < G * F && out_row < count && out_ch < a.n;
+    f32x4 ws{}, bias{};
+    float rs = 0.0f;
+    if (out) {
+        ws = *reinterpret_cast<const f32x4*>(a.w_scale + out_ch);
+        bias = load_bias<T>(a.bias, out_ch, a.n);
+        if constexpr (NORM == 0) rs = a.q_scale[out_row];
+    }
+
+    const int row_bytes = steps * 64 + 16;                     // (16: rows start on different banks)
+    int8_t* rows = lds + FewShape<G, F>::sums;
+    if constexpr (NORM > 0) {
+        constexpr int E = RowVec<T>::E;
+        int turn = 0;
+        const float inv_c = 1.0f / (float)n.c;
+#pragma unroll
+        for (int r = 0; r < NORM; ++r) {
+            int i = r;
+            if (n.idx != nullptr) i = r < count ? n.idx[r] : -1;
+            const bool token = r < count && i >= 0 && i < n.map_rows;
+            const T* x = static_cast<const T*>(n.x) + (int64_t)(token ? i : 0) * n.ldx;
+            float v[NV][E];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const typename RowVec<T>::type xv = row_load<T>(x, token ? (j * L + (int)threadIdx.x) * E : n.c, n.c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j][e] = (float)xv[e];
+            }
+            if (n.kind != DCNN_NORM_NONE)
+                norm_row<T, L, NV>(v, n.kind, n.eps, static_cast<const T*>(n.w), static_cast<const T*>(n.b), threadIdx.x, n.c, inv_c, red, turn);
+            if (!token) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[j][e] = 0.0f;
+            }
+            float inv;
+            const float scale = quantize_scale(row_amax<L, NV, E>(v, red, turn), &inv);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {                     // (zeros behind the row's end)
+                const int at = (j * L + (int)threadIdx.x) * E;
+                if (at < steps * 64) store_quantized<E>(rows + r * row_bytes + at, v[j], inv);
+            }
+            if (threadIdx.x == 0) scales[r] = scale;
+        }
+        __syncthreads();
+    }
+    const __amdgpu_buffer_rsrc_t q = ws_rsrc(a.q, NORM > 0 ? 0 : kWsMaxBytes);
+    const int token = lane % 16 < count ? lane % 16 : count - 1;
+    uint32_t q_lane[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {                              // tokens behind the last one read the last one
+        const int row = g * 16 + lane % 16;
+        q_lane[g] = (uint32_t)(row < count ? row : count - 1) * (uint32_t)a.ldq;
+    }
+    auto tokens = [&](int step, int g) {
+        const int chunk = step * 4 + lane / 16;
+        if constexpr (NORM > 0) {                              // (steps behind the last one have no weights: any tokens do)
+            return *reinterpret_cast<const i32x4*>(rows + (token < NORM ? token : 0) * row_bytes + (step < steps ? chunk : 0) * 16);
+        } else {
+            return ws_load16<i32x4>(q, chunk < a.kc ? q_lane[g] + (uint32_t)chunk * 16 : kOob);
+        }
+    };
+    i32x4 acc[G][F] = {};
+    for (int s0 = wave; s0 < steps; s0 += kAhead * kFewWaves) {
+        i32x4 qv[kAhead][G];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int g = 0; g < G; ++g) qv[i][g] = tokens(s0 + i * kFewWaves, g);
+        i32x4 next[kAhead][F];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int f = 0; f < F; ++f) next[i][f] = weights(s0 + (kAhead + i) * kFewWaves, f);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int f = 0; f < F; ++f) acc[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[i][f], qv[i][g], acc[g][f], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int f = 0; f < F; ++f) wv[i][f] = next[i][f];
+    }
+    i32x4* sums = reinterpret_cast<i32x4*>(lds);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int f = 0; f < F; ++f) sums[((wave * G + g) * F + f) * kWave + lane] = acc[g][f];
+    __syncthreads();
+    if (!out) return;
+    i32x4 s = sums[wave * kWave + lane];
+#pragma unroll
+    for (int i = 1; i < kFewWaves; ++i) s += sums[(i * G * F + wave) * kWave + lane];
+    if constexpr (NORM > 0) rs = scales[out_row < NORM ? out_row : 0];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * (rs * ws[e]) + bias[e];
+    act_keep_nan(v, a.act, act_hi(a.act));
+    T* y = static_cast<T*>(a.y) + (int64_t)out_row * a.ldy + out_ch;
+    if (out_ch + 4 <= a.n) {
+        typename RowQuad<T>::type quad;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) quad[e] = (T)v[e];
+        *reinterpret_cast<typename RowQuad<T>::type*>(y) = quad;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (out_ch + e < a.n) y[e] = (T)v[e];
+    }
+}
+
+template <typename T, int G, int F, int NORM, int NV> static dcnn_status launch_few(dcnn_ctx* ctx, const MatmulArgs& a, const FewRows& n) {
+    const size_t lds = FewShape<G, F>::sums + (NORM > 0 ? (size_t)NORM * (cdiv(a.kc, 4) * 64 + 16) : 0);
+    hipLaunchKernelGGL((rows_few_kernel<T, G, F, NORM, NV>), dim3((unsigned)cdiv(a.n, F * 16)), dim3(kFewWaves * kWave), lds, ctx->stream, a, n);
+    return check_hip(ctx, hipGetLastError(), "rows_few_kernel launch");
+}
+
+// Rows that every workgroup norms for itself: 512 lanes hold a row in one or two vectors each.
+constexpr int kFewNorm = 4;
+bool rows_linear_fuses(int dtype, int64_t rows, int64_t k) { return rows <= kFewNorm && align_up((size_t)k, 64) <= (dtype == DCNN_F32 ? 4096 : 8192); }
+
+template <typename T> static dcnn_status launch_linear_few_t(dcnn_ctx* ctx, const FewRows& n, const MatmulArgs& a) {
+    const bool one = (int64_t)cdiv(n.c, 64) * 64 <= kFewWaves * kWave * RowVec<T>::E;
+    if (a.rows == 1) return one ? launch_few<T, 1, 1, 1, 1>(ctx, a, n) : launch_few<T, 1, 1, 1, 2>(ctx, a, n);
+    return one ? launch_few<T, 1, 1, kFewNorm, 1>(ctx, a, n) : launch_few<T, 1, 1, kFewNorm, 2>(ctx, a, n);
+}
+
+dcnn_status launch_rows_linear_few(dcnn_ctx* ctx, int dtype, const NormArgs& norm, const MatmulArgs& a) {
+    const FewRows n{norm.x, norm.pre_w, norm.pre_b, norm.idx, norm.ldx, norm.map_rows, norm.c, norm.pre, norm.pre_eps};
+    if (dtype == DCNN_F16) return launch_linear_few_t<f16>(ctx, n, a);
+    if (dtype == DCNN_BF16) return launch_linear_few_t<bf16>(ctx, n, a);
+    return launch_linear_few_t<float>(ctx, n, a);
+}
+
 template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const MatmulArgs& a) {
-    return launch_tile<T, 2, 2, 2, 2>(ctx, a);
+    if (a.rows <= 16) return launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{});
+    if (a.rows <= 32) return launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
+    return launch_tile<T, 2, 4, 4, 2, 2>(ctx, a);
 }
 
 dcnn_status launch_rows_matmul(dcnn_ctx* ctx, int dtype, const MatmulArgs& a) {

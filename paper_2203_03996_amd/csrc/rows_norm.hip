@@ -13,73 +13,6 @@ template <typename T, int L> struct NormShape {
     static constexpr int threads = L > 256 ? L : 256, rows = threads / L;
 };
 
-// A lane's 16 bytes of vector v of a row of c elements; what lies behind the row is zero (or `fill` nowhere).
-template <typename T> __device__ __forceinline__ typename RowVec<T>::type row_load(const T* row, int base, int c) {
-    constexpr int E = RowVec<T>::E;
-    typename RowVec<T>::type v;
-    if (base + E <= c) return *reinterpret_cast<const typename RowVec<T>::type*>(row + base);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = base + e < c ? row[base + e] : (T)0.0f;
-    return v;
-}
-template <typename T> __device__ __forceinline__ void row_store(T* row, int base, int c, const float* o) {
-    constexpr int E = RowVec<T>::E;
-    typename RowVec<T>::type v;
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = (T)o[e];
-    if (base + E <= c) {
-        *reinterpret_cast<typename RowVec<T>::type*>(row + base) = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (base + e < c) row[base + e] = v[e];
-    }
-}
-
-// v <- norm(v); elements behind the row's end are zero before and after.
-template <typename T, int L, int NV>
-__device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const T* w, const T* b, int lane, int c, float inv_c,
-                                         uint32_t* red, int& turn) {
-    constexpr int E = RowVec<T>::E;
-    typename RowVec<T>::type wv[NV], bv[NV];
-    if (w != nullptr) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) wv[j] = row_load<T>(w, (j * L + lane) * E, c);
-    }
-    if (b != nullptr) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) bv[j] = row_load<T>(b, (j * L + lane) * E, c);
-    }
-    float mean = 0.0f;
-    if (kind == DCNN_NORM_LAYER) {
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < E; ++e) s += v[j][e];
-        mean = row_reduce<SumOp, L>(s, red, turn) * inv_c;
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int left = c - (j * L + lane) * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[j][e] = e < left ? v[j][e] - mean : 0.0f;
-            s += v[j][e] * v[j][e];
-        }
-    }
-    const float r = 1.0f / sqrtf(row_reduce<SumOp, L>(s, red, turn) * inv_c + eps);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[j][e] *= r;
-            if (w != nullptr) v[j][e] *= (float)wv[j][e];
-            if (b != nullptr) v[j][e] += (float)bv[j][e];
-        }
-}
-
 template <typename T, int L, int NV> __global__ __launch_bounds__((NormShape<T, L>::threads)) void rows_norm_kernel(NormArgs a) {
     constexpr int E = RowVec<T>::E, R = NormShape<T, L>::rows;
     typedef typename RowVec<T>::type Vec;
@@ -151,29 +84,15 @@ template <typename T, int L, int NV> __global__ __launch_bounds__((NormShape<T, 
             for (int j = 0; j < NV; ++j) row_store<T>(z, (j * L + lane) * E, c, v[j]);
         }
         if (a.q != nullptr) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < E; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu);
-            m = row_reduce<MaxOp, L>(m, red, turn);
             float inv;
-            const float scale = quantize_scale(m, &inv);
+            const float scale = quantize_scale(row_amax<L, NV, E>(v, red, turn), &inv);
             if (live) {
                 int8_t* q = a.q + r * a.ldq;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
-                    const int at = (j * L + lane) * E;
-                    uint32_t word[E / 4];
-#pragma unroll
-                    for (int e = 0; e < E; e += 4)
-                        word[e / 4] = inv == 0.0f ? 0u : pack_bytes(quantize_bits(v[j][e], inv), quantize_bits(v[j][e + 1], inv),
-                                                                   quantize_bits(v[j][e + 2], inv), quantize_bits(v[j][e + 3], inv));
                     // (a row's last vector ends within the multiple of 16 that a row of 8-bit integers takes)
-                    if (at < c) {
-                        if constexpr (E == 8) *reinterpret_cast<uint2*>(q + at) = make_uint2(word[0], word[1]);
-                        else *reinterpret_cast<uint32_t*>(q + at) = word[0];
-                    }
+                    const int at = (j * L + lane) * E;
+                    if (at < c) store_quantized<E>(q + at, v[j], inv);
                 }
                 if (lane == 0) a.q_scale[r] = scale;
             }

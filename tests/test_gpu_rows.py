@@ -440,9 +440,12 @@ def linear64(v, w, ws, bias, act):
 @pytest.mark.parametrize("dt", list(TYPES))
 @pytest.mark.parametrize("rows,k,n", [(1, 64, 40), (1, 4096, 300), (2, 2048, 513), (4, 1000, 77), (7, 513, 1000), (16, 4096, 96), (17, 96, 33), (40, 300, 200), (200, 256, 1024), (700, 130, 260)])
 @pytest.mark.parametrize("kind", ["none", "rms", "layer"])
-def test_linear(ctx, dt, rows, k, n, kind):
+@pytest.mark.parametrize("on_map", [False, True])
+def test_linear(ctx, dt, rows, k, n, kind, on_map):
     rng = np.random.default_rng([rows, k])
-    case = NormCase(dt, rows, k, pre=kind, on_map=True, seed=2)
+    case = NormCase(dt, rows, k, pre=kind, on_map=on_map, seed=2)
+    if on_map and rows <= 4:                                       # a list without room to spare: rows are normed on the spot
+        case.idx = case.idx[:rows]
     w, ws = q_weights(rng, k, n)
     bias = rand(rng, n, dt)
     y = pkg.RowWeights(ctx, w, scale=ws, bias=bias, act="relu").linear(case.x, pre=case.norms[1], idx=case.idx, count=case.count)
@@ -456,7 +459,9 @@ def test_linear(ctx, dt, rows, k, n, kind):
     # ... and the scale of a row is as good as its largest value
     slack += (128 * U32 * mag.max(1, keepdims=True) / 127 + 8 * U32 * scale) * (np.abs(np.rint(at)) @ np.abs(np64(w))) * np64(ws) + 4 * U32 * np.abs(np64(bias))
     close(y[:rows], want, dt, slack, f"{dt} {rows}x{k}x{n} {kind}")
-    # the same bits as its two steps called one after the other
+    if kind != "none":
+        return
+    # without a norm, whose sums may be formed in another order, the same bits as its two steps called one after the other
     q, qs = ctx.rows_quantize(case.x, pre=case.norms[1], idx=case.idx, count=case.count)
     two = pkg.RowWeights(ctx, w, scale=ws, bias=bias, act="relu").matmul(q, qs, dtype=TYPES[dt][0], count=case.count)
     ctx.sync()
@@ -473,8 +478,11 @@ def test_linear_of_rows_without_a_token_and_broken_rows(ctx, rows):
     idx[0] = -5
     w, ws = q_weights(rng, 72, 90)
     bias = rand(rng, 90, "f32")
-    y = pkg.RowWeights(ctx, w, scale=ws, bias=bias).linear(x, idx=idx)
+    weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias)
+    y = weights.linear(x, idx=idx)
+    few = torch.cat([weights.linear(x, idx=idx[i:i + 3].contiguous()) for i in range(0, rows + 4, 3)])    # by threes: normed on the spot
     ctx.sync()
+    assert np.array_equal(np64(few), np64(y), equal_nan=True)
     y = np64(y)
     assert (y[[0, rows + 1, rows + 2, rows + 3]] == np64(bias)).all() and np.isnan(y[rows]).all() and not np.isnan(y[:rows]).any()
 
