@@ -48,9 +48,20 @@ void set_norm(const dcnn_row_norm& n, int* kind, float* eps, const void** w, con
     *w = n.kind == DCNN_NORM_NONE ? nullptr : n.w_dev;
     *b = n.kind == DCNN_NORM_NONE ? nullptr : n.b_dev;
 }
-// 8-bit rows that a call keeps in scratch: scales, then rows
-int64_t scratch_ldq(int64_t k) { return (int64_t)align_up((size_t)k, 64); }
-size_t scratch_rows_offset(int64_t rows) { return align_up((size_t)rows * sizeof(float)); }
+// Scratch: the counts of workgroups that share a tile (at the same place whatever the sizes: they are zero between calls), their
+// partial sums, then the 8-bit rows of a call that makes some: scales, rows
+struct Scratch {
+    int64_t ldq;
+    size_t partial, scales, rows, bytes;
+    Scratch(int64_t count, int64_t k, int64_t n) {
+        const size_t a = matmul_plan(count, k, n, false).partial_bytes, b = matmul_plan(count, k, n, true).partial_bytes;
+        ldq = (int64_t)align_up((size_t)k, 64);
+        partial = align_up(kArrivedBytes);
+        scales = partial + align_up(a > b ? a : b);
+        rows = scales + align_up((size_t)count * sizeof(float));
+        bytes = rows + align_up((size_t)count * (size_t)ldq);
+    }
+};
 
 dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul_args* p, MatmulArgs* m) {
     if (!rows_float(p->dtype)) return fail(ctx, DCNN_EDTYPE, "%s: dtype %d", what, p->dtype);
@@ -79,6 +90,9 @@ dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul
     m->kc = (int)cdiv(p->k, 16);
     m->kt = (int)(packed_k(p->k) / kPackK);
     m->act = p->act;
+    char* scratch = static_cast<char*>(p->scratch_dev);
+    m->arrived = reinterpret_cast<uint32_t*>(scratch);
+    m->partial = reinterpret_cast<int32_t*>(scratch + Scratch(p->list.rows, p->k, p->n).partial);
     return DCNN_OK;
 }
 
@@ -149,7 +163,7 @@ dcnn_status dcnn_rows_pack(dcnn_ctx* ctx, int32_t dtype, int64_t k, int64_t n, c
 
 size_t dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n) {
     if (rows < 0 || rows > kRowsMax || dcnn_rows_weights_bytes(k, n) == 0) return 0;
-    return scratch_rows_offset(rows) + align_up((size_t)rows * (size_t)scratch_ldq(k));
+    return Scratch(rows, k, n).bytes;
 }
 
 dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
@@ -162,7 +176,7 @@ dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     if (st == DCNN_OK) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->k);
     if (st != DCNN_OK) return st;
     m.q = p->q_dev, m.q_scale = p->q_scale_dev, m.ldq = (int)p->ldq;
-    return launch_rows_matmul(ctx, p->dtype, m);
+    return launch_rows_matmul(ctx, p->dtype, matmul_plan(p->list.rows, p->k, p->n, p->list.count_dev != nullptr), m);
 }
 
 dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
@@ -184,14 +198,15 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     a.x = p->x_dev, a.ldx = (int)p->ldx, a.c = (int)p->k, a.scale = 1.0f;
     a.idx = p->list.idx_dev, a.count = p->list.count_dev;
     a.rows = (int)p->list.rows, a.map_rows = (int)p->list.map_rows;
-    a.q_scale = reinterpret_cast<float*>(scratch);
-    a.q = reinterpret_cast<int8_t*>(scratch + scratch_rows_offset(p->list.rows)), a.ldq = (int)scratch_ldq(p->k);
+    const Scratch at(p->list.rows, p->k, p->n);
+    a.q_scale = reinterpret_cast<float*>(scratch + at.scales);
+    a.q = reinterpret_cast<int8_t*>(scratch + at.rows), a.ldq = (int)at.ldq;
     set_norm(p->pre, &a.pre, &a.pre_eps, &a.pre_w, &a.pre_b);
     if (rows_linear_fuses(p->dtype, p->list.rows, p->k)) return launch_rows_linear_few(ctx, p->dtype, a, m);
     st = launch_rows_norm(ctx, p->dtype, a);
     if (st != DCNN_OK) return st;
     m.q = a.q, m.q_scale = a.q_scale, m.ldq = a.ldq;
-    return launch_rows_matmul(ctx, p->dtype, m);
+    return launch_rows_matmul(ctx, p->dtype, matmul_plan(p->list.rows, p->k, p->n, p->list.count_dev != nullptr), m);
 }
 
 }  // extern "C"

@@ -108,6 +108,54 @@ __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
 }
 
+// Workgroups that share a tile: each leaves its sums, in the order of its registers, and counts itself; the last one to do so adds up the
+// others' (32-bit integers: in any order the same) and goes on.  Nobody waits for anybody.
+// Sums and count go past the XCDs' caches, one access at a time (atomic accesses of the GPU's scope); a thread's stores are done before its
+// workgroup counts itself.  A fence in their place writes a whole L2 back for every workgroup: 256 of them took 35 us.
+template <int N, int THREADS>
+__device__ __forceinline__ bool last_part(i32x16* acc, int32_t* partial, uint32_t* arrived, int tile, int part, int parts, int8_t* lds) {
+    uint64_t* const sums = reinterpret_cast<uint64_t*>(partial) + (int64_t)tile * parts * (N * 8 * THREADS);
+    uint64_t* mine = sums + part * (N * 8 * THREADS) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            __hip_atomic_store(mine + (i * 8 + j) * THREADS, (uint64_t)(uint32_t)acc[i][j * 2] | (uint64_t)(uint32_t)acc[i][j * 2 + 1] << 32,
+                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    wait_loads<0>();                                           // (stores count as loads do)
+    __syncthreads();
+    uint32_t* const before = reinterpret_cast<uint32_t*>(lds);
+    if (threadIdx.x == 0) *before = __hip_atomic_fetch_add(arrived + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (*before != (uint32_t)parts - 1) return false;
+    constexpr int K = 4;                                       // parts whose sums are on their way together
+    for (int p = 1; p < parts; p += K) {
+        uint64_t v[K][N * 8];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {                          // (behind the last one: the last one again)
+            const int at = part + (p + k < parts ? p + k : parts - 1);
+            const uint64_t* from = sums + (at < parts ? at : at - parts) * (N * 8 * THREADS) + threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < N * 8; ++i) v[k][i] = __hip_atomic_load(from + i * THREADS, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (p + k >= parts) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    acc[i][j * 2] += (int32_t)(uint32_t)v[k][i * 8 + j];
+                    acc[i][j * 2 + 1] += (int32_t)(uint32_t)(v[k][i * 8 + j] >> 32);
+                }
+        }
+    }
+    if (threadIdx.x == 0) __hip_atomic_store(arrived + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();                                           // (the LDS word is about to be overwritten)
+    return true;
+}
+
 template <int I> using Int = std::integral_constant<int, I>;
 template <int N, int I = 0, typename F> __device__ __forceinline__ void unrolled(F&& f) {
     if constexpr (I < N) {
@@ -116,8 +164,8 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void unrolled
     }
 }
 
-template <typename T, int TW, int CW, int FT, int FC, int NB>
-__global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a) {
+template <typename T, int TW, int CW, int FT, int FC, int NB, bool SPLIT>
+__global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a, int splits, int share) {
     using S = TileShape<T, TW, CW, FT, FC, NB>;
     constexpr int QL = S::tokens / 8 / S::waves, WL = S::channels / 8 / S::waves;        // copies of 1 KB per K-tile and wave
     static_assert(S::threads >= S::channels && S::threads >= S::tokens && (2 * S::channels + S::tokens) * 4 <= S::waves * S::unit, "a thread for each factor");
@@ -137,18 +185,21 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     };
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int tw = wave / CW, cw = wave % CW;
-    const int count = row_count(a.count, a.rows), kts = a.kt;
+    const int count = row_count(a.count, a.rows);
     const int tiles_t = (count + S::tokens - 1) / S::tokens, tiles_c = (a.n + S::channels - 1) / S::channels;
     const int blocks_c = (a.n + kPackC - 1) / kPackC;
-    const int w_block_bytes = kts * kPackK * kPackC;           // 2 MB at most
-    const WgTileRange range = wg_tile_range((int64_t)tiles_t * tiles_c);
+    const int w_block_bytes = a.kt * kPackK * kPackC;          // 2 MB at most
+    // SPLIT: one of `splits` workgroups that share a tile's K-tiles (neighbours, so on one XCD); the grid has one for each
+    const WgTileRange range = wg_tile_range((int64_t)tiles_t * tiles_c * (SPLIT ? splits : 1));
     if (range.begin >= range.end) return;
+    const int part = SPLIT ? (int)(range.begin % splits) : 0, k0 = part * share;
+    const int kts = SPLIT ? (a.kt - k0 < share ? a.kt - k0 : share) : a.kt;
 
     // of the tile that is being copied: rows behind the last one read the last one, blocks behind the last one the last one
     __amdgpu_buffer_rsrc_t q_tile, w_tile;
     int q_at[QL], w_at[WL];
     auto aim = [&](int64_t tile) {
-        const TileAt at = tile_at((int)tile, tiles_t, tiles_c);
+        const TileAt at = tile_at((int)(SPLIT ? tile / splits : tile), tiles_t, tiles_c);
         const int t0 = at.t * S::tokens, b0 = at.c * (S::channels / kPackC);
         q_tile = ws_rsrc(a.q + (int64_t)t0 * a.ldq, kWsMaxBytes);
         w_tile = ws_rsrc(a.w + (int64_t)b0 * w_block_bytes, kWsMaxBytes);
@@ -165,7 +216,8 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     };
     // (rows 8 on: their low bits are the same but for one)
     const int q_chunk[2] = {lane % 8 ^ chunk_swizzle(lane / 8), lane % 8 ^ chunk_swizzle(lane / 8 + 8)};
-    auto copy = [&](int8_t* buf, int kt) {
+    auto copy = [&](int8_t* buf, int tile_kt) {
+        const int kt = SPLIT ? k0 + tile_kt : tile_kt;
         int at[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {                          // chunks behind a row's last one: any, their weights are zero
@@ -243,7 +295,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     operands(buf0, 0);
     const float hi = act_hi(a.act);
     for (int64_t tile = range.begin; tile < range.end; tile += range.step) {
-        const TileAt at = tile_at((int)tile, tiles_t, tiles_c);
+        const TileAt at = tile_at((int)(SPLIT ? tile / splits : tile), tiles_t, tiles_c);
         const int t0 = at.t * S::tokens, c0 = at.c * S::channels;
 #pragma unroll
         for (int t = 0; t < FT; ++t)
@@ -265,6 +317,9 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             if (kt + decltype(i)::value < kts) k_tile(kt + decltype(i)::value, buffer(i), buffer(Int<decltype(i)::value + 1>{}));
         });
         arrived = NB;
+        if constexpr (SPLIT) {
+            if (!last_part<FT * FC, S::threads>(reinterpret_cast<i32x16*>(acc), a.partial, a.arrived, (int)(tile / splits), part, splits, out_lds)) return;
+        }
         wait_loads<0>();                                       // the next tile's first K-tiles have arrived, ...
         float* const factors = reinterpret_cast<float*>(out_lds);
         if ((int)threadIdx.x < S::channels) {
@@ -329,12 +384,13 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     }
 }
 
-template <typename T, int TW, int CW, int FT, int FC, int NB> static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a) {
+template <typename T, int TW, int CW, int FT, int FC, int NB, bool SPLIT = false>
+static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 1, int share = 0) {
     using S = TileShape<T, TW, CW, FT, FC, NB>;
-    const int64_t tiles = cdiv(a.rows, S::tokens) * cdiv(a.n, S::channels);
-    const int64_t most = (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
+    const int64_t tiles = cdiv(a.rows, S::tokens) * cdiv(a.n, S::channels) * splits;
+    const int64_t most = SPLIT ? tiles : (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
     const int64_t grid = cdiv(tiles < most ? tiles : most, kXcd) * kXcd;   // (tile_range deals out to whole rounds of XCDs)
-    hipLaunchKernelGGL((rows_matmul_kernel<T, TW, CW, FT, FC, NB>), dim3((unsigned)grid), dim3(S::threads), 0, ctx->stream, a);
+    hipLaunchKernelGGL((rows_matmul_kernel<T, TW, CW, FT, FC, NB, SPLIT>), dim3((unsigned)grid), dim3(S::threads), 0, ctx->stream, a, splits, share);
     return check_hip(ctx, hipGetLastError(), "rows_matmul_kernel launch");
 }
 
@@ -521,17 +577,60 @@ dcnn_status launch_rows_linear_few(dcnn_ctx* ctx, int dtype, const NormArgs& nor
     return launch_linear_few_t<float>(ctx, n, a);
 }
 
-template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const MatmulArgs& a) {
-    if (a.rows <= 16) return launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{});
-    if (a.rows <= 32) return launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
-    return launch_tile<T, 2, 4, 4, 2, 2>(ctx, a);
+// ---- which kernel ------------------------------------------------------------------------------------------------------
+constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
+
+// us, in a row on the GPU, weights from memory (rows, k -> n); a launch alone is 3.2:
+//   17 to 32 rows: few / tiles of 64   24, 4096 -> 4096: 8.9 / 11.1   24, 1024 -> 256: 4.6 / 5.1   32, 8192 -> 1024: 11.3 / 10.9   32, 16384 -> 512: 19.5 / 12.5
+//   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 51   1000, 4096 -> 4096 (256): 39 / 25 / 33 / 51
+//                                        2000, 4096 -> 4096 (512): 74 / 48 / 40 / 53   4000, 4096 -> 4096 (1024; 256 of 256): 128 / 94 / 81 / 66
+//                                        8000, 8192 -> 1024 (504; 128): 123 / 90 / 69 / 93   16384, 1000 -> 1531 (1536; 384): 59 / 45 / 40 / 45
+//   k of a tile of 64 in one / in parts  64, 8192 -> 1024: 22 / 10.9 (8)   64, 4096 -> 4096: 17 / 11.0 (4)   200, 8192 -> 1024: 22 / 12.5 (4), 14.4 (8)
+//                                        500, 8192 -> 1024: 24 / 18.2 (2), 16.4 (4)   64, 1024 -> 256: 5.1 / 6.7 (2)
+MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
+    MatmulPlan p{kFewRows, 1, 0, 0};
+    const int64_t kt = packed_k(k) / kPackK;
+    if (rows <= 16 || (rows <= 32 && kt < 64)) return p;
+    // a list's length is on the GPU; its room is that of the whole map, and few maps are flagged all over
+    const int64_t likely = counted ? cdiv(rows, 4) : rows;
+    const int64_t tiles64 = cdiv(rows, 64) * cdiv(n, 64), tiles128 = cdiv(likely, 128) * cdiv(n, 128), tiles256 = cdiv(likely, 256) * cdiv(n, 256);
+    if (tiles128 <= kPlanCus / 2) {
+        p.kernel = kTile64;
+        // few tiles: workgroups for all compute units, which take eight K-tiles at least; of a long k, four parts where there are twice as many
+        const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+        int64_t splits = least(least(kPlanCus / tiles64, kt / 8), 8);
+        const int64_t more = least(2 * kPlanCus / tiles64, 4);
+        if (kt >= 64 && splits < more) splits = more;
+        if (splits > 1) {
+            p.share = (int)cdiv(kt, splits);
+            p.splits = (int)cdiv(kt, p.share);
+            p.partial_bytes = (size_t)(tiles64 * p.splits) * 64 * 64 * sizeof(int32_t);
+        }
+    } else if (tiles128 <= kPlanCus) {
+        p.kernel = kTile128Deep;
+    } else {
+        // (a tile of 256 takes 1.7 times as long as two of 128 side by side, on all compute units)
+        p.kernel = 17 * cdiv(tiles256, kPlanCus) <= 10 * cdiv(tiles128, 2 * kPlanCus) ? kTile256 : kTile128;
+    }
+    return p;
 }
 
-dcnn_status launch_rows_matmul(dcnn_ctx* ctx, int dtype, const MatmulArgs& a) {
+template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const MatmulPlan& p, const MatmulArgs& a) {
+    switch (p.kernel) {
+        case kFewRows: return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
+        case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, true>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
+        case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 4>(ctx, a);
+        case kTile128: return launch_tile<T, 2, 2, 2, 2, 2>(ctx, a);
+        case kTile256: return launch_tile<T, 2, 4, 4, 2, 2>(ctx, a);
+    }
+    return DCNN_EINVAL;
+}
+
+dcnn_status launch_rows_matmul(dcnn_ctx* ctx, int dtype, const MatmulPlan& plan, const MatmulArgs& a) {
     if (a.rows == 0) return DCNN_OK;
-    if (dtype == DCNN_F16) return launch_matmul_t<f16>(ctx, a);
-    if (dtype == DCNN_BF16) return launch_matmul_t<bf16>(ctx, a);
-    return launch_matmul_t<float>(ctx, a);
+    if (dtype == DCNN_F16) return launch_matmul_t<f16>(ctx, plan, a);
+    if (dtype == DCNN_BF16) return launch_matmul_t<bf16>(ctx, plan, a);
+    return launch_matmul_t<float>(ctx, plan, a);
 }
 
 }  // namespace dcnn
