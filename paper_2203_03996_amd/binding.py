@@ -298,7 +298,7 @@ class Context:
         elif x is None:
             map_rows = rows if idx is None else 0x7fffffff
         if gate is not None:
-            a.gate, a.ldg, n = _as_rows(gate if gate.dim() > 1 else gate[None], "gate", c, dt, dev)
+            a.gate, a.ldg, n = _as_rows(gate, "gate", c, dt, dev) if gate.dim() > 1 else (_vector(gate, "gate", c, dt, dev), c, 1)
             a.gate_rows = gate_rows
             if n < (-(-map_rows // gate_rows) if gate_rows > 0 else 1):
                 raise ValueError(f"rows_norm: {n} rows of gate for {map_rows} map rows, {gate_rows} to each")
@@ -443,15 +443,22 @@ def _as_rows(t, name, c, dt, dev):
     if t.dim() != 2:
         t = t.view(-1, t.shape[-1])
     n, cols = t.shape
+    if cols != c or t.dtype is not dt or t.get_device() != dev:
+        raise ValueError(f"{name} must hold rows of {c} {dt} on GPU {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if n <= 1 or t.is_contiguous():
+        if c > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the elements of a row must lie side by side (strides {t.stride()})")
+        return t.data_ptr(), c, n
     ld, one = t.stride()
-    if cols != c or t.dtype != dt or t.get_device() != dev or (one != 1 and c > 1):
-        raise ValueError(f"{name} must hold rows of {c} {dt} side by side on GPU {dev}, got {tuple(t.shape)} {t.dtype} strides {t.stride()} "
-                         f"on {t.device}")
-    if n <= 1:
-        ld = c
-    elif ld < c:
-        raise ValueError(f"{name}: rows overlap (stride {ld}, {c} columns)")
+    if ld < c or (one != 1 and c > 1):
+        raise ValueError(f"{name}: rows of {c} elements side by side, apart from each other (strides {t.stride()})")
     return t.data_ptr(), ld, n
+
+
+def _vector(t, name, c, dt, dev):
+    if t.numel() != c or t.dtype is not dt or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{c}] {dt} on GPU {dev}, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
 
 
 def _check_q(q, q_scale, c, dev):

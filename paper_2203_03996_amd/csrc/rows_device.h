@@ -10,12 +10,12 @@ typedef __bf16 bf16;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-// 16 bytes of a row.  Rows start at any multiple of the element's size (odd widths, views), and the memory path takes vectors
-// at such addresses: the alignment is the element's.
-template <typename T> struct RowVec;
-template <> struct RowVec<float> { static constexpr int E = 4; typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
-template <> struct RowVec<f16> { static constexpr int E = 8; typedef f16 type __attribute__((ext_vector_type(8), aligned(2))); };
-template <> struct RowVec<bf16> { static constexpr int E = 8; typedef bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
+// 16 bytes of a row: E elements, and a vector of them where rows lie.  Rows start at any multiple of the element's size (odd widths,
+// views), and the memory path takes vectors at such addresses: the alignment is the element's.
+template <typename T> struct RowVec {
+    static constexpr int E = 16 / (int)sizeof(T);
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
 // Four consecutive outputs.
 template <typename T> struct RowQuad { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 
@@ -121,71 +121,132 @@ __device__ __forceinline__ float quantize_scale(uint32_t bits, float* inv) {
 }
 
 // ---- rows in registers ----------------------------------------------------------------------------------------------
-// 16 bytes of a row of c elements from element `base` on; what lies behind the row is zero.
-template <typename T> __device__ __forceinline__ typename RowVec<T>::type row_load(const T* row, int base, int c) {
+// A row is cut into vectors of 16 bytes; where its length is no multiple of that the last one ends where the row does, and its first
+// elements are the vector's before it once more: they count in no sum and are stored twice, with the same values.  (So no load is masked
+// and no store is in pieces, wherever rows start.)
+// Vector `base` of a row of c elements: where it lies (below c), and the elements that do not count (E: all, it is behind the row).
+struct RowPart { int at, skip; };
+template <typename T> __device__ __forceinline__ RowPart row_part(int base, int c) {
     constexpr int E = RowVec<T>::E;
-    typename RowVec<T>::type v;
-    if (base + E <= c) return *reinterpret_cast<const typename RowVec<T>::type*>(row + base);
+    if (base + E <= c || c < E) return {base, base < c ? 0 : E};           // (rows shorter than a vector: the first one)
+    return base < c ? RowPart{c - E, base + E - c} : RowPart{base, E};
+}
+template <typename T> __device__ __forceinline__ u32x4 row_load(const T* row, int base, int c) {
+    constexpr int E = RowVec<T>::E;
+    const RowPart p = row_part<T>(base, c);
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (p.skip >= E) return v;
+    if (c >= E) return __builtin_bit_cast(u32x4, *reinterpret_cast<const typename RowVec<T>::type*>(row + p.at));
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = base + e < c ? row[base + e] : (T)0.0f;
+    for (int e = 0; e < E; ++e)
+        if (e < c) v[e * (int)sizeof(T) / 4] |= (uint32_t) reinterpret_cast<const Bits*>(row)[e] << (e * (int)sizeof(T) % 4 * 8);
     return v;
+}
+template <typename T> __device__ __forceinline__ float row_get(u32x4 v, int e) {
+    typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
+    return (float)__builtin_bit_cast(Vec, v)[e];
 }
 template <typename T> __device__ __forceinline__ void row_store(T* row, int base, int c, const float* o) {
     constexpr int E = RowVec<T>::E;
+    const RowPart p = row_part<T>(base, c);
+    if (p.skip >= E) return;
     typename RowVec<T>::type v;
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = (T)o[e];
-    if (base + E <= c) {
-        *reinterpret_cast<typename RowVec<T>::type*>(row + base) = v;
+    if (c >= E) {
+        *reinterpret_cast<typename RowVec<T>::type*>(row + p.at) = v;
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (base + e < c) row[base + e] = v[e];
+            if (e < c) row[e] = v[e];
     }
 }
 
-// v <- norm(v); elements behind the row's end are zero before and after.
-template <typename T, int L, int NV>
-__device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const T* w, const T* b, int lane, int c, float inv_c,
-                                         uint32_t* red, int& turn) {
+// The same value, of which the compiler knows nothing: what is made of it in a loop is not made once before it and kept.  (Parameters held
+// as 16-bit values would be held as fp32 values, in twice the registers.)
+__device__ __forceinline__ u32x4 unknown(u32x4 v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A norm's parameters for the channels of a lane: read once for many rows (HOLD), or where they are used.
+template <typename T, int L, int NV, bool HOLD> struct NormParams {
+    const T *w, *b;
+    u32x4 wv[HOLD ? NV : 1], bv[HOLD ? NV : 1];
+    __device__ __forceinline__ void read(const void* w_, const void* b_, int lane, int c) {
+        w = static_cast<const T*>(w_), b = static_cast<const T*>(b_);
+        if constexpr (HOLD) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (w != nullptr) wv[j] = row_load<T>(w, (j * L + lane) * RowVec<T>::E, c);
+                if (b != nullptr) bv[j] = row_load<T>(b, (j * L + lane) * RowVec<T>::E, c);
+            }
+        }
+    }
+    __device__ __forceinline__ u32x4 weight(int j, int lane, int c) const { return HOLD ? unknown(wv[HOLD ? j : 0]) : row_load<T>(w, (j * L + lane) * RowVec<T>::E, c); }
+    __device__ __forceinline__ u32x4 bias(int j, int lane, int c) const { return HOLD ? unknown(bv[HOLD ? j : 0]) : row_load<T>(b, (j * L + lane) * RowVec<T>::E, c); }
+};
+
+// f(v[j][e], e) for the elements that count in the row's sums.
+template <typename T, int L, int NV, typename F> __device__ __forceinline__ void each_once(int lane, int c, F&& f) {
     constexpr int E = RowVec<T>::E;
-    typename RowVec<T>::type wv[NV], bv[NV];
-    if (w != nullptr) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) wv[j] = row_load<T>(w, (j * L + lane) * E, c);
-    }
-    if (b != nullptr) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) bv[j] = row_load<T>(b, (j * L + lane) * E, c);
-    }
-    float mean = 0.0f;
-    if (kind == DCNN_NORM_LAYER) {
-        float s = 0.0f;
+    if (c % E == 0) {                                          // (what lies behind the row is zero)
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int e = 0; e < E; ++e) s += v[j][e];
-        mean = row_reduce<SumOp, L>(s, red, turn) * inv_c;
+            for (int e = 0; e < E; ++e) f(j, e, true);
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int skip = c < E ? 0 : row_part<T>((j * L + lane) * E, c).skip;
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(j, e, e >= skip);
+        }
+    }
+}
+
+// v <- norm(v); vectors behind the row's end are zero before and after.
+template <typename T, int L, int NV, bool HOLD>
+__device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const NormParams<T, L, NV, HOLD>& params, int lane, int c, float inv_c,
+                                         uint32_t* red, int& turn) {
+    constexpr int E = RowVec<T>::E;
+    if (kind == DCNN_NORM_LAYER) {
+        float s = 0.0f;
+        each_once<T, L, NV>(lane, c, [&](int j, int e, bool counts) { s += counts ? v[j][e] : 0.0f; });
+        const float mean = row_reduce<SumOp, L>(s, red, turn) * inv_c;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int base = (j * L + lane) * E;
+            if (c < E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j][e] = base + e < c ? v[j][e] - mean : 0.0f;
+            } else {
+                const float m = base < c ? mean : 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j][e] -= m;
+            }
+        }
     }
     float s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int left = c - (j * L + lane) * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[j][e] = e < left ? v[j][e] - mean : 0.0f;
-            s += v[j][e] * v[j][e];
-        }
-    }
+    each_once<T, L, NV>(lane, c, [&](int j, int e, bool counts) { s += counts ? v[j][e] * v[j][e] : 0.0f; });
     const float r = 1.0f / sqrtf(row_reduce<SumOp, L>(s, red, turn) * inv_c + eps);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+        if (params.w != nullptr) {
+            const u32x4 w = params.weight(j, lane, c);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[j][e] *= r;
-            if (w != nullptr) v[j][e] *= (float)wv[j][e];
-            if (b != nullptr) v[j][e] += (float)bv[j][e];
+            for (int e = 0; e < E; ++e) v[j][e] *= r * row_get<T>(w, e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[j][e] *= r;
         }
+        if (params.b != nullptr) {
+            const u32x4 b = params.bias(j, lane, c);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[j][e] += row_get<T>(b, e);
+        }
+    }
 }
 
 // A row's largest magnitude, as bits, over its lanes.
@@ -197,14 +258,17 @@ template <int L, int NV, int E> __device__ __forceinline__ uint32_t row_amax(con
         for (int e = 0; e < E; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu);
     return row_reduce<MaxOp, L>(m, red, turn);
 }
-// E values in 8 bits at p.
-template <int E> __device__ __forceinline__ void store_quantized(int8_t* p, const float (&v)[E], float inv) {
-    uint32_t word[E / 4];
+// E values in 8 bits, vector `base` of a row of c.
+template <typename T> __device__ __forceinline__ void row_store_quantized(int8_t* row, int base, int c, const float (&v)[RowVec<T>::E], float inv) {
+    constexpr int E = RowVec<T>::E;
+    const RowPart p = row_part<T>(base, c);
+    if (p.skip >= E) return;
+    typedef uint32_t Words __attribute__((ext_vector_type(E / 4), aligned(1)));
+    Words w;
 #pragma unroll
     for (int e = 0; e < E; e += 4)
-        word[e / 4] = inv == 0.0f ? 0u : pack_bytes(quantize_bits(v[e], inv), quantize_bits(v[e + 1], inv), quantize_bits(v[e + 2], inv), quantize_bits(v[e + 3], inv));
-    if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(word[0], word[1]);
-    else *reinterpret_cast<uint32_t*>(p) = word[0];
+        w[e / 4] = inv == 0.0f ? 0u : pack_bytes(quantize_bits(v[e], inv), quantize_bits(v[e + 1], inv), quantize_bits(v[e + 2], inv), quantize_bits(v[e + 3], inv));
+    *reinterpret_cast<Words*>(row + p.at) = w;                 // (a row shorter than a vector has room for one)
 }
 
 }  // namespace dcnn

@@ -455,6 +455,8 @@ __global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs 
         constexpr int E = RowVec<T>::E;
         int turn = 0;
         const float inv_c = 1.0f / (float)n.c;
+        NormParams<T, L, NV, true> params;
+        params.read(n.w, n.b, threadIdx.x, n.c);
 #pragma unroll
         for (int r = 0; r < NORM; ++r) {
             int i = r;
@@ -464,12 +466,12 @@ __global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs 
             float v[NV][E];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const typename RowVec<T>::type xv = row_load<T>(x, token ? (j * L + (int)threadIdx.x) * E : n.c, n.c);
+                const u32x4 xv = row_load<T>(x, token ? (j * L + (int)threadIdx.x) * E : n.c, n.c);
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[j][e] = (float)xv[e];
+                for (int e = 0; e < E; ++e) v[j][e] = row_get<T>(xv, e);
             }
             if (n.kind != DCNN_NORM_NONE)
-                norm_row<T, L, NV>(v, n.kind, n.eps, static_cast<const T*>(n.w), static_cast<const T*>(n.b), threadIdx.x, n.c, inv_c, red, turn);
+                norm_row<T, L, NV, true>(v, n.kind, n.eps, params, threadIdx.x, n.c, inv_c, red, turn);
             if (!token) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
@@ -479,10 +481,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs 
             float inv;
             const float scale = quantize_scale(row_amax<L, NV, E>(v, red, turn), &inv);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {                     // (zeros behind the row's end)
-                const int at = (j * L + (int)threadIdx.x) * E;
-                if (at < steps * 64) store_quantized<E>(rows + r * row_bytes + at, v[j], inv);
-            }
+            for (int j = 0; j < NV; ++j) row_store_quantized<T>(rows + r * row_bytes, (j * L + (int)threadIdx.x) * E, n.c, v[j], inv);
             if (threadIdx.x == 0) scales[r] = scale;
         }
         __syncthreads();
@@ -585,6 +584,7 @@ constexpr int kPlanCus = 256;                  // compute units of an MI355X: wh
 //   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 51   1000, 4096 -> 4096 (256): 39 / 25 / 33 / 51
 //                                        2000, 4096 -> 4096 (512): 74 / 48 / 40 / 53   4000, 4096 -> 4096 (1024; 256 of 256): 128 / 94 / 81 / 66
 //                                        8000, 8192 -> 1024 (504; 128): 123 / 90 / 69 / 93   16384, 1000 -> 1531 (1536; 384): 59 / 45 / 40 / 45
+//   short k, 128 in eight waves / in four / 256   26214, 256 -> 1024: 20.3 / 21.9 / 21.4   4000, 1000 -> 1531: 15.0 / 15.5 / 25   16384, 4096 -> 4096: 292 / 284 / 244
 //   k of a tile of 64 in one / in parts  64, 8192 -> 1024: 22 / 10.9 (8)   64, 4096 -> 4096: 17 / 11.0 (4)   200, 8192 -> 1024: 22 / 12.5 (4), 14.4 (8)
 //                                        500, 8192 -> 1024: 24 / 18.2 (2), 16.4 (4)   64, 1024 -> 256: 5.1 / 6.7 (2)
 MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
@@ -608,9 +608,11 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
         }
     } else if (tiles128 <= kPlanCus) {
         p.kernel = kTile128Deep;
+    } else if (kt <= 4) {
+        p.kernel = kTile128Short;
     } else {
         // (a tile of 256 takes 1.7 times as long as two of 128 side by side, on all compute units)
-        p.kernel = 17 * cdiv(tiles256, kPlanCus) <= 10 * cdiv(tiles128, 2 * kPlanCus) ? kTile256 : kTile128;
+        p.kernel = 17 * cdiv(tiles256, kPlanCus) <= 10 * cdiv(tiles128, 2 * kPlanCus) ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
     }
     return p;
 }
@@ -620,6 +622,7 @@ template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const Ma
         case kFewRows: return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
         case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, true>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
         case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 4>(ctx, a);
+        case kTile128Short: return launch_tile<T, 2, 4, 2, 1, 2>(ctx, a);
         case kTile128: return launch_tile<T, 2, 2, 2, 2, 2>(ctx, a);
         case kTile256: return launch_tile<T, 2, 4, 4, 2, 2>(ctx, a);
     }
