@@ -677,3 +677,48 @@ def test_c_refusals(ctx):
         assert call(None, None) == 1 and call(ctx.handle, None) == 1
     ctx.sync()
     assert (np64(out) == 3.0).all(), "a refused call wrote something"
+
+
+# ---- blocks on a network's updates ------------------------------------------------------------------------------------
+def block64(x, up, down, ub, db, pre, post, gate, scale):
+    """A block in 64 bits, quantised where the operators quantise."""
+    quant = lambda v: (np.rint(v * 127 / np.abs(v).max(-1, keepdims=True)), np.abs(v).max(-1, keepdims=True) / 127)  # noqa: E731
+    wq = lambda w: tuple(a.T for a in quant(w.T))  # noqa: E731
+    q, s = quant(norm64(x, *pre)[0])
+    w, ws = wq(up)
+    hidden = np.maximum((q @ w) * s * ws + ub, 0)
+    q, s = quant(hidden)
+    w, ws = wq(down)
+    return x + scale * gate * norm64((q @ w) * s * ws + db, *post)[0]
+
+
+def test_block_follows_its_formula(ctx):
+    """Between the two products the hidden rows are rounded to fp16, which moves an 8-bit value by one step now and then;
+    that is 1/127 of a row's largest value, at most, times a weight.  Over `hidden` of them the steps add up like a random walk."""
+    rng = np.random.default_rng(8)
+    c, hidden, px = 96, 200, 300
+    t = {k: rand(rng, s, "f16", sc, m) for k, (s, sc, m) in {"up": ((c, hidden), c ** -0.5, 0), "down": ((hidden, c), hidden ** -0.5, 0), "ub": (hidden, 0.1, 0), "db": (c, 0.1, 0),
+                                                             "w1": (c, 0.1, 1), "b1": (c, 0.1, 0), "w2": (c, 0.1, 1), "gate": (c, 0.1, 0.5), "x": ((px, c), 1, 0)}.items()}
+    block = pkg.RowBlock(ctx, t["up"], t["down"], t["ub"], t["db"], pre=pkg.RowNorm("layer", t["w1"], t["b1"]), post=pkg.RowNorm("rms", t["w2"]), gate=t["gate"], scale=0.5)
+    y = block.step(t["x"], torch.zeros_like(t["x"]))
+    ctx.sync()
+    v = {k: np64(a) for k, a in t.items()}
+    want = block64(v["x"], v["up"], v["down"], v["ub"], v["db"], ("layer", v["w1"], v["b1"], 1e-5), ("rms", v["w2"], None, 1e-5), v["gate"], 0.5)
+    # the block's branch is of the size of `gate`; a hidden value of 127 steps is off by half of fp16's spacing there, 127 * 2^-11 of a step at most,
+    # so about one in sixteen moves a step: sqrt(hidden / 16) steps of 1 / 127 of the largest hidden value (about 3 of its rms), relative to sqrt(hidden) rms
+    off = np.abs(np64(y) - want).max()
+    assert off <= 0.5 * 1.0 * (6 * 3 / 127 / 4) + 2.0 ** -11 * np.abs(want).max(), off
+
+
+def test_blocks_on_the_flagged_pixels_of_a_network():
+    import examples.video_tokens as example
+    found = example.run(streams=2, size=32, hidden=192, frames=5)
+    assert len(found) == 4 and all(0 < n < px for n, px, _, _ in found)
+
+
+def test_token_stack_wants_its_first_frame(ctx):
+    stack = pkg.TokenStack([pkg.RowBlock(ctx, torch.ones(8, 16, device="cuda"), torch.ones(16, 8, device="cuda"))])
+    with pytest.raises(ValueError):
+        stack.step(torch.ones(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        pkg.RowBlock(ctx, torch.ones(8, 16, device="cuda"), torch.ones(8, 16, device="cuda"))
