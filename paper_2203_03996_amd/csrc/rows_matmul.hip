@@ -262,8 +262,15 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
 #pragma unroll
         for (int ks = 0; ks < kSteps - 1; ++ks) {
             operands(buf, ks + 1);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FT * FC < 8) __builtin_amdgcn_sched_barrier(0);
             multiply(ks);
+            if constexpr (FT * FC >= 8) {                      // an operand read between two products (2 % of large tiles)
+#pragma unroll
+                for (int i = 0; i < FT + FC; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         if (kt + 1 >= arrived) {                               // K-tile kt + 1: those behind it may be on their way
@@ -611,15 +618,20 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
     } else if (kt <= 4) {
         p.kernel = kTile128Short;
     } else {
-        // (a tile of 256 takes 1.7 times as long as two of 128 side by side, on all compute units)
-        p.kernel = 17 * cdiv(tiles256, kPlanCus) <= 10 * cdiv(tiles128, 2 * kPlanCus) ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
+        // a tile of 256 takes 1.7 times as long as two of 128 side by side, on all compute units; pairs of the latter go out of step, so that
+        // half a round of them takes half the time
+        const int64_t rounds128 = tiles128 > 2 * kPlanCus ? tiles128 : 2 * kPlanCus;
+        p.kernel = 17 * 2 * kPlanCus * cdiv(tiles256, kPlanCus) <= 10 * rounds128 ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
     }
     return p;
 }
 
 template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const MatmulPlan& p, const MatmulArgs& a) {
     switch (p.kernel) {
-        case kFewRows: return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
+        case kFewRows:
+            // 32 channels to a workgroup where that makes one for every compute unit: 32, 2048 -> 8192: 9.3 against 10.2; 4096 -> 4096: 10.7, 9.3
+            if (a.n >= 32 * kPlanCus) return a.rows <= 16 ? launch_few<T, 1, 2, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 2, 0, 1>(ctx, a, FewRows{});
+            return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
         case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, true>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
         case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 4>(ctx, a);
         case kTile128Short: return launch_tile<T, 2, 4, 2, 1, 2>(ctx, a);
