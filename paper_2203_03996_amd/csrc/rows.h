@@ -64,8 +64,8 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted);
 constexpr size_t kArrivedBytes = 2048;         // counts of the workgroups of 512 tiles
 dcnn_status launch_rows_matmul(dcnn_ctx* ctx, int dtype, const MatmulPlan& plan, const MatmulArgs& a);
 // Norm, 8-bit rows and product in one kernel, for a token or a few: x, idx, map_rows, ldx, c and pre of NormArgs, all of MatmulArgs but q.
-bool rows_linear_fuses(int dtype, int64_t rows, int64_t k);
-dcnn_status launch_rows_linear_few(dcnn_ctx* ctx, int dtype, const NormArgs& norm, const MatmulArgs& a);
+bool rows_linear_fuses(int dtype, int64_t rows, int64_t k, int64_t n, bool counted);
+dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& norm, const MatmulArgs& a);
 dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, const void* w, int64_t ldw, const float* scale,
                              int8_t* packed, float* packed_scale);
 

@@ -202,7 +202,7 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     a.q_scale = reinterpret_cast<float*>(scratch + at.scales);
     a.q = reinterpret_cast<int8_t*>(scratch + at.rows), a.ldq = (int)at.ldq;
     set_norm(p->pre, &a.pre, &a.pre_eps, &a.pre_w, &a.pre_b);
-    if (rows_linear_fuses(p->dtype, p->list.rows, p->k)) return launch_rows_linear_few(ctx, p->dtype, a, m);
+    if (rows_linear_fuses(p->dtype, p->list.rows, p->k, p->n, p->list.count_dev != nullptr)) return launch_rows_linear_fused(ctx, p->dtype, a, m);
     st = launch_rows_norm(ctx, p->dtype, a);
     if (st != DCNN_OK) return st;
     m.q = a.q, m.q_scale = a.q_scale, m.ldq = a.ldq;

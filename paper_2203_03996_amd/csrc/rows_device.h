@@ -258,17 +258,21 @@ template <int L, int NV, int E> __device__ __forceinline__ uint32_t row_amax(con
         for (int e = 0; e < E; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu);
     return row_reduce<MaxOp, L>(m, red, turn);
 }
-// E values in 8 bits, vector `base` of a row of c.
-template <typename T> __device__ __forceinline__ void row_store_quantized(int8_t* row, int base, int c, const float (&v)[RowVec<T>::E], float inv) {
-    constexpr int E = RowVec<T>::E;
-    const RowPart p = row_part<T>(base, c);
-    if (p.skip >= E) return;
-    typedef uint32_t Words __attribute__((ext_vector_type(E / 4), aligned(1)));
-    Words w;
+// E values in 8 bits.
+template <typename T> struct QuantWords {
+    typedef uint32_t type __attribute__((ext_vector_type(16 / sizeof(T) / 4), aligned(1)));
+};
+template <typename T> __device__ __forceinline__ typename QuantWords<T>::type quantized(const float (&v)[RowVec<T>::E], float inv) {
+    typename QuantWords<T>::type w;
 #pragma unroll
-    for (int e = 0; e < E; e += 4)
+    for (int e = 0; e < RowVec<T>::E; e += 4)
         w[e / 4] = inv == 0.0f ? 0u : pack_bytes(quantize_bits(v[e], inv), quantize_bits(v[e + 1], inv), quantize_bits(v[e + 2], inv), quantize_bits(v[e + 3], inv));
-    *reinterpret_cast<Words*>(row + p.at) = w;                 // (a row shorter than a vector has room for one)
+    return w;
+}
+// Vector `base` of a row of c in 8 bits.  (A row shorter than a vector has room for one.)
+template <typename T> __device__ __forceinline__ void row_store_quantized(int8_t* row, int base, int c, const float (&v)[RowVec<T>::E], float inv) {
+    const RowPart p = row_part<T>(base, c);
+    if (p.skip < RowVec<T>::E) *reinterpret_cast<typename QuantWords<T>::type*>(row + p.at) = quantized<T>(v, inv);
 }
 
 }  // namespace dcnn

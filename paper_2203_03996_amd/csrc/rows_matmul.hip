@@ -78,10 +78,14 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 // The sums leave through LDS, a wave's 32 tokens by 128 bytes at a time: pieces of rows, 16 bytes a lane, where the matrix cores' order
 // would store 16 bytes from 32 rows.
 constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
-template <typename T, int TW, int CW, int FT, int FC, int NB> struct TileShape {
+constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
+constexpr int kPanelTiles = 2;                 // K-tiles of rows that a workgroup makes for itself and keeps
+enum TileMode { kWhole, kParts, kPanel };      // rows_matmul_kernel: see there
+template <typename T, int TW, int CW, int FT, int FC, int NB, TileMode MODE> struct TileShape {
     static constexpr int waves = TW * CW, threads = waves * kWave, tokens = TW * FT * 32, channels = CW * FC * 32;
     static constexpr int row = FC * 32 * (int)sizeof(T) < 128 ? FC * 32 * (int)sizeof(T) : 128;      // bytes of a token on their way out
-    static constexpr int stage = (tokens + channels) * kPackK, unit = 32 * row, lds = NB * stage + waves * unit;
+    static constexpr int copied = MODE == kPanel ? 0 : tokens;                                       // tokens of a buffer
+    static constexpr int stage = (copied + channels) * kPackK, unit = 32 * row, lds = NB * stage + waves * unit;
 };
 __device__ __forceinline__ int chunk_swizzle(int row) { return (row >> 1) & 7; }
 
@@ -164,12 +168,71 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void unrolled
     }
 }
 
-template <typename T, int TW, int CW, int FT, int FC, int NB, bool SPLIT>
-__global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a, int splits, int share) {
-    using S = TileShape<T, TW, CW, FT, FC, NB>;
-    constexpr int QL = S::tokens / 8 / S::waves, WL = S::channels / 8 / S::waves;        // copies of 1 KB per K-tile and wave
+struct FewRows {                 // the rows that a kernel norms and quantises for itself
+    const void *x, *w, *b;
+    const int32_t* idx;
+    int ldx, map_rows, c, kind;
+    float eps;
+};
+
+// kPanel: the rows of a token tile, normed (or not), in 8 bits, in LDS: K-tiles one behind the other, laid out as the others' buffers are.
+// Eight lanes to a row, so that a wave has its eight rows in hand at once: a wave to a row, eight rows one behind the other, took 5 to 10 us
+// longer (reductions that wait for each other, code that is run once).
+constexpr int kPanelLanes = 8;
+template <typename T, int NV, int TOKENS, int WAVES>
+__device__ __forceinline__ void make_panel(const FewRows& n, int t0, int count, int8_t* panel, float* scales) {
+    constexpr int E = RowVec<T>::E, L = kPanelLanes;
+    static_assert(TOKENS == WAVES * (kWave / L), "a row for each eight lanes");
+    const int lane = threadIdx.x % L, r = threadIdx.x / L, c = n.c;
+    const float inv_c = 1.0f / (float)c;
+    int turn = 0, i = t0 + r;
+    if (n.idx != nullptr) i = i < count ? n.idx[i] : -1;
+    const bool token = t0 + r < count && i >= 0 && i < n.map_rows;
+    const T* x = static_cast<const T*>(n.x) + (int64_t)(token ? i : 0) * n.ldx;
+    u32x4 raw[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[j] = row_load<T>(x, (j * L + lane) * E, token ? c : 0);
+    NormParams<T, L, NV, true> params;
+    params.read(n.w, n.b, lane, c);
+    float v[NV][E];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[j][e] = row_get<T>(raw[j], e);
+    if (n.kind != DCNN_NORM_NONE) norm_row<T, L, NV, true>(v, n.kind, n.eps, params, lane, c, inv_c, nullptr, turn);
+    if (!token) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[j][e] = 0.0f;
+    }
+    float inv;
+    const float scale = quantize_scale(row_amax<L, NV, E>(v, nullptr, turn), &inv);
+    if (lane == 0) scales[r] = scale;
+    auto place = [&](int k) { return panel + (k / kPackK * TOKENS + r) * kPackK + ((k % kPackK / 16 ^ chunk_swizzle(r)) * 16 + k % 16); };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const RowPart part = row_part<T>((j * L + lane) * E, c);
+        if (part.skip >= E) continue;
+        const typename QuantWords<T>::type w = quantized<T>(v[j], inv);
+        if (part.at % E == 0) {
+            typedef uint32_t Words __attribute__((ext_vector_type(E / 4)));
+            *reinterpret_cast<Words*>(place(part.at)) = w;
+        } else {                                               // (a row's last vector where its length is odd: across two chunks)
+#pragma unroll
+            for (int e = 0; e < E; ++e) *place(part.at + e) = (int8_t)(w[e / 4] >> (e % 4 * 8));
+        }
+    }
+}
+
+// kWhole: workgroups stride through the tiles.  kParts: `splits` workgroups share a tile, each `share` of its K-tiles.  kPanel: a workgroup
+// makes the 8-bit rows of a token tile itself and keeps them; `splits` workgroups share its channel tiles, `share` to each.
+template <typename T, int TW, int CW, int FT, int FC, int NB, TileMode MODE>
+__global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a, int splits, int share, std::conditional_t<MODE == kPanel, FewRows, int> n) {
+    using S = TileShape<T, TW, CW, FT, FC, NB, MODE>;
+    constexpr int QL = S::copied / 8 / S::waves, WL = S::channels / 8 / S::waves;        // copies of 1 KB per K-tile and wave
     static_assert(S::threads >= S::channels && S::threads >= S::tokens && (2 * S::channels + S::tokens) * 4 <= S::waves * S::unit, "a thread for each factor");
-    static_assert(QL * 8 * S::waves == S::tokens && WL * 8 * S::waves == S::channels, "whole rounds of copies");
+    static_assert(QL * 8 * S::waves == S::copied && WL * 8 * S::waves == S::channels, "whole rounds of copies");
     // (an array each: what is read from one buffer does not wait for copies into the others)
     __shared__ __align__(1024) int8_t buf0[S::stage], buf1[S::stage], buf2[NB > 2 ? S::stage : 16], buf3[NB > 3 ? S::stage : 16],
         buf4[NB > 4 ? S::stage : 16], buf5[NB > 5 ? S::stage : 16], out_lds[S::waves * S::unit];
@@ -189,19 +252,27 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     const int tiles_t = (count + S::tokens - 1) / S::tokens, tiles_c = (a.n + S::channels - 1) / S::channels;
     const int blocks_c = (a.n + kPackC - 1) / kPackC;
     const int w_block_bytes = a.kt * kPackK * kPackC;          // 2 MB at most
-    // SPLIT: one of `splits` workgroups that share a tile's K-tiles (neighbours, so on one XCD); the grid has one for each
-    const WgTileRange range = wg_tile_range((int64_t)tiles_t * tiles_c * (SPLIT ? splits : 1));
-    if (range.begin >= range.end) return;
-    const int part = SPLIT ? (int)(range.begin % splits) : 0, k0 = part * share;
-    const int kts = SPLIT ? (a.kt - k0 < share ? a.kt - k0 : share) : a.kt;
+    // (workgroups that share a tile are neighbours, so on one XCD; the grid has one for each)
+    const WgTileRange mine_of = wg_tile_range(MODE == kPanel ? (int64_t)tiles_t * splits : (int64_t)tiles_t * tiles_c * (MODE == kParts ? splits : 1));
+    if (mine_of.begin >= mine_of.end) return;
+    const int part = MODE != kWhole ? (int)(mine_of.begin % splits) : 0, k0 = MODE == kParts ? part * share : 0;
+    const int kts = MODE == kParts ? (a.kt - k0 < share ? a.kt - k0 : share) : a.kt;
+    const int panel_t = MODE == kPanel ? (int)(mine_of.begin / splits) : 0;
+    const WgTileRange range = MODE == kPanel ? WgTileRange{(int64_t)part * share, (part + 1) * share < tiles_c ? (part + 1) * share : tiles_c, 1} : mine_of;
+    if (MODE == kPanel && range.begin >= range.end) return;
+    auto place_of = [&](int64_t tile) -> TileAt {
+        if constexpr (MODE == kPanel) return {panel_t, (int)tile};
+        else return tile_at((int)(MODE == kParts ? tile / splits : tile), tiles_t, tiles_c);
+    };
+    extern __shared__ __align__(16) int8_t panel[];
 
     // of the tile that is being copied: rows behind the last one read the last one, blocks behind the last one the last one
     __amdgpu_buffer_rsrc_t q_tile, w_tile;
-    int q_at[QL], w_at[WL];
+    int q_at[QL > 0 ? QL : 1], w_at[WL];
     auto aim = [&](int64_t tile) {
-        const TileAt at = tile_at((int)(SPLIT ? tile / splits : tile), tiles_t, tiles_c);
+        const TileAt at = place_of(tile);
         const int t0 = at.t * S::tokens, b0 = at.c * (S::channels / kPackC);
-        q_tile = ws_rsrc(a.q + (int64_t)t0 * a.ldq, kWsMaxBytes);
+        if constexpr (QL > 0) q_tile = ws_rsrc(a.q + (int64_t)t0 * a.ldq, kWsMaxBytes);
         w_tile = ws_rsrc(a.w + (int64_t)b0 * w_block_bytes, kWsMaxBytes);
 #pragma unroll
         for (int i = 0; i < QL; ++i) {
@@ -217,7 +288,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     // (rows 8 on: their low bits are the same but for one)
     const int q_chunk[2] = {lane % 8 ^ chunk_swizzle(lane / 8), lane % 8 ^ chunk_swizzle(lane / 8 + 8)};
     auto copy = [&](int8_t* buf, int tile_kt) {
-        const int kt = SPLIT ? k0 + tile_kt : tile_kt;
+        const int kt = k0 + tile_kt;
         int at[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {                          // chunks behind a row's last one: any, their weights are zero
@@ -230,15 +301,16 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             copy_to_lds(q_tile, q_at[i] + (S::waves % 2 == 0 ? (wave % 2 ? at[1] : at[0]) : (rows / 8 % 2 ? at[1] : at[0])), 0, buf + rows * kPackK);
         }
 #pragma unroll
-        for (int i = 0; i < WL; ++i) copy_to_lds(w_tile, w_at[i], kt * (kPackK * kPackC), buf + S::tokens * kPackK + (i * S::waves + wave) * 1024);
+        for (int i = 0; i < WL; ++i) copy_to_lds(w_tile, w_at[i], kt * (kPackK * kPackC), buf + S::copied * kPackK + (i * S::waves + wave) * 1024);
     };
     i32x4 qf[2][FT], wf[2][FC];
     // (32 rows on, the low bits that exchange chunks are the same)
     const int q_lane = (tw * FT * 32 + lane % 32) * kPackK + (lane / 32 ^ chunk_swizzle(lane % 32)) * 16;
-    const int w_lane = S::tokens * kPackK + cw * FC * (kPackK * kPackC) + lane * 16;
-    auto operands = [&](int8_t* buf, int ks) {
+    const int w_lane = S::copied * kPackK + cw * FC * (kPackK * kPackC) + lane * 16;
+    auto operands = [&](int8_t* buf, int kt, int ks) {
+        const int8_t* rows = MODE == kPanel ? panel + kt * (S::tokens * kPackK) : buf;
 #pragma unroll
-        for (int t = 0; t < FT; ++t) qf[ks % 2][t] = *reinterpret_cast<const i32x4*>(buf + (q_lane ^ ks * 32) + t * (32 * kPackK));
+        for (int t = 0; t < FT; ++t) qf[ks % 2][t] = *reinterpret_cast<const i32x4*>(rows + (q_lane ^ ks * 32) + t * (32 * kPackK));
 #pragma unroll
         for (int f = 0; f < FC; ++f) wf[ks % 2][f] = *reinterpret_cast<const i32x4*>(buf + w_lane + f * (kPackK * kPackC) + ks * 1024);
     };
@@ -261,7 +333,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     auto k_tile = [&](int kt, int8_t* buf, int8_t* next) {
 #pragma unroll
         for (int ks = 0; ks < kSteps - 1; ++ks) {
-            operands(buf, ks + 1);
+            operands(buf, kt, ks + 1);
             if constexpr (FT * FC < 8) __builtin_amdgcn_sched_barrier(0);
             multiply(ks);
             if constexpr (FT * FC >= 8) {                      // an operand read between two products (2 % of large tiles)
@@ -279,7 +351,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             else wait_but(behind > 0 ? behind : 0);
         }
         meet();
-        operands(next, 0);                                     // (behind a tile's last K-tile: anything, nobody uses it)
+        operands(next, kt + 1 < kts ? kt + 1 : kt, 0);         // (behind a tile's last K-tile: anything, nobody uses it)
         int from = kt + NB;
         if (from >= kts) {                                     // the next tile's K-tile of this buffer
             if (from == kts || (kts < NB && kt == 0)) {
@@ -296,13 +368,22 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     unrolled<NB>([&](auto i) {
         if (decltype(i)::value < kts) copy(buffer(i), decltype(i)::value);
     });
+    if constexpr (MODE == kPanel) {
+        float* const scales = reinterpret_cast<float*>(panel + kts * (S::tokens * kPackK));
+        constexpr int X = 8 / RowVec<T>::E;                    // (vectors of a lane: twice as many in fp32)
+        const int t0 = panel_t * S::tokens;
+        if (n.c <= 64) make_panel<T, X, S::tokens, S::waves>(n, t0, count, panel, scales);
+        else if (n.c <= 128) make_panel<T, 2 * X, S::tokens, S::waves>(n, t0, count, panel, scales);
+        else make_panel<T, 4 * X, S::tokens, S::waves>(n, t0, count, panel, scales);
+        static_assert(kPanelTiles * kPackK == 256, "... of rows that long");
+    }
     wait_but((kts < NB ? kts : NB) - 1);
     arrived = 1;
     meet();
-    operands(buf0, 0);
+    operands(buf0, 0, 0);
     const float hi = act_hi(a.act);
     for (int64_t tile = range.begin; tile < range.end; tile += range.step) {
-        const TileAt at = tile_at((int)(SPLIT ? tile / splits : tile), tiles_t, tiles_c);
+        const TileAt at = place_of(tile);
         const int t0 = at.t * S::tokens, c0 = at.c * S::channels;
 #pragma unroll
         for (int t = 0; t < FT; ++t)
@@ -315,7 +396,8 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             my_ws = a.w_scale[my_ch];
             if (a.bias != nullptr) my_bias = (float)static_cast<const T*>(a.bias)[my_ch];
         }
-        if ((int)threadIdx.x < S::tokens && my_row < count) my_rs = a.q_scale[my_row];
+        if constexpr (MODE != kPanel)
+            if ((int)threadIdx.x < S::tokens && my_row < count) my_rs = a.q_scale[my_row];
         int kt = 0;
 #pragma clang loop unroll(disable)
         for (; kt + NB <= kts; kt += NB)
@@ -324,7 +406,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             if (kt + decltype(i)::value < kts) k_tile(kt + decltype(i)::value, buffer(i), buffer(Int<decltype(i)::value + 1>{}));
         });
         arrived = NB;
-        if constexpr (SPLIT) {
+        if constexpr (MODE == kParts) {
             if (!last_part<FT * FC, S::threads>(reinterpret_cast<i32x16*>(acc), a.partial, a.arrived, (int)(tile / splits), part, splits, out_lds)) return;
         }
         wait_loads<0>();                                       // the next tile's first K-tiles have arrived, ...
@@ -333,12 +415,14 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             factors[threadIdx.x] = my_ws;
             factors[S::channels + threadIdx.x] = my_bias;
         }
-        if ((int)threadIdx.x < S::tokens) factors[2 * S::channels + threadIdx.x] = my_rs;
+        if constexpr (MODE != kPanel)
+            if ((int)threadIdx.x < S::tokens) factors[2 * S::channels + threadIdx.x] = my_rs;
+        const float* row_factors = MODE == kPanel ? reinterpret_cast<const float*>(panel + kts * (S::tokens * kPackK)) : factors + 2 * S::channels;
         meet();                                                // ... everybody's
         f32x4 ws[FC][4], bias[FC][4];
         float rs[FT];
 #pragma unroll
-        for (int t = 0; t < FT; ++t) rs[t] = factors[2 * S::channels + (tw * FT + t) * 32 + lane % 32];
+        for (int t = 0; t < FT; ++t) rs[t] = row_factors[(tw * FT + t) * 32 + lane % 32];
 #pragma unroll
         for (int f = 0; f < FC; ++f)
 #pragma unroll
@@ -387,17 +471,30 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
                 }
                 lds_wave_sync();
             }
-        operands(buf0, 0);                                     // (read here and not at the tile's begin: nothing is left to be waited for)
+        operands(buf0, 0, 0);                                  // (read here and not at the tile's begin: nothing is left to be waited for)
     }
 }
 
-template <typename T, int TW, int CW, int FT, int FC, int NB, bool SPLIT = false>
-static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 1, int share = 0) {
-    using S = TileShape<T, TW, CW, FT, FC, NB>;
-    const int64_t tiles = cdiv(a.rows, S::tokens) * cdiv(a.n, S::channels) * splits;
-    const int64_t most = SPLIT ? tiles : (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
+template <typename T, int TW, int CW, int FT, int FC, int NB, TileMode MODE = kWhole>
+static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 1, int share = 0, const FewRows* rows = nullptr) {
+    using S = TileShape<T, TW, CW, FT, FC, NB, MODE>;
+    const int64_t tiles = cdiv(a.rows, S::tokens) * (MODE == kPanel ? 1 : cdiv(a.n, S::channels)) * splits;
+    const int64_t most = MODE != kWhole ? tiles : (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
     const int64_t grid = cdiv(tiles < most ? tiles : most, kXcd) * kXcd;   // (tile_range deals out to whole rounds of XCDs)
-    hipLaunchKernelGGL((rows_matmul_kernel<T, TW, CW, FT, FC, NB, SPLIT>), dim3((unsigned)grid), dim3(S::threads), 0, ctx->stream, a, splits, share);
+    if constexpr (MODE == kPanel) {
+        auto kern = rows_matmul_kernel<T, TW, CW, FT, FC, NB, MODE>;
+        const size_t panel = (size_t)a.kt * S::tokens * kPackK + S::tokens * sizeof(float);
+        static bool attr_set = false;
+        if (!attr_set) {
+            const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                       kPanelTiles * S::tokens * kPackK + S::tokens * (int)sizeof(float));
+            if (err != hipSuccess) return check_hip(ctx, err, "hipFuncSetAttribute(rows_matmul_kernel)");
+            attr_set = true;
+        }
+        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(S::threads), panel, ctx->stream, a, splits, share, *rows);
+    } else {
+        hipLaunchKernelGGL((rows_matmul_kernel<T, TW, CW, FT, FC, NB, MODE>), dim3((unsigned)grid), dim3(S::threads), 0, ctx->stream, a, splits, share, 0);
+    }
     return check_hip(ctx, hipGetLastError(), "rows_matmul_kernel launch");
 }
 
@@ -411,12 +508,6 @@ static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 
 constexpr int kFewWaves = 8, kAhead = 8;
 template <int G, int F> struct FewShape {
     static constexpr int sums = kFewWaves * G * F * kWave * 16;
-};
-struct FewRows {                 // what NORM > 0 needs to know of the rows
-    const void *x, *w, *b;
-    const int32_t* idx;
-    int ldx, map_rows, c, kind;
-    float eps;
 };
 
 template <typename T, int G, int F, int NORM, int NV>
@@ -566,26 +657,34 @@ template <typename T, int G, int F, int NORM, int NV> static dcnn_status launch_
     return check_hip(ctx, hipGetLastError(), "rows_few_kernel launch");
 }
 
+// ---- norm, 8-bit rows and product in one kernel ---------------------------------------------------------------------------
 // Rows that every workgroup norms for itself: 512 lanes hold a row in one or two vectors each.
 constexpr int kFewNorm = 4;
-bool rows_linear_fuses(int dtype, int64_t rows, int64_t k) { return rows <= kFewNorm && align_up((size_t)k, 64) <= (dtype == DCNN_F32 ? 4096 : 8192); }
+static bool fuses_few(int dtype, int64_t rows, int64_t k) { return rows <= kFewNorm && align_up((size_t)k, 64) <= (dtype == DCNN_F32 ? 4096 : 8192); }
+// Short rows of which all tiles are in work at a time, in workgroups that norm 64 of them each.
+static int64_t panel_tiles(int64_t rows, int64_t n, bool counted) { return cdiv(counted ? cdiv(rows, 4) : rows, 64) * cdiv(n, 128); }
+bool rows_linear_fuses(int dtype, int64_t rows, int64_t k, int64_t n, bool counted) {
+    return fuses_few(dtype, rows, k) || (packed_k(k) <= kPanelTiles * kPackK && panel_tiles(rows, n, counted) <= 2 * kPlanCus);
+}
 
-template <typename T> static dcnn_status launch_linear_few_t(dcnn_ctx* ctx, const FewRows& n, const MatmulArgs& a) {
+template <typename T> static dcnn_status launch_linear_t(dcnn_ctx* ctx, const FewRows& n, const MatmulArgs& a) {
+    if (!fuses_few(sizeof(T) == 4 ? DCNN_F32 : DCNN_F16, a.rows, n.c)) {
+        const int64_t tiles_c = cdiv(a.n, 128);
+        return launch_tile<T, 2, 4, 1, 1, 2, kPanel>(ctx, a, (int)tiles_c, 1, &n);
+    }
     const bool one = (int64_t)cdiv(n.c, 64) * 64 <= kFewWaves * kWave * RowVec<T>::E;
     if (a.rows == 1) return one ? launch_few<T, 1, 1, 1, 1>(ctx, a, n) : launch_few<T, 1, 1, 1, 2>(ctx, a, n);
     return one ? launch_few<T, 1, 1, kFewNorm, 1>(ctx, a, n) : launch_few<T, 1, 1, kFewNorm, 2>(ctx, a, n);
 }
 
-dcnn_status launch_rows_linear_few(dcnn_ctx* ctx, int dtype, const NormArgs& norm, const MatmulArgs& a) {
+dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& norm, const MatmulArgs& a) {
     const FewRows n{norm.x, norm.pre_w, norm.pre_b, norm.idx, norm.ldx, norm.map_rows, norm.c, norm.pre, norm.pre_eps};
-    if (dtype == DCNN_F16) return launch_linear_few_t<f16>(ctx, n, a);
-    if (dtype == DCNN_BF16) return launch_linear_few_t<bf16>(ctx, n, a);
-    return launch_linear_few_t<float>(ctx, n, a);
+    if (dtype == DCNN_F16) return launch_linear_t<f16>(ctx, n, a);
+    if (dtype == DCNN_BF16) return launch_linear_t<bf16>(ctx, n, a);
+    return launch_linear_t<float>(ctx, n, a);
 }
 
 // ---- which kernel ------------------------------------------------------------------------------------------------------
-constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
-
 // us, in a row on the GPU, weights from memory (rows, k -> n); a launch alone is 3.2:
 //   17 to 32 rows: few / tiles of 64   24, 4096 -> 4096: 8.9 / 11.1   24, 1024 -> 256: 4.6 / 5.1   32, 8192 -> 1024: 11.3 / 10.9   32, 16384 -> 512: 19.5 / 12.5
 //   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 51   1000, 4096 -> 4096 (256): 39 / 25 / 33 / 51
@@ -632,7 +731,7 @@ template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const Ma
             // 32 channels to a workgroup where that makes one for every compute unit: 32, 2048 -> 8192: 9.3 against 10.2; 4096 -> 4096: 10.7, 9.3
             if (a.n >= 32 * kPlanCus) return a.rows <= 16 ? launch_few<T, 1, 2, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 2, 0, 1>(ctx, a, FewRows{});
             return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
-        case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, true>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
+        case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, kParts>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
         case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 4>(ctx, a);
         case kTile128Short: return launch_tile<T, 2, 4, 2, 1, 2>(ctx, a);
         case kTile128: return launch_tile<T, 2, 2, 2, 2, 2>(ctx, a);

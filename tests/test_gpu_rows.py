@@ -363,6 +363,26 @@ def test_product_large(ctx, rows, k, n):
     check_product(ctx, np.random.default_rng(rows), "bf16", rows, k, n, "none")
 
 
+@pytest.mark.parametrize("rows,k,n", [(2000, 1200, 1500), (4100, 700, 4100), (4100, 1100, 4400), (9000, 300, 4100), (8200, 1100, 8200), (2300, 2500, 2100), (130, 9000, 130), (33, 16500, 70)])
+def test_product_tiles(ctx, rows, k, n):
+    """Every size of tile, workgroups with several of them, even and odd numbers of K-tiles; all rows, a part of them by a count on the GPU.
+    (The reference in 64 bits is of some rows, on the GPU: a product of whole numbers below 2^53.)"""
+    rng = np.random.default_rng(rows)
+    q, qs = q_rows(rng, rows, k)
+    w, ws = q_weights(rng, k, n)
+    bias = rand(rng, n, "f32")
+    weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias)
+    for count in (rows, rows - 37, 70, 1):
+        out = torch.full((rows, n), 3.0, device="cuda")
+        weights.matmul(q, qs, out=out, dtype=torch.float32, count=torch.tensor([count], dtype=torch.int32, device="cuda") if count < rows else None)
+        ctx.sync()
+        some = np.unique(np.concatenate([np.arange(min(count, 40)), rng.integers(0, count, 200), np.arange(max(0, count - 40), count)]))
+        at = torch.from_numpy(some).cuda()
+        s = (q[at].double() @ w.double()) * qs[at].double()[:, None] * ws.double()
+        close(out[at], np64(s + bias.double()), "f32", np64(4 * U32 * (s.abs() + bias.double().abs())), f"{rows}x{k}x{n} count {count}")
+        assert (out[count:] == 3.0).all()
+
+
 def test_product_sums_are_exact_at_their_largest(ctx):
     """Every product at its largest magnitude over the longest k: 65536 * 127 * 127 and 65536 * 128 * 128 fit 32 bits."""
     for rows in (1, 3, 20, 140):
@@ -437,11 +457,7 @@ def linear64(v, w, ws, bias, act):
     return act64(np.rint(at) @ np64(w) * (amax / 127) * np64(ws) + (0 if bias is None else np64(bias)), act), at, amax / 127
 
 
-@pytest.mark.parametrize("dt", list(TYPES))
-@pytest.mark.parametrize("rows,k,n", [(1, 64, 40), (1, 4096, 300), (2, 2048, 513), (4, 1000, 77), (7, 513, 1000), (16, 4096, 96), (17, 96, 33), (40, 300, 200), (200, 256, 1024), (700, 130, 260)])
-@pytest.mark.parametrize("kind", ["none", "rms", "layer"])
-@pytest.mark.parametrize("on_map", [False, True])
-def test_linear(ctx, dt, rows, k, n, kind, on_map):
+def check_linear(ctx, dt, rows, k, n, kind, on_map):
     rng = np.random.default_rng([rows, k])
     case = NormCase(dt, rows, k, pre=kind, on_map=on_map, seed=2)
     if on_map and rows <= 4:                                       # a list without room to spare: rows are normed on the spot
@@ -466,6 +482,22 @@ def test_linear(ctx, dt, rows, k, n, kind, on_map):
     two = pkg.RowWeights(ctx, w, scale=ws, bias=bias, act="relu").matmul(q, qs, dtype=TYPES[dt][0], count=case.count)
     ctx.sync()
     assert torch.equal(y[:rows], two[:rows])
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows,k,n", [(1, 64, 40), (1, 4096, 300), (2, 2048, 513), (4, 1000, 77), (7, 513, 1000), (16, 4096, 96), (17, 96, 33), (40, 300, 200), (200, 256, 1024), (700, 130, 260)])
+@pytest.mark.parametrize("kind", ["none", "rms", "layer"])
+@pytest.mark.parametrize("on_map", [False, True])
+def test_linear(ctx, dt, rows, k, n, kind, on_map):
+    check_linear(ctx, dt, rows, k, n, kind, on_map)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("k", [1, 2, 3, 5, 7, 8, 9, 16, 17, 31, 33, 63, 64, 65, 100, 127, 128, 129, 200, 255, 256, 257])
+def test_linear_of_short_rows(ctx, dt, k):
+    """Rows of a few channels, which one kernel norms, quantises and multiplies; on both sides of a tile of 64 tokens."""
+    for rows, n, kind, on_map in ((5, 70, "rms", False), (64, 33, "none", True), (65, 200, "layer" if k > 1 else "rms", True), (150, 129, "none", False)):
+        check_linear(ctx, dt, rows, k, n, kind, on_map)
 
 
 @pytest.mark.parametrize("rows", [1, 6, 90])
