@@ -372,7 +372,7 @@ def test_product_tiles(ctx, rows, k, n):
     w, ws = q_weights(rng, k, n)
     bias = rand(rng, n, "f32")
     weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias)
-    for count in (rows, rows - 37, 70, 1):
+    for count in (rows, max(1, rows - 37), min(70, rows), 1):
         out = torch.full((rows, n), 3.0, device="cuda")
         weights.matmul(q, qs, out=out, dtype=torch.float32, count=torch.tensor([count], dtype=torch.int32, device="cuda") if count < rows else None)
         ctx.sync()
