@@ -279,7 +279,8 @@ dcnn_status dcnn_net_stats(dcnn_net* net, dcnn_stats* stats_host);
 /* ---- rows: per-token operators ---------------------------------------------------------------- */
 /* A row is the channel vector of one token: one pixel of an NHWC map seen as [map_rows, c], or one row of a plain
  * matrix.  Blocks that treat every pixel by itself (norm, expansion, projection, gated residual) give the same values
- * whether they run on the whole map or on the flagged pixels alone, so each operator takes a list as layers hand it out:
+ * whether they run on the whole map or on the flagged pixels alone (up to the order of a norm's sums, which depends on
+ * the size of a call), so each operator takes a list as layers hand it out:
  *   idx_dev    NULL: row r of the operator is row r of the maps.  Else entry r names the map row (dcnn_delta.idx).
  *              An entry outside 0 .. map_rows-1 is a row without a token: nothing of a map is read or written for it,
  *              its compact outputs are zero.  Entries that are written through (y) must be distinct.
@@ -342,8 +343,9 @@ dcnn_status dcnn_rows_pack(dcnn_ctx* ctx, int32_t dtype, int64_t k, int64_t n, c
 /* y[r][j] = act( (sum_k q[r][k] * w[k][j]) * (q_scale[r] * w_scale[j]) + bias[j] ).
  * dcnn_rows_matmul takes rows that are 8-bit integers already; dcnn_rows_linear takes the rows of a map in the type of
  * y, norms them with `pre` (or not: NONE) and quantises them as dcnn_rows_norm does: two of a block's steps in one call.
- * scratch_dev: dcnn_rows_scratch_bytes(rows, k, n) bytes (may be 0), 256-byte aligned, zero-filled before its first use
- * and left alone by the caller between calls; calls that share it must not overlap. */
+ * scratch_dev: dcnn_rows_scratch_bytes(rows, k, n, linear) bytes (linear: 1 for dcnn_rows_linear, 0 for dcnn_rows_matmul;
+ * 0 bytes where a size is out of range), 256-byte aligned, zero-filled before its first use and left alone by the caller
+ * between calls; calls of any sizes may share it one after the other, calls that share it must not overlap. */
 typedef struct {
     dcnn_row_list list;         /* matmul: rows and count_dev only                      */
     int32_t       dtype;        /* of y, bias and x: F32, F16, BF16                     */
@@ -362,7 +364,7 @@ typedef struct {
     void*         scratch_dev;
     size_t        scratch_bytes;
 } dcnn_rows_matmul_args;
-size_t      dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n);
+size_t      dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n, int32_t linear);
 dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
 dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
 

@@ -158,7 +158,7 @@ def load_library() -> C.CDLL:
     lib.dcnn_rows_weights_bytes.argtypes = [C.c_int64, C.c_int64]
     lib.dcnn_rows_weights_bytes.restype = sz
     lib.dcnn_rows_pack.argtypes = [vp, i32, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp, sz]
-    lib.dcnn_rows_scratch_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+    lib.dcnn_rows_scratch_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64, i32]
     lib.dcnn_rows_scratch_bytes.restype = sz
     lib.dcnn_rows_matmul.argtypes = [vp, P(RowsMatmulArgs)]
     lib.dcnn_rows_linear.argtypes = [vp, P(RowsMatmulArgs)]
@@ -512,20 +512,22 @@ class RowWeights:
         if (scale is not None) != (code == I8) or (scale is not None and (scale.shape != (n,) or scale.dtype != torch.float32 or
                                                                           not scale.is_contiguous() or not scale.is_cuda)):
             raise ValueError(f"8-bit weights come with a float32 scale [{n}] on the device, others without one")
-        self.k, self.n, self.bias, self.scale = k, n, bias, scale
+        self.k, self.n, self.bias = k, n, bias
         nbytes = lib.dcnn_rows_weights_bytes(k, n)
         if nbytes == 0:
             raise ValueError(f"weights [{k}, {n}] are out of range")
         self.packed = ctx.empty(nbytes, torch.uint8)
         ctx.check(lib.dcnn_rows_pack(ctx.handle, code, k, n, weights.data_ptr(), weights.stride(0) if k > 1 else n, _ptr(scale),
                                      self.packed.data_ptr(), nbytes))
-        self._source = weights                                    # until the stream has read it
+        for t in (weights, scale):                                # (their memory is theirs until the stream has read them)
+            if t is not None:
+                t.record_stream(ctx.stream)
         if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
             raise ValueError(f"bias must be a contiguous device tensor [{n}]")
         self.act, self._bias = ACT_CODES[act], _ptr(bias) or None
-        self._scratch, self._scratch_bytes, self._scratch_rows = None, 0, -1
+        self._scratch, self._scratch_bytes, self._scratch_rows = None, 0, [-1, -1]
 
-    def _call(self, call, a, rows, dt, count, out):
+    def _call(self, call, linear, a, rows, dt, count, out):
         ctx = self.ctx
         if self.bias is not None and self.bias.dtype != dt:
             raise ValueError(f"the bias is {self.bias.dtype}, the output {dt}")
@@ -539,26 +541,28 @@ class RowWeights:
             a.y, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.index)
             rows = min(rows, n)
         a.rows = rows
-        if rows > self._scratch_rows:
-            self._grow(rows)
+        if rows > self._scratch_rows[linear]:
+            self._grow(rows, linear)
         a.scratch, a.scratch_bytes = self._scratch.data_ptr(), self._scratch_bytes
         st = call(ctx.handle, a)
         if st:
             ctx.check(st)
         return out
 
-    def _grow(self, rows):
-        """Scratch for up to this many rows."""
-        self._scratch_bytes = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n)
-        with torch.cuda.stream(self.ctx.stream):
-            self._scratch = torch.zeros(self._scratch_bytes, dtype=torch.uint8, device=self.ctx.device)
-        self._scratch_rows = rows
+    def _grow(self, rows, linear):
+        """Scratch for calls of one kind with up to this many rows."""
+        need = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n, linear)
+        self._scratch_rows[linear] = rows
+        if need > self._scratch_bytes:
+            with torch.cuda.stream(self.ctx.stream):
+                self._scratch = torch.zeros(need, dtype=torch.uint8, device=self.ctx.device)
+            self._scratch_bytes = need
 
     def matmul(self, q, q_scale, *, dtype=torch.float16, count=None, out=None):
         """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`."""
         a = RowsMatmulArgs()
         a.q, a.q_scale, a.ldq = _check_q(q, q_scale, self.k, self.ctx.index)
-        return self._call(self.ctx.lib.dcnn_rows_matmul, a, q.shape[0], dtype, count, out)
+        return self._call(self.ctx.lib.dcnn_rows_matmul, 0, a, q.shape[0], dtype, count, out)
 
     def linear(self, x, *, pre=None, idx=None, count=None, out=None):
         """dcnn_rows_linear: rows of the map x (those that idx names), normed with `pre`, quantised and multiplied; [rows, n]."""
@@ -569,7 +573,7 @@ class RowWeights:
             a.idx, rows = _int32(idx, "idx", dev), idx.numel()
         if pre is not None:
             a.pre_kind, a.pre_eps, a.pre_w, a.pre_b = pre.pointers(self.k, dt, dev)
-        return self._call(self.ctx.lib.dcnn_rows_linear, a, rows, dt, count, out)
+        return self._call(self.ctx.lib.dcnn_rows_linear, 1, a, rows, dt, count, out)
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

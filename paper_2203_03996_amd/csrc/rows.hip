@@ -63,7 +63,7 @@ struct Scratch {
     }
 };
 
-dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul_args* p, MatmulArgs* m) {
+dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul_args* p, int linear, MatmulArgs* m) {
     if (!rows_float(p->dtype)) return fail(ctx, DCNN_EDTYPE, "%s: dtype %d", what, p->dtype);
     if (p->act < DCNN_ACT_NONE || p->act > DCNN_ACT_RELU6) return fail(ctx, DCNN_EINVAL, "%s: activation %d", what, p->act);
     if (dcnn_rows_weights_bytes(p->k, p->n) == 0) return fail(ctx, DCNN_EINVAL, "%s: k %lld, n %lld", what, (long long)p->k, (long long)p->n);
@@ -76,7 +76,7 @@ dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul
     st = check_ld(ctx, what, "y", p->y_dev, p->ldy, p->n, es);
     if (st != DCNN_OK) return st;
     if (!aligned(p->bias_dev, es)) return fail(ctx, DCNN_EINVAL, "%s: bias is not aligned to its elements", what);
-    const size_t need = dcnn_rows_scratch_bytes(p->list.rows, p->k, p->n);
+    const size_t need = dcnn_rows_scratch_bytes(p->list.rows, p->k, p->n, linear);
     if (p->scratch_bytes < need) return fail(ctx, DCNN_ENOMEM, "%s: scratch of %zu bytes, %zu needed", what, p->scratch_bytes, need);
     if (p->scratch_dev == nullptr || !aligned(p->scratch_dev, kAlign)) return fail(ctx, DCNN_EINVAL, "%s: scratch null or not 256-byte aligned", what);
     m->w = static_cast<const int8_t*>(p->packed_dev);
@@ -161,9 +161,10 @@ dcnn_status dcnn_rows_pack(dcnn_ctx* ctx, int32_t dtype, int64_t k, int64_t n, c
     return launch_rows_pack(ctx, dtype, k, n, w_dev, ldw, scale_dev, packed, reinterpret_cast<float*>(packed + packed_scale_offset(k, n)));
 }
 
-size_t dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n) {
+size_t dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n, int32_t linear) {
     if (rows < 0 || rows > kRowsMax || dcnn_rows_weights_bytes(k, n) == 0) return 0;
-    return Scratch(rows, k, n).bytes;
+    const Scratch s(rows, k, n);
+    return linear ? s.bytes : s.scales;
 }
 
 dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
@@ -171,7 +172,7 @@ dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     if (!ctx || !p) return DCNN_EINVAL;
     if (p->x_dev != nullptr || p->list.idx_dev != nullptr) return fail(ctx, DCNN_EINVAL, "%s: x and idx belong to rows_linear", what);
     MatmulArgs m;
-    dcnn_status st = check_matmul(ctx, what, p, &m);
+    dcnn_status st = check_matmul(ctx, what, p, 0, &m);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->k);
     if (st != DCNN_OK) return st;
@@ -185,7 +186,7 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     if (p->q_dev != nullptr || p->q_scale_dev != nullptr) return fail(ctx, DCNN_EINVAL, "%s: q belongs to rows_matmul", what);
     if (p->k > kRowsMaxC) return fail(ctx, DCNN_EUNSUPPORTED, "%s: k %lld, %d at most", what, (long long)p->k, kRowsMaxC);
     MatmulArgs m;
-    dcnn_status st = check_matmul(ctx, what, p, &m);
+    dcnn_status st = check_matmul(ctx, what, p, 1, &m);
     if (st == DCNN_OK) st = check_map(ctx, what, p->list);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK && p->x_dev == nullptr) st = fail(ctx, DCNN_EINVAL, "%s: x is null", what);

@@ -75,6 +75,12 @@ __global__ __launch_bounds__((NormShape<T, L>::threads), 4) void rows_norm_kerne
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[j][e] = have_x ? row_get<T>(xv[j], e) + a.scale * v[j][e] : a.scale * v[j][e];
             }
+            // in place, where a row's last vector holds elements of the one before it and another wave may have that one: all of the row has
+            // been read before any of it is written
+            if (L > kWave && a.y == a.x && c % E != 0) {
+                __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0)
+                __syncthreads();
+            }
             if (a.y != nullptr && token) {
                 T* y = static_cast<T*>(a.y) + i * a.ldy;
 #pragma unroll

@@ -204,6 +204,18 @@ def test_norm_in_place_and_strided(ctx):
         assert (np64(z)[19:] == 0.0).all(), "rows behind the count were written"
 
 
+@pytest.mark.parametrize("dt,widths", [("f16", (513, 1025, 1029, 2049, 4097, 8195)), ("bf16", (1025, 4100)), ("f32", (257, 513, 514, 1025, 4097))])
+def test_norm_in_place_at_odd_widths(ctx, dt, widths):
+    """A row's last vector shares elements with the one before it, which another wave may hold: nothing is written that is still to be read."""
+    for c in widths:
+        for post in ("none", "rms"):
+            case = NormCase(dt, 300, c, post, "rms", "none", seed=4)
+            y64, ys, z64, zs = case.want()
+            case.run(ctx, y=case.x, z=True)
+            ctx.sync()
+            close(case.x, y64, dt, ys, f"c={c} post {post}")
+
+
 def test_norm_lists(ctx):
     """Counts of zero, below zero and beyond the room; entries that name no row."""
     case = NormCase("f16", 40, 72, on_map=True)
@@ -684,7 +696,7 @@ def test_c_refusals(ctx):
     assert lib.dcnn_rows_pack(ctx.handle, 0, 64, 64, None, 64, None, packed, nbytes) == 1
     assert lib.dcnn_rows_pack(None, 0, 64, 64, p, 64, None, packed, nbytes) == 1
 
-    scratch = torch.zeros(lib.dcnn_rows_scratch_bytes(4, 64, 64) + 256, dtype=torch.uint8, device="cuda")
+    scratch = torch.zeros(lib.dcnn_rows_scratch_bytes(4, 64, 64, 1) + 256, dtype=torch.uint8, device="cuda")
 
     def product(linear, **kw):
         a = RowsMatmulArgs(k=64, n=64, packed=packed, y=o, ldy=64, scratch=scratch.data_ptr(), scratch_bytes=scratch.numel())
@@ -703,7 +715,7 @@ def test_c_refusals(ctx):
     assert product(False, x=p) == 1 and product(False, idx=p) == 1 and product(False, q=None) == 1 and product(False, q_scale=None) == 1
     assert product(False, ldq=60) == 1 and product(False, ldq=48) == 2 and product(False, q=q.data_ptr() + 4) == 1
     assert product(True, q=q.data_ptr()) == 1 and product(True, x=None) == 1 and product(True, ldx=60) == 2 and product(True, rows=5) == 2
-    assert product(True, scratch_bytes=64) == 5 and product(True, scratch=None) == 1 and product(True, scratch=scratch.data_ptr() + 16) == 1
+    assert product(True, scratch_bytes=64) == 5 and product(False, scratch_bytes=64) == 5 and product(True, scratch=None) == 1 and product(True, scratch=scratch.data_ptr() + 16) == 1
     assert product(True, k=40000, packed=packed) == 7
     for call in (lib.dcnn_rows_linear, lib.dcnn_rows_matmul):
         assert call(None, None) == 1 and call(ctx.handle, None) == 1

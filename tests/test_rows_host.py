@@ -14,10 +14,11 @@ def test_sizes_of_packed_weights_and_scratch():
         need = -(-k // 128) * 128 * (-(-n // 32) * 32) + -(-n // 32) * 32 * 4      # 8-bit weights in whole blocks, a scale per channel
         assert need <= size(k, n) < need + 256 and size(k, n) % 256 == 0
     for k, n in ((0, 4), (4, 0), (-1, 4), (65537, 4), (4, (1 << 24) + 1)):
-        assert size(k, n) == 0 and lib.dcnn_rows_scratch_bytes(4, k, n) == 0
+        assert size(k, n) == 0 and lib.dcnn_rows_scratch_bytes(4, k, n, 1) == 0
     for rows, k in ((0, 64), (1, 1), (7, 65), (1000, 4096)):
-        assert lib.dcnn_rows_scratch_bytes(rows, k, 64) >= rows * (k + 4)
-    assert lib.dcnn_rows_scratch_bytes(-1, 64, 64) == 0
+        assert lib.dcnn_rows_scratch_bytes(rows, k, 64, 1) >= rows * (k + 4) + lib.dcnn_rows_scratch_bytes(rows, k, 64, 0)
+        assert lib.dcnn_rows_scratch_bytes(rows, k, 64, 0) < 16 << 20          # (counts and partial sums)
+    assert lib.dcnn_rows_scratch_bytes(-1, 64, 64, 0) == 0
 
 
 def test_calls_without_a_context_are_refused():
