@@ -717,10 +717,10 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
     } else if (kt <= 4) {
         p.kernel = kTile128Short;
     } else {
-        // a tile of 256 takes 1.7 times as long as two of 128 side by side, on all compute units; pairs of the latter go out of step, so that
-        // half a round of them takes half the time
-        const int64_t rounds128 = tiles128 > 2 * kPlanCus ? tiles128 : 2 * kPlanCus;
-        p.kernel = 17 * 2 * kPlanCus * cdiv(tiles256, kPlanCus) <= 10 * rounds128 ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
+        // a round of tiles of 256 takes 1.7 times as long as one of tiles of 128 (two to a compute unit), of a short k or where it is not full 2.1
+        const int64_t rounds256 = cdiv(tiles256, kPlanCus), rounds128 = cdiv(tiles128, 2 * kPlanCus);
+        const bool full = 10 * tiles256 >= 9 * rounds256 * kPlanCus;
+        p.kernel = (kt >= 8 && full ? 17 : 21) * rounds256 <= 10 * rounds128 ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
     }
     return p;
 }
