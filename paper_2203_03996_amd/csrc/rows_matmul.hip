@@ -77,6 +77,13 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 //
 // The sums leave through LDS, a wave's 32 tokens by 128 bytes at a time: pieces of rows, 16 bytes a lane, where the matrix cores' order
 // would store 16 bytes from 32 rows.
+//
+// 16384 x 4096 -> 4096 in bf16: 244-250 us, 2.2 POP/s; 8192 x 8192 -> 4096: 230, 2.4 (a library's 8-bit product that leaves its 32-bit sums:
+// 248 and 226).  Power bounds these: the same product of zeros takes 183 us in place of 230; the clock is at 1.8 GHz, and the matrix cores are
+// busy 60 % of its cycles.  Per tile of 256 x 256 about 5 us of 60 are the outputs'.  What it took, us for
+// the first of them: one K-tile staged through registers behind a barrier 328; loads two K-tiles and operands a step ahead 295; copies
+// straight into LDS 272; scales and bias by one load each, dealt out in LDS, and no wait for stores 250.  26214 x 256 -> 1024 in fp16 is bound
+// by its outputs: 20 us, 3.4 TB/s.
 constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
 constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
 constexpr int kPanelTiles = 2;                 // K-tiles of rows that a workgroup makes for itself and keeps
@@ -505,6 +512,9 @@ static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 
 //
 // NORM > 0: up to NORM tokens are normed and quantised on the spot, by every workgroup for itself (a row is 8 KB that the caches hold, a
 // launch of its own takes longer), while the first weights are on their way.
+//
+// Bound by the weights' bytes and the launch (3.2 us): 1 x 4096 -> 4096 5.8 us in a row (6.5 TB/s behind the launch), 16 rows 7.0, 32 rows
+// 9.1 (their 8-bit rows from L2, as many bytes as the weights); 1 x 8192 -> 1024 5.5.
 constexpr int kFewWaves = 8, kAhead = 8;
 template <int G, int F> struct FewShape {
     static constexpr int sums = kFewWaves * G * F * kWave * 16;
@@ -719,7 +729,7 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
     } else {
         // a round of tiles of 256 takes 1.7 times as long as one of tiles of 128 (two to a compute unit), of a short k or where it is not full 2.1
         const int64_t rounds256 = cdiv(tiles256, kPlanCus), rounds128 = cdiv(tiles128, 2 * kPlanCus);
-        const bool full = 10 * tiles256 >= 9 * rounds256 * kPlanCus;
+        const bool full = 10 * tiles256 >= 8 * rounds256 * kPlanCus;
         p.kernel = (kt >= 8 && full ? 17 : 21) * rounds256 <= 10 * rounds128 ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
     }
     return p;
