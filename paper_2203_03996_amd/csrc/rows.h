@@ -53,7 +53,7 @@ struct MatmulArgs {
     uint32_t* arrived;           //    zero before the launch and after it
 };
 // Which kernel: a function of the sizes alone, since the scratch depends on it.
-enum MatmulKernel { kFewRows, kTile64, kTile128Deep, kTile128Short, kTile128, kTile256 };
+enum MatmulKernel { kFewRows, kTile64, kTile128Deep, kTile128, kTile256 };
 struct MatmulPlan {
     MatmulKernel kernel;
     int splits;                  // workgroups that share a tile's k (kTile64), each `share` K-tiles of it

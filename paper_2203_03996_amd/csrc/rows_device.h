@@ -147,6 +147,8 @@ template <typename T> __device__ __forceinline__ float row_get(u32x4 v, int e) {
     typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
     return (float)__builtin_bit_cast(Vec, v)[e];
 }
+// Stored past the L2: none of a row's elements is wanted there again before the kernel's end, and its lines would take the inputs' places
+// (16384 x 4096 bf16, y and z: 111 us -> 90; 26214 rows of 256 by a list 14.3 -> 12.4.)
 template <typename T> __device__ __forceinline__ void row_store(T* row, int base, int c, const float* o) {
     constexpr int E = RowVec<T>::E;
     const RowPart p = row_part<T>(base, c);
@@ -155,7 +157,7 @@ template <typename T> __device__ __forceinline__ void row_store(T* row, int base
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = (T)o[e];
     if (c >= E) {
-        *reinterpret_cast<typename RowVec<T>::type*>(row + p.at) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<typename RowVec<T>::type*>(row + p.at));
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)

@@ -76,14 +76,15 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 // of its number: the 16 lanes of a quarter of an operand load, 16 rows at one k, then cover all 64 banks.
 //
 // The sums leave through LDS, a wave's 32 tokens by 128 bytes at a time: pieces of rows, 16 bytes a lane, where the matrix cores' order
-// would store 16 bytes from 32 rows.
+// would store 16 bytes from 32 rows; past the L2, which has the operands to keep (26214 x 256 -> 1024: 20.3 us -> 18.7, 8000 x 256 -> 256:
+// 8.4 -> 6.9; 4096 -> 4096 the same, or 4 % at 60000 rows).
 //
 // 16384 x 4096 -> 4096 in bf16: 244-250 us, 2.2 POP/s; 8192 x 8192 -> 4096: 230, 2.4 (a library's 8-bit product that leaves its 32-bit sums:
 // 248 and 226).  Power bounds these: the same product of zeros takes 183 us in place of 230; the clock is at 1.8 GHz, and the matrix cores are
 // busy 60 % of its cycles.  Per tile of 256 x 256 about 5 us of 60 are the outputs'.  What it took, us for
 // the first of them: one K-tile staged through registers behind a barrier 328; loads two K-tiles and operands a step ahead 295; copies
 // straight into LDS 272; scales and bias by one load each, dealt out in LDS, and no wait for stores 250.  26214 x 256 -> 1024 in fp16 is bound
-// by its outputs: 20 us, 3.4 TB/s.
+// by its outputs: 18.7 us, 3.7 TB/s behind the launch.
 constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
 constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
 constexpr int kPanelTiles = 2;                 // K-tiles of rows that a workgroup makes for itself and keeps
@@ -241,17 +242,13 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     static_assert(S::threads >= S::channels && S::threads >= S::tokens && (2 * S::channels + S::tokens) * 4 <= S::waves * S::unit, "a thread for each factor");
     static_assert(QL * 8 * S::waves == S::copied && WL * 8 * S::waves == S::channels, "whole rounds of copies");
     // (an array each: what is read from one buffer does not wait for copies into the others)
-    __shared__ __align__(1024) int8_t buf0[S::stage], buf1[S::stage], buf2[NB > 2 ? S::stage : 16], buf3[NB > 3 ? S::stage : 16],
-        buf4[NB > 4 ? S::stage : 16], buf5[NB > 5 ? S::stage : 16], out_lds[S::waves * S::unit];
-    static_assert(NB >= 2 && NB <= 6, "an array for each buffer");
+    __shared__ __align__(1024) int8_t buf0[S::stage], buf1[S::stage], buf2[NB > 2 ? S::stage : 16], out_lds[S::waves * S::unit];
+    static_assert(NB == 2 || NB == 3, "an array for each buffer");
     auto buffer = [&](auto i) -> int8_t* {
         constexpr int I = decltype(i)::value % NB;
         if constexpr (I == 0) return buf0;
         else if constexpr (I == 1) return buf1;
-        else if constexpr (I == 2) return buf2;
-        else if constexpr (I == 3) return buf3;
-        else if constexpr (I == 4) return buf4;
-        else return buf5;
+        else return buf2;
     };
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int tw = wave / CW, cw = wave % CW;
@@ -469,7 +466,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
                     if (row >= count || ch >= a.n) continue;
                     T* y = static_cast<T*>(a.y) + (int64_t)row * a.ldy + ch;
                     if (ch + E <= a.n) {
-                        *reinterpret_cast<typename RowVec<T>::type*>(y) = v;
+                        __builtin_nontemporal_store((typename RowVec<T>::type)v, reinterpret_cast<typename RowVec<T>::type*>(y));
                     } else {
                         const T* from = reinterpret_cast<const T*>(mine + (r * PW + (p ^ r % PW)) * 16);
 #pragma clang loop unroll(disable)
@@ -697,10 +694,12 @@ dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& n
 // ---- which kernel ------------------------------------------------------------------------------------------------------
 // us, in a row on the GPU, weights from memory (rows, k -> n); a launch alone is 3.2:
 //   17 to 32 rows: few / tiles of 64   24, 4096 -> 4096: 8.9 / 11.1   24, 1024 -> 256: 4.6 / 5.1   32, 8192 -> 1024: 11.3 / 10.9   32, 16384 -> 512: 19.5 / 12.5
-//   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 51   1000, 4096 -> 4096 (256): 39 / 25 / 33 / 51
-//                                        2000, 4096 -> 4096 (512): 74 / 48 / 40 / 53   4000, 4096 -> 4096 (1024; 256 of 256): 128 / 94 / 81 / 66
-//                                        8000, 8192 -> 1024 (504; 128): 123 / 90 / 69 / 93   16384, 1000 -> 1531 (1536; 384): 59 / 45 / 40 / 45
-//   short k, 128 in eight waves / in four / 256   26214, 256 -> 1024: 20.3 / 21.9 / 21.4   4000, 1000 -> 1531: 15.0 / 15.5 / 25   16384, 4096 -> 4096: 292 / 284 / 244
+//   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 50   1000, 4096 -> 4096 (256): 35 / 25 / 33 / 50
+//                                        2000, 4096 -> 4096 (512): 67 / 46 / 40 / 50   4000, 4096 -> 4096 (1024; 256 of 256): 128 / 94 / 78 / 63
+//                                        8000, 8192 -> 1024 (504; 128): 123 / 90 / 69 / 93   16384, 1000 -> 1531 (1536; 384): 61 / 45 / 43 / 53
+//   128 in eight waves, three buffers / four   500, 2048 -> 8192: 13.8 / 14.4   2000, 2048 -> 2048: 13.6 / 14.2   1000, 4096 -> 4096: 25.0 / 24.5
+//   pairs of 128, in four waves each / in eight   26214, 256 -> 1024: 18.0 / 18.6   6000, 512 -> 1024: 9.1 / 8.6   26214, 1000 -> 1531: 65 / 73
+//   pairs of 128 / 256                   26214, 256 -> 1024: 17.9 / 19.4   16384, 512 -> 2048: 29.5 / 27.5   16384, 1000 -> 1531: 43 / 53   8000, 4096 -> 4096: 150 / 132
 //   k of a tile of 64 in one / in parts  64, 8192 -> 1024: 22 / 10.9 (8)   64, 4096 -> 4096: 17 / 11.0 (4)   200, 8192 -> 1024: 22 / 12.5 (4), 14.4 (8)
 //                                        500, 8192 -> 1024: 24 / 18.2 (2), 16.4 (4)   64, 1024 -> 256: 5.1 / 6.7 (2)
 MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
@@ -724,13 +723,11 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
         }
     } else if (tiles128 <= kPlanCus) {
         p.kernel = kTile128Deep;
-    } else if (kt <= 4) {
-        p.kernel = kTile128Short;
     } else {
         // a round of tiles of 256 takes 1.7 times as long as one of tiles of 128 (two to a compute unit), of a short k or where it is not full 2.1
         const int64_t rounds256 = cdiv(tiles256, kPlanCus), rounds128 = cdiv(tiles128, 2 * kPlanCus);
         const bool full = 10 * tiles256 >= 8 * rounds256 * kPlanCus;
-        p.kernel = (kt >= 8 && full ? 17 : 21) * rounds256 <= 10 * rounds128 ? kTile256 : (kt <= 8 ? kTile128Short : kTile128);
+        p.kernel = (kt >= 8 && full ? 17 : 21) * rounds256 <= 10 * rounds128 ? kTile256 : kTile128;
     }
     return p;
 }
@@ -742,8 +739,7 @@ template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const Ma
             if (a.n >= 32 * kPlanCus) return a.rows <= 16 ? launch_few<T, 1, 2, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 2, 0, 1>(ctx, a, FewRows{});
             return a.rows <= 16 ? launch_few<T, 1, 1, 0, 1>(ctx, a, FewRows{}) : launch_few<T, 2, 1, 0, 1>(ctx, a, FewRows{});
         case kTile64: return p.splits > 1 ? launch_tile<T, 2, 2, 1, 1, 3, kParts>(ctx, a, p.splits, p.share) : launch_tile<T, 2, 2, 1, 1, 3>(ctx, a);
-        case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 4>(ctx, a);
-        case kTile128Short: return launch_tile<T, 2, 4, 2, 1, 2>(ctx, a);
+        case kTile128Deep: return launch_tile<T, 2, 4, 2, 1, 3>(ctx, a);
         case kTile128: return launch_tile<T, 2, 2, 2, 2, 2>(ctx, a);
         case kTile256: return launch_tile<T, 2, 4, 4, 2, 2>(ctx, a);
     }

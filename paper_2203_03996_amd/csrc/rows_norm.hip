@@ -7,12 +7,13 @@
 // are reductions over registers and nothing is read twice.  Few vectors and many lanes: with four vectors to a lane (what y needs, what
 // the parameters hold) registers left one wave to a SIMD, 8192 rows of 8192 in 8 bits took 116 us in place of 48.
 // fp32 all through; y, z and q are rounded once each, z and q from the unrounded y.
+// y and z are stored past the L2 (non-temporal; see row_store): 5 to 20 % of the time.  x and h are not read so: 5 to 15 % more.
 //
 // Bound by HBM, 2 * c elements read and up to 2 * c written a row, and by the launch (3 us) below some 10 MB:
-//   16384 x 4096 bf16, both norms, gate, y and z     105-108 us   5.0 TB/s (a copy of 2 GB: 4.94)
-//   16384 x 1024 bf16                                31           4.3
-//   26214 of 262144 x 256 fp16 by a list             14           3.8    20000 x 500 fp16 21, x 512 20 (rows at odd addresses cost little)
-//   4099 x 1037 fp32                                 18           3.8    1 x 2048 fp16 4.6 us
+//   16384 x 4096 bf16, both norms, gate, y and z     104 us, inputs from memory (5.2 TB/s; a copy of 2 GB: 4.94); 90 on the same rows again
+//   16384 x 1024 bf16                                28           4.8
+//   26214 of 262144 x 256 fp16 by a list             12           4.4    20000 x 500 fp16 19, x 512 19 (rows at odd addresses cost little)
+//   4099 x 1037 fp32                                 17           4.0    1 x 2048 fp16 4.7 us
 //   8192 x 8192 fp16 to 8 bits                       48           4.2    26214 x 256 by a list 9.4
 #include "rows_device.h"
 
