@@ -311,7 +311,7 @@ typedef struct {
  * x NULL: 0; h NULL: y is x (and y_dev must be NULL); gate NULL: 1.  z is formed from y before y is rounded.
  * q / q_scale: z in 8 bits, q[r] = round_half_even(z[r] * (127 / max|z[r]|)) with q_scale[r] = max|z[r]| / 127.  A row
  * whose largest magnitude is below 1e-36 becomes zeros with scale 0, a row that holds a NaN or an infinity zeros with
- * scale NaN (products of it are NaN).  At least one of y, z, q is wanted; y_dev may equal x_dev (in place), outputs
+ * scale NaN (products of it are NaN).  At least one of y, z, q is wanted; y_dev may equal x_dev (in place, ldy = ldx), outputs
  * overlap nothing else.  c <= 32768. */
 typedef struct {
     dcnn_row_list list;
@@ -355,7 +355,8 @@ typedef struct {
     const void*   bias_dev;     /* [n] or NULL                                         */
     void*         y_dev;        /* [rows, n] compact                                   */
     int64_t       ldy;
-    const int8_t* q_dev;        /* matmul: [rows, k], aligned and spaced as in dcnn_rows_norm_args (the bytes behind k may hold anything) */
+    const int8_t* q_dev;        /* matmul: [rows, k], aligned and spaced as in dcnn_rows_norm_args (the bytes behind k may hold anything; up to a
+                                 * multiple of 16 they are read) */
     const float*  q_scale_dev;  /* matmul: [rows]                                      */
     int64_t       ldq;
     const void*   x_dev;        /* linear: map [map_rows, k]; k <= 32768                */

@@ -125,6 +125,8 @@ dcnn_status dcnn_rows_norm(dcnn_ctx* ctx, const dcnn_rows_norm_args* p) {
     if (st == DCNN_OK) st = check_ld(ctx, what, "gate", p->gate_dev, p->gate_rows ? p->ldg : p->c, p->c, es);
     if (st == DCNN_OK && (p->q_dev != nullptr || p->q_scale_dev != nullptr)) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->c);
     if (st != DCNN_OK) return st;
+    if (p->y_dev != nullptr && p->y_dev == p->x_dev && p->ldy != p->ldx && p->list.map_rows > 1)
+        return fail(ctx, DCNN_ESHAPE, "%s: in place with leading dimensions %lld and %lld", what, (long long)p->ldx, (long long)p->ldy);
 
     NormArgs a;
     a.x = p->x_dev, a.h = p->h_dev, a.gate = p->gate_dev;

@@ -659,6 +659,22 @@ def test_python_refusals(ctx):
         assert e.value.status == status, e.value
 
 
+def test_in_place_needs_one_spacing(ctx):
+    """Rows that lie elsewhere in y than in x would be written over before they are read."""
+    base = torch.ones(8, 32, device="cuda")
+    x, h = base[:4], torch.ones(4, 32, device="cuda")
+    with pytest.raises(pkg.DcnnError) as e:
+        ctx.rows_norm(x, h, y=base[::2])
+    assert e.value.status == 2, e.value
+    ctx.rows_norm(x[:1], h[:1], y=base[::2][:1])               # (one row lies where it lies)
+    ctx.rows_norm(base[::2], h, y=base[::2])
+    ctx.sync()
+    want = torch.ones(8, 32)
+    want[::2] += 1
+    want[0] += 1
+    assert torch.equal(base.cpu(), want)
+
+
 def test_c_refusals(ctx):
     """The C entry points check what the binding would not let through; nothing is launched."""
     import ctypes as C
