@@ -70,14 +70,11 @@ template <typename Op, int L> __device__ __forceinline__ typename Op::type row_r
     return u;
 }
 
-// Activation of a product's outputs.  A NaN (of a row that held one) stays one: no comparison with it holds.
-__device__ __forceinline__ void act_keep_nan(float (&v)[4], int act, float hi) {
-    if (act == DCNN_ACT_NONE) return;
+// ReLU up to hi of a product's outputs.  A NaN (of a row that held one) stays one: maximum and minimum hand it on.  (Two instructions; with
+// comparisons four and their waits, 26214 x 256 -> 1024 took 21.8 us in place of 19.2.)
+__device__ __forceinline__ void act_keep_nan(float (&v)[4], float hi) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[e] = v[e] < 0.0f ? 0.0f : v[e];
-        v[e] = v[e] > hi ? hi : v[e];
-    }
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v[e], 0.0f), hi);
 }
 
 // Four channels of a bias, zero where there is none.

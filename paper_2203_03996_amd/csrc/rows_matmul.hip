@@ -77,14 +77,15 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 //
 // The sums leave through LDS, a wave's 32 tokens by 128 bytes at a time: pieces of rows, 16 bytes a lane, where the matrix cores' order
 // would store 16 bytes from 32 rows; past the L2, which has the operands to keep (26214 x 256 -> 1024: 20.3 us -> 18.7, 8000 x 256 -> 256:
-// 8.4 -> 6.9; 4096 -> 4096 the same, or 4 % at 60000 rows).
+// 8.4 -> 6.9; 4096 -> 4096 the same, or 4 % at 60000 rows).  An output costs three and a half instructions and an activation two more: that,
+// and not the matrix cores, is what a short k waits for.
 //
 // 16384 x 4096 -> 4096 in bf16: 244-250 us, 2.2 POP/s; 8192 x 8192 -> 4096: 230, 2.4 (a library's 8-bit product that leaves its 32-bit sums:
 // 248 and 226).  Power bounds these: the same product of zeros takes 183 us in place of 230; the clock is at 1.8 GHz, and the matrix cores are
 // busy 60 % of its cycles.  Per tile of 256 x 256 about 5 us of 60 are the outputs'.  What it took, us for
 // the first of them: one K-tile staged through registers behind a barrier 328; loads two K-tiles and operands a step ahead 295; copies
 // straight into LDS 272; scales and bias by one load each, dealt out in LDS, and no wait for stores 250.  26214 x 256 -> 1024 in fp16 is bound
-// by its outputs: 18.7 us, 3.7 TB/s behind the launch.
+// by its outputs: 17.1 us, 3.9 TB/s behind the launch.
 constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
 constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
 constexpr int kPanelTiles = 2;                 // K-tiles of rows that a workgroup makes for itself and keeps
@@ -438,43 +439,59 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
         meet();
         int8_t* mine = out_lds + wave * S::unit;
         constexpr int E = RowVec<T>::E, PW = S::row / 16, UF = PW * E / 32;
+        // this lane's first 16 bytes on their way out: row r0, channel ch0
+        const int r0 = t0 + tw * FT * 32 + lane / PW, ch0 = c0 + cw * FC * 32 + lane % PW * E;
+        T* const y0 = static_cast<T*>(a.y) + (int64_t)r0 * a.ldy + ch0;
+        const bool cut = c0 + S::channels > a.n && a.n % E != 0;
+        constexpr int kAsk = 2;
+        auto leave = [&](auto acts) {                          // 0: no activation, 1: one, kAsk: see there
 #pragma unroll
-        for (int t = 0; t < FT; ++t)
+            for (int t = 0; t < FT; ++t)
 #pragma unroll
-            for (int u = 0; u < FC / UF; ++u) {
-                // PW places of 16 bytes to a token, exchanged by the token's low bits
+                for (int u = 0; u < FC / UF; ++u) {
+                    // PW places of 16 bytes to a token, exchanged by the token's low bits
 #pragma unroll
-                for (int fu = 0; fu < UF; ++fu)
+                    for (int fu = 0; fu < UF; ++fu)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int f = u * UF + fu, c = fu * 32 + g * 8 + lane / 32 * 4;
-                        float v[4];
+                        for (int g = 0; g < 4; ++g) {
+                            const int f = u * UF + fu, c = fu * 32 + g * 8 + lane / 32 * 4;
+                            float v[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = (float)acc[t][f][g * 4 + e] * (rs[t] * ws[f][g][e]) + bias[f][g][e];
-                        act_keep_nan(v, a.act, hi);
-                        AlignedQuad<T> out;
+                            for (int e = 0; e < 4; ++e) v[e] = (float)acc[t][f][g * 4 + e] * (rs[t] * ws[f][g][e]) + bias[f][g][e];
+                            if (decltype(acts)::value == kAsk ? a.act != DCNN_ACT_NONE : decltype(acts)::value != 0) act_keep_nan(v, hi);
+                            AlignedQuad<T> out;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) out[e] = (T)v[e];
-                        *reinterpret_cast<AlignedQuad<T>*>(mine + ((lane % 32) * PW + (c / E ^ lane % PW)) * 16 + c % E * sizeof(T)) = out;
+                            for (int e = 0; e < 4; ++e) out[e] = (T)v[e];
+                            *reinterpret_cast<AlignedQuad<T>*>(mine + ((lane % 32) * PW + (c / E ^ lane % PW)) * 16 + c % E * sizeof(T)) = out;
+                        }
+                    lds_wave_sync();
+                    const int8_t* from = mine + (lane / PW * PW + (lane % PW ^ lane / PW % PW)) * 16;      // (rows further on: the same low bits)
+                    static_assert(kWave / PW % PW == 0, "whole exchanges of places");
+                    T* y = y0 + (int64_t)(t * 32) * a.ldy + u * UF * 32;
+                    const auto piece = [&](int i) { return *reinterpret_cast<const AlignedVec<T>*>(from + i * kWave * 16); };
+                    const int ch = ch0 + u * UF * 32, left = count - r0 - t * 32;        // rows from this lane's first one on
+                    const int whole = ch + E <= a.n ? left : 0;
+#pragma unroll
+                    for (int i = 0; i < 32 * PW / kWave; ++i) {
+                        const AlignedVec<T> v = piece(i);
+                        if (i * (kWave / PW) < whole)
+                            __builtin_nontemporal_store((typename RowVec<T>::type)v, reinterpret_cast<typename RowVec<T>::type*>(y + (int64_t)(i * (kWave / PW)) * a.ldy));
                     }
-                lds_wave_sync();
-#pragma unroll
-                for (int i = 0; i < 32 * PW / kWave; ++i) {
-                    const int r = i * (kWave / PW) + lane / PW, p = lane % PW;
-                    const int row = t0 + (tw * FT + t) * 32 + r, ch = c0 + (cw * FC + u * UF) * 32 + p * E;
-                    const AlignedVec<T> v = *reinterpret_cast<const AlignedVec<T>*>(mine + (r * PW + (p ^ r % PW)) * 16);
-                    if (row >= count || ch >= a.n) continue;
-                    T* y = static_cast<T*>(a.y) + (int64_t)row * a.ldy + ch;
-                    if (ch + E <= a.n) {
-                        __builtin_nontemporal_store((typename RowVec<T>::type)v, reinterpret_cast<typename RowVec<T>::type*>(y));
-                    } else {
-                        const T* from = reinterpret_cast<const T*>(mine + (r * PW + (p ^ r % PW)) * 16);
+                    if (__builtin_expect(cut, 0) && ch < a.n && ch + E > a.n) {          // a lane's last 16 bytes are not all there
 #pragma clang loop unroll(disable)
-                        for (int e = 0; e < a.n - ch; ++e) y[e] = from[e];
+                        for (int i = 0; i < 32 * PW / kWave && i * (kWave / PW) < left; ++i, y += (int64_t)(kWave / PW) * a.ldy)
+#pragma clang loop unroll(disable)
+                            for (int e = 0; e < a.n - ch; ++e) y[e] = reinterpret_cast<const T*>(from + i * kWave * 16)[e];
                     }
+                    lds_wave_sync();
                 }
-                lds_wave_sync();
-            }
+        };
+        // (a copy for each, where tiles follow one another: 26214 x 256 -> 1024 17.5 us, asked at every four outputs 18.3.  The largest tile's
+        // wants more registers than there are, 8000 x 4096 -> 4096 144 us in place of 127; the smallest is a workgroup's only one: 4.2 / 3.8
+        // for 512 x 256 -> 1024, the code is read once)
+        if constexpr (FT * FC >= 8 || FT * FC == 1) leave(Int<kAsk>{});
+        else if (a.act == DCNN_ACT_NONE) leave(Int<0>{});
+        else leave(Int<1>{});
         operands(buf0, 0, 0);                                  // (read here and not at the tile's begin: nothing is left to be waited for)
     }
 }
@@ -644,7 +661,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs 
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * (rs * ws[e]) + bias[e];
-    act_keep_nan(v, a.act, act_hi(a.act));
+    if (a.act != DCNN_ACT_NONE) act_keep_nan(v, act_hi(a.act));
     T* y = static_cast<T*>(a.y) + (int64_t)out_row * a.ldy + out_ch;
     if (out_ch + 4 <= a.n) {
         typename RowQuad<T>::type quad;
