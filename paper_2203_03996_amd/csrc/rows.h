@@ -52,15 +52,15 @@ struct MatmulArgs {
     int32_t* partial;            // sums of workgroups that share a tile, and a count of those that are done for each tile:
     uint32_t* arrived;           //    zero before the launch and after it
 };
-// Which kernel: a function of the sizes alone, since the scratch depends on it.
+// Which kernel: a function of the sizes alone.
 enum MatmulKernel { kFewRows, kTile64, kTile128Deep, kTile128, kTile256 };
 struct MatmulPlan {
     MatmulKernel kernel;
     int splits;                  // workgroups that share a tile's k (kTile64), each `share` K-tiles of it
     int share;
-    size_t partial_bytes;
 };
 MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted);
+size_t partial_bytes(int64_t rows, int64_t k, int64_t n);
 constexpr size_t kArrivedBytes = 2048;         // counts of the workgroups of 512 tiles
 dcnn_status launch_rows_matmul(dcnn_ctx* ctx, int dtype, const MatmulPlan& plan, const MatmulArgs& a);
 // Norm, 8-bit rows and product in one kernel, for a token or a few: x, idx, map_rows, ldx, c and pre of NormArgs, all of MatmulArgs but q.

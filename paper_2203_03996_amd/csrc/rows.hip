@@ -48,16 +48,15 @@ void set_norm(const dcnn_row_norm& n, int* kind, float* eps, const void** w, con
     *w = n.kind == DCNN_NORM_NONE ? nullptr : n.w_dev;
     *b = n.kind == DCNN_NORM_NONE ? nullptr : n.b_dev;
 }
-// Scratch: the counts of workgroups that share a tile (at the same place whatever the sizes: they are zero between calls), their
+// Scratch, which grows with the rows: the counts of workgroups that share a tile (at the same place whatever the sizes: they are zero between calls), their
 // partial sums, then the 8-bit rows of a call that makes some: scales, rows
 struct Scratch {
     int64_t ldq;
     size_t partial, scales, rows, bytes;
     Scratch(int64_t count, int64_t k, int64_t n) {
-        const size_t a = matmul_plan(count, k, n, false).partial_bytes, b = matmul_plan(count, k, n, true).partial_bytes;
         ldq = (int64_t)align_up((size_t)k, 64);
         partial = align_up(kArrivedBytes);
-        scales = partial + align_up(a > b ? a : b);
+        scales = partial + align_up(partial_bytes(count, k, n));
         rows = scales + align_up((size_t)count * sizeof(float));
         bytes = rows + align_up((size_t)count * (size_t)ldq);
     }

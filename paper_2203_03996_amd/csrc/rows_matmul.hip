@@ -720,7 +720,7 @@ dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& n
 //   k of a tile of 64 in one / in parts  64, 8192 -> 1024: 22 / 10.9 (8)   64, 4096 -> 4096: 17 / 11.0 (4)   200, 8192 -> 1024: 22 / 12.5 (4), 14.4 (8)
 //                                        500, 8192 -> 1024: 24 / 18.2 (2), 16.4 (4)   64, 1024 -> 256: 5.1 / 6.7 (2)
 MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
-    MatmulPlan p{kFewRows, 1, 0, 0};
+    MatmulPlan p{kFewRows, 1, 0};
     const int64_t kt = packed_k(k) / kPackK;
     if (rows <= 16 || (rows <= 32 && kt < 64)) return p;
     // a list's length is on the GPU; its room is that of the whole map, and few maps are flagged all over
@@ -736,7 +736,6 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
         if (splits > 1) {
             p.share = (int)cdiv(kt, splits);
             p.splits = (int)cdiv(kt, p.share);
-            p.partial_bytes = (size_t)(tiles64 * p.splits) * 64 * 64 * sizeof(int32_t);
         }
     } else if (tiles128 <= kPlanCus) {
         p.kernel = kTile128Deep;
@@ -747,6 +746,15 @@ MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
         p.kernel = (kt >= 8 && full ? 17 : 21) * rounds256 <= 10 * rounds128 ? kTile256 : kTile128;
     }
     return p;
+}
+
+// Room for the partial sums of calls with up to so many rows, whichever plan they get: workgroups that share tiles are at most eight to a tile
+// and no more than the plan above allows in all.
+size_t partial_bytes(int64_t rows, int64_t k, int64_t n) {
+    const int64_t kt = packed_k(k) / kPackK, tiles_c = cdiv(n, 64), most = kt >= 64 ? 2 * kPlanCus : kPlanCus;
+    if (rows <= 16 || kt < 16 || 2 * tiles_c > most) return 0;
+    const int64_t parts = 8 * cdiv(rows, 64) * tiles_c;
+    return (size_t)(parts < most ? parts : most) * 64 * 64 * sizeof(int32_t);
 }
 
 template <typename T> static dcnn_status launch_matmul_t(dcnn_ctx* ctx, const MatmulPlan& p, const MatmulArgs& a) {

@@ -619,6 +619,24 @@ def test_results_do_not_change_from_run_to_run(ctx):
             assert torch.equal(first, weights.linear(x, pre=pkg.RowNorm("layer")))
 
 
+@pytest.mark.parametrize("order", [(3000, 100), (100, 3000, 200), (5, 20000, 64, 1, 400)])
+def test_sizes_in_any_order(ctx, order):
+    """Weights are called with many rows and then with few, whose k is shared out among workgroups (and their scratch is the larger one)."""
+    rng = np.random.default_rng(3)
+    k, n = 4096, 128
+    w, ws = q_weights(rng, k, n)
+    weights, other = pkg.RowWeights(ctx, w, scale=ws), pkg.RowWeights(ctx, w, scale=ws)
+    x = torch.randn(max(order), k, device="cuda", dtype=torch.float16)
+    q, q_scale = ctx.rows_quantize(x)
+    sums = (q[:64].cpu().double() @ w.cpu().double()).numpy()
+    want = sums * (np64(q_scale[:64])[:, None] * np64(ws))
+    for r in order:
+        for y in (weights.matmul(q[:r], q_scale[:r], dtype=torch.float32), other.linear(x[:r])):
+            tol = 2.0 ** -21 if y.dtype == torch.float32 else 2.0 ** -10      # (three roundings to 24 bits; one to 11 on top of them)
+            m = min(r, 64)
+            assert np.abs(np64(y[:m]) - want[:m]).max() <= tol * np.abs(want).max(), (r, y.dtype)
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------------------
 def test_no_rows(ctx):
     e = torch.empty(0, 48, device="cuda")

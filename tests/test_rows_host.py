@@ -21,6 +21,17 @@ def test_sizes_of_packed_weights_and_scratch():
     assert lib.dcnn_rows_scratch_bytes(-1, 64, 64, 0) == 0
 
 
+def test_scratch_grows_with_the_rows():
+    """Scratch of some rows is enough for every call with fewer of them."""
+    lib = pkg.load_library()
+    rows = sorted({int(2 ** (i / 8)) + d for i in range(8, 137) for d in (-1, 0, 1)})
+    for k, n in ((64, 64), (2048, 256), (4096, 512), (4096, 4096), (8192, 1024), (16384, 8192), (65536, 64), (8192, 16384), (8192, 16385)):
+        for linear in (0, 1):
+            sizes = [lib.dcnn_rows_scratch_bytes(r, k, n, linear) for r in rows]
+            assert sizes == sorted(sizes), (k, n, linear)
+        assert lib.dcnn_rows_scratch_bytes(rows[-1], k, n, 0) < 16 << 20
+
+
 def test_calls_without_a_context_are_refused():
     lib = pkg.load_library()
     assert lib.dcnn_rows_norm(None, C.byref(RowsNormArgs())) == 1
