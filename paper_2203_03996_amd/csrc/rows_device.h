@@ -70,6 +70,14 @@ template <typename Op, int L> __device__ __forceinline__ typename Op::type row_r
     return u;
 }
 
+// A product's output before its activation: the sum, the factor and the output are rounded to fp32, one after the other, whatever comes
+// behind.  (Left alone, the compiler folds the last of these into the rounding to fp16 where nothing stands between, and a row's outputs
+// would depend on the kernel that makes them, once in 20000.)
+__device__ __forceinline__ float scaled_sum(int32_t sum, float row_scale, float w_scale, float bias) {
+    float v = __builtin_fmaf((float)sum, row_scale * w_scale, bias);
+    asm("" : "+v"(v));
+    return v;
+}
 // ReLU up to hi of a product's outputs.  A NaN (of a row that held one) stays one: maximum and minimum hand it on.  (Two instructions; with
 // comparisons four and their waits, 26214 x 256 -> 1024 took 21.8 us in place of 19.2.)
 __device__ __forceinline__ void act_keep_nan(float (&v)[4], float hi) {

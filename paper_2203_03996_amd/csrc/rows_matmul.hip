@@ -457,7 +457,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
                             const int f = u * UF + fu, c = fu * 32 + g * 8 + lane / 32 * 4;
                             float v[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = (float)acc[t][f][g * 4 + e] * (rs[t] * ws[f][g][e]) + bias[f][g][e];
+                            for (int e = 0; e < 4; ++e) v[e] = scaled_sum(acc[t][f][g * 4 + e], rs[t], ws[f][g][e], bias[f][g][e]);
                             if (decltype(acts)::value == kAsk ? a.act != DCNN_ACT_NONE : decltype(acts)::value != 0) act_keep_nan(v, hi);
                             AlignedQuad<T> out;
 #pragma unroll
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void rows_few_kernel(MatmulArgs 
     if constexpr (NORM > 0) rs = scales[out_row < NORM ? out_row : 0];
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * (rs * ws[e]) + bias[e];
+    for (int e = 0; e < 4; ++e) v[e] = scaled_sum(s[e], rs, ws[e], bias[e]);
     if (a.act != DCNN_ACT_NONE) act_keep_nan(v, act_hi(a.act));
     T* y = static_cast<T*>(a.y) + (int64_t)out_row * a.ldy + out_ch;
     if (out_ch + 4 <= a.n) {

@@ -637,6 +637,21 @@ def test_sizes_in_any_order(ctx, order):
             assert np.abs(np64(y[:m]) - want[:m]).max() <= tol * np.abs(want).max(), (r, y.dtype)
 
 
+@pytest.mark.parametrize("act", ["none", "relu6"])
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_an_output_has_the_same_bits_whichever_kernel_makes_it(ctx, dt, act):
+    """The sums are exact: how many rows there are, and so which tile or split they get, shows in nothing."""
+    rng = np.random.default_rng(17)
+    k, n, rows = 2048, 512, 32000
+    q, qs = q_rows(rng, rows, k)
+    w, ws = q_weights(rng, k, n)
+    bias = rand(rng, n, dt)
+    weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias, act=act)
+    all_rows = weights.matmul(q, qs, dtype=TYPES[dt][0])
+    for r in (20000, 8000, 3000, 200, 24, 5):
+        assert torch.equal(weights.matmul(q[:r], qs[:r], dtype=TYPES[dt][0]), all_rows[:r]), r
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------------------
 def test_no_rows(ctx):
     e = torch.empty(0, 48, device="cuda")
