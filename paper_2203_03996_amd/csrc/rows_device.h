@@ -195,33 +195,44 @@ template <typename T, int L, int NV, bool HOLD> struct NormParams {
     __device__ __forceinline__ u32x4 bias(int j, int lane, int c) const { return HOLD ? unknown(bv[HOLD ? j : 0]) : row_load<T>(b, (j * L + lane) * RowVec<T>::E, c); }
 };
 
-// f(v[j][e], e) for the elements that count in the row's sums.
-template <typename T, int L, int NV, typename F> __device__ __forceinline__ void each_once(int lane, int c, F&& f) {
-    constexpr int E = RowVec<T>::E;
+// s = f(s, v[j][e]) over the elements that count in the row's sums, over the row's lanes.  Where a part of a wave has more than one vector to a
+// lane the vectors are added up as twice, four or eight times as many lanes would: a row's sums have the same bits either way.
+template <typename T, int L, int NV, typename F>
+__device__ __forceinline__ float row_sum(const float (&v)[NV][RowVec<T>::E], int lane, int c, uint32_t* red, int& turn, F&& f) {
+    constexpr int E = RowVec<T>::E, S = L < kWave ? NV : 1;
+    static_assert(S == 1 || ((S & (S - 1)) == 0 && S * L <= kWave), "pairs of vectors");
+    float s[S] = {};
     if (c % E == 0) {                                          // (what lies behind the row is zero)
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(j, e, true);
+            for (int e = 0; e < E; ++e) s[j % S] = f(s[j % S], v[j][e]);
     } else {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int skip = c < E ? 0 : row_part<T>((j * L + lane) * E, c).skip;
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(j, e, e >= skip);
+            for (int e = 0; e < E; ++e) s[j % S] = e >= skip ? f(s[j % S], v[j][e]) : s[j % S];
         }
     }
+#pragma unroll
+    for (int j = 0; j < S; ++j) s[j] = row_reduce<SumOp, L>(s[j], red, turn);
+#pragma unroll
+    for (int d = 1; d < S; d *= 2)
+#pragma unroll
+        for (int j = 0; j < S; j += 2 * d) s[j] += s[j + d];
+    return s[0];
 }
 
-// v <- norm(v); vectors behind the row's end are zero before and after.
+// v <- norm(v); vectors behind the row's end are zero before and after.  (What is fused into one rounding is written so: the kernels that norm
+// rows agree to the bit.)
 template <typename T, int L, int NV, bool HOLD>
 __device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const NormParams<T, L, NV, HOLD>& params, int lane, int c, float inv_c,
                                          uint32_t* red, int& turn) {
+#pragma clang fp contract(off)
     constexpr int E = RowVec<T>::E;
     if (kind == DCNN_NORM_LAYER) {
-        float s = 0.0f;
-        each_once<T, L, NV>(lane, c, [&](int j, int e, bool counts) { s += counts ? v[j][e] : 0.0f; });
-        const float mean = row_reduce<SumOp, L>(s, red, turn) * inv_c;
+        const float mean = row_sum<T, L, NV>(v, lane, c, red, turn, [](float s, float a) { return s + a; }) * inv_c;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int base = (j * L + lane) * E;
@@ -235,23 +246,28 @@ __device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind,
             }
         }
     }
-    float s = 0.0f;
-    each_once<T, L, NV>(lane, c, [&](int j, int e, bool counts) { s += counts ? v[j][e] * v[j][e] : 0.0f; });
-    const float r = 1.0f / sqrtf(row_reduce<SumOp, L>(s, red, turn) * inv_c + eps);
+    const float squares = row_sum<T, L, NV>(v, lane, c, red, turn, [](float s, float a) { return __builtin_fmaf(a, a, s); });
+    const float r = 1.0f / sqrtf(__builtin_fmaf(squares, inv_c, eps));
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        // (the four cases apart: a vector of factors held between them is registers that large rows have not left)
         if (params.w != nullptr) {
             const u32x4 w = params.weight(j, lane, c);
+            if (params.b != nullptr) {
+                const u32x4 b = params.bias(j, lane, c);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[j][e] *= r * row_get<T>(w, e);
+                for (int e = 0; e < E; ++e) v[j][e] = __builtin_fmaf(v[j][e], r * row_get<T>(w, e), row_get<T>(b, e));
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j][e] *= r * row_get<T>(w, e);
+            }
+        } else if (params.b != nullptr) {
+            const u32x4 b = params.bias(j, lane, c);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[j][e] = __builtin_fmaf(v[j][e], r, row_get<T>(b, e));
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[j][e] *= r;
-        }
-        if (params.b != nullptr) {
-            const u32x4 b = params.bias(j, lane, c);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[j][e] += row_get<T>(b, e);
         }
     }
 }

@@ -652,6 +652,33 @@ def test_an_output_has_the_same_bits_whichever_kernel_makes_it(ctx, dt, act):
         assert torch.equal(weights.matmul(q[:r], qs[:r], dtype=TYPES[dt][0]), all_rows[:r]), r
 
 
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("k", [5, 64, 77, 128, 200, 256])
+def test_short_rows_have_the_same_bits_among_few_and_many(ctx, k, dt, kind):
+    """Rows that a product's kernel norms for itself against rows that the norm's kernel handed over."""
+    rng = np.random.default_rng(k)
+    x = rand(rng, (20000, k), dt, 1.5, 0.5)
+    weights = pkg.RowWeights(ctx, rand(rng, (k, 1024), "f32"))
+    for norm in (pkg.RowNorm(kind), pkg.RowNorm(kind, rand(rng, k, dt), rand(rng, k, dt)), pkg.RowNorm(kind, rand(rng, k, dt))):
+        all_rows = weights.linear(x, pre=norm)
+        for r in (3000, 500, 40):
+            assert torch.equal(weights.linear(x[:r], pre=norm), all_rows[:r]), r
+
+
+@pytest.mark.parametrize("rows,n", [(8192, 1024), (2000, 300)])
+def test_listed_rows_have_the_bits_of_the_whole_map(ctx, rows, n):
+    """A list has room for the whole map: its length, which is on the GPU, may weigh in which kernel is taken and in nothing else."""
+    rng = np.random.default_rng(rows)
+    x = rand(rng, (rows, 256), "f16", 1.5, 0.5)
+    weights, norm = pkg.RowWeights(ctx, rand(rng, (256, n), "f16")), pkg.RowNorm("layer", rand(rng, 256, "f16"), rand(rng, 256, "f16"))
+    whole = weights.linear(x, pre=norm)
+    idx = torch.arange(rows, dtype=torch.int32, device="cuda").roll(-7)
+    for m in (0, 1, 100, rows):
+        some = weights.linear(x, pre=norm, idx=idx, count=torch.tensor([m], dtype=torch.int32, device="cuda"))
+        assert torch.equal(some[:m], whole[idx[:m].long()]), m
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------------------
 def test_no_rows(ctx):
     e = torch.empty(0, 48, device="cuda")
