@@ -431,6 +431,10 @@ class Layer:
             pass
 
 
+_ROWS_MAX = 0x7fffffff                     # of a map or a compact matrix
+_SCRATCH_ROWS = 64                         # linear products of more rows take scratch of their own
+
+
 def _row_dtype(dt) -> int:
     code = ROW_DTYPE_CODE.get(dt)
     if code is None:
@@ -525,7 +529,12 @@ class RowWeights:
         if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
             raise ValueError(f"bias must be a contiguous device tensor [{n}]")
         self.act, self._bias = ACT_CODES[act], _ptr(bias) or None
-        self._scratch, self._scratch_bytes, self._scratch_rows = None, 0, [-1, -1]
+        # scratch for all products of 8-bit rows (partial sums: 8 MB at most) and the linear ones of few rows
+        nbytes = max(lib.dcnn_rows_scratch_bytes(_ROWS_MAX, k, n, 0), lib.dcnn_rows_scratch_bytes(_SCRATCH_ROWS, k, n, 1))
+        with torch.cuda.stream(ctx.stream):
+            self._scratch = torch.zeros(nbytes, dtype=torch.uint8, device=ctx.device)
+        self._scratch_at = self._scratch.data_ptr(), nbytes
+        self._grown, self._grown_rows, self._captured = None, 0, set()         # _captured: what graphs hold the address of
 
     def _call(self, call, linear, a, rows, dt, count, out):
         ctx = self.ctx
@@ -541,22 +550,25 @@ class RowWeights:
             a.y, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.index)
             rows = min(rows, n)
         a.rows = rows
-        if rows > self._scratch_rows[linear]:
-            self._grow(rows, linear)
-        a.scratch, a.scratch_bytes = self._scratch.data_ptr(), self._scratch_bytes
+        a.scratch, a.scratch_bytes = self._scratch_at if not linear or rows <= _SCRATCH_ROWS else self._linear_scratch(rows)
         st = call(ctx.handle, a)
         if st:
             ctx.check(st)
         return out
 
-    def _grow(self, rows, linear):
-        """Scratch for calls of one kind with up to this many rows."""
-        need = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n, linear)
-        self._scratch_rows[linear] = rows
-        if need > self._scratch_bytes:
+    def _linear_scratch(self, rows):
+        """(address, bytes) of scratch that holds so many 8-bit rows; a larger one takes the place of a smaller one."""
+        capturing = torch.cuda.is_current_stream_capturing()
+        scratch = self._grown
+        if scratch is None or rows > self._grown_rows:
+            need = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n, 1)
             with torch.cuda.stream(self.ctx.stream):
-                self._scratch = torch.zeros(need, dtype=torch.uint8, device=self.ctx.device)
-            self._scratch_bytes = need
+                scratch = torch.zeros(need, dtype=torch.uint8, device=self.ctx.device)
+            if not capturing:                                     # (else it is the graph's: the kernel that clears it runs when the graph does)
+                self._grown, self._grown_rows = scratch, rows
+        elif capturing:
+            self._captured.add(scratch)
+        return scratch.data_ptr(), scratch.numel()
 
     def matmul(self, q, q_scale, *, dtype=torch.float16, count=None, out=None):
         """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`."""

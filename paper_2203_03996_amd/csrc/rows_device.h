@@ -224,8 +224,8 @@ __device__ __forceinline__ float row_sum(const float (&v)[NV][RowVec<T>::E], int
     return s[0];
 }
 
-// v <- norm(v); vectors behind the row's end are zero before and after.  (What is fused into one rounding is written so: the kernels that norm
-// rows agree to the bit.)
+// v <- norm(v); vectors behind the row's end are zero before and after.  (What is fused into one rounding is written so: rows that
+// fit a wave have the same bits in every kernel that norms them.)
 template <typename T, int L, int NV, bool HOLD>
 __device__ __forceinline__ void norm_row(float (&v)[NV][RowVec<T>::E], int kind, float eps, const NormParams<T, L, NV, HOLD>& params, int lane, int c, float inv_c,
                                          uint32_t* red, int& turn) {

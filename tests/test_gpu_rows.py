@@ -608,6 +608,37 @@ def test_graph_replays_and_side_stream(rows):
             assert torch.equal(got[name], eager[name]), (step, name)
 
 
+@pytest.mark.parametrize("before", [None, 160])
+def test_graphs_keep_their_scratch(before):
+    """Captured without a call before it, or behind a small one; then larger calls without the graph, whose scratch takes the place of the first."""
+    rng = np.random.default_rng(23)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = pkg.Context(0)
+    k, n, rows = 4096, 128, 160                                     # (few tiles and a long k: partial sums and counts in the scratch)
+    w, ws = q_weights(rng, k, n)
+    x = rand(rng, (5000, k), "f16")
+    torch.cuda.synchronize()
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    want = pkg.RowWeights(ctx, w, scale=ws).linear(x)
+    if before is not None:
+        weights.linear(x[:before])
+    out = torch.zeros(rows, n, dtype=torch.float16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        weights.linear(x[:rows], out=out)
+    for eager in (rows, 200, 5000, 100):
+        got = weights.linear(x[:eager])
+        with torch.cuda.stream(stream):
+            other = torch.full((1 << 22,), 77, dtype=torch.uint8, device="cuda")         # (in the place of scratch that was let go, if any was)
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want[:eager]) and torch.equal(out, want[:rows]) and bool((other == 77).all()), eager
+        out.zero_()
+        torch.cuda.synchronize()
+
+
 def test_results_do_not_change_from_run_to_run(ctx):
     rng = np.random.default_rng(5)
     for rows, k, n in ((1, 8192, 512), (20, 4096, 256), (300, 1000, 500)):
