@@ -353,7 +353,7 @@ typedef struct {
     int64_t       k, n;
     const void*   packed_dev;   /* of dcnn_rows_pack with the same k and n              */
     const void*   bias_dev;     /* [n] or NULL                                         */
-    void*         y_dev;        /* [rows, n] compact                                   */
+    void*         y_dev;        /* [rows, n] compact; overlaps no input                */
     int64_t       ldy;
     const int8_t* q_dev;        /* matmul: [rows, k], aligned and spaced as in dcnn_rows_norm_args (the bytes behind k may hold anything; up to a
                                  * multiple of 16 they are read) */

@@ -124,6 +124,9 @@ dcnn_status dcnn_rows_norm(dcnn_ctx* ctx, const dcnn_rows_norm_args* p) {
     if (st == DCNN_OK) st = check_ld(ctx, what, "gate", p->gate_dev, p->gate_rows ? p->ldg : p->c, p->c, es);
     if (st == DCNN_OK && (p->q_dev != nullptr || p->q_scale_dev != nullptr)) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->c);
     if (st != DCNN_OK) return st;
+    const auto same = [](const void* a, const void* b) { return a != nullptr && a == b; };
+    if (same(p->y_dev, p->h_dev) || same(p->z_dev, p->h_dev) || same(p->z_dev, p->x_dev) || same(p->z_dev, p->y_dev))
+        return fail(ctx, DCNN_EINVAL, "%s: an output in the place of an input or another output (y may be x)", what);
     if (p->y_dev != nullptr && p->y_dev == p->x_dev && p->ldy != p->ldx && p->list.map_rows > 1)
         return fail(ctx, DCNN_ESHAPE, "%s: in place with leading dimensions %lld and %lld", what, (long long)p->ldx, (long long)p->ldy);
 
@@ -176,6 +179,7 @@ dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     dcnn_status st = check_matmul(ctx, what, p, 0, &m);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->k);
+    if (st == DCNN_OK && p->q_dev == p->y_dev) st = fail(ctx, DCNN_EINVAL, "%s: y in the place of q, which other workgroups read", what);
     if (st != DCNN_OK) return st;
     m.q = p->q_dev, m.q_scale = p->q_scale_dev, m.ldq = (int)p->ldq;
     return launch_rows_matmul(ctx, p->dtype, matmul_plan(p->list.rows, p->k, p->n, p->list.count_dev != nullptr), m);
@@ -191,6 +195,7 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     if (st == DCNN_OK) st = check_map(ctx, what, p->list);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK && p->x_dev == nullptr) st = fail(ctx, DCNN_EINVAL, "%s: x is null", what);
+    if (st == DCNN_OK && p->x_dev == p->y_dev) st = fail(ctx, DCNN_EINVAL, "%s: y in the place of x, which other workgroups read", what);
     if (st == DCNN_OK) st = check_ld(ctx, what, "x", p->x_dev, p->ldx, p->k, rows_dtype_size(p->dtype));
     if (st == DCNN_OK) st = check_norm(ctx, what, p->pre, rows_dtype_size(p->dtype));
     if (st != DCNN_OK) return st;

@@ -766,6 +766,19 @@ def test_in_place_needs_one_spacing(ctx):
     assert torch.equal(base.cpu(), want)
 
 
+def test_outputs_in_the_place_of_inputs_are_refused(ctx):
+    x, h, y, z = (torch.zeros(8, 32, device="cuda") for _ in range(4))
+    weights = pkg.RowWeights(ctx, torch.ones(32, 32, device="cuda"))
+    for bad in (lambda: ctx.rows_norm(x, h, y=h), lambda: ctx.rows_norm(x, h, z=h), lambda: ctx.rows_norm(x, h, z=x), lambda: ctx.rows_norm(x, h, y=y, z=y),
+                lambda: ctx.rows_norm(x, z=x), lambda: ctx.rows_norm(None, h, y=h), lambda: weights.linear(x, out=x)):
+        with pytest.raises(pkg.DcnnError) as e:
+            bad()
+        assert e.value.status == 1, e.value
+    ctx.rows_norm(x, x, y=y, z=z)                              # (inputs may be one)
+    ctx.rows_norm(x, h, y=x, z=z)
+    ctx.sync()
+
+
 def test_c_refusals(ctx):
     """The C entry points check what the binding would not let through; nothing is launched."""
     import ctypes as C
