@@ -4,6 +4,7 @@
 //
 // The sums are exact in 32-bit integers, so how a sum is cut up never changes a result.
 #include "rows_device.h"
+#include "tile_schedule.h"
 
 namespace dcnn {
 
@@ -351,19 +352,19 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             __builtin_amdgcn_sched_barrier(0);
         }
         if (kt + 1 >= arrived) {                               // K-tile kt + 1: those behind it may be on their way
-            const int behind = ahead < range.end ? NB - 2 : kts - 2 - kt;
-            if (behind >= NB - 2) wait_loads<(NB - 2) * (QL + WL)>();
-            else wait_but(behind > 0 ? behind : 0);
+            const int behind = may_be_in_flight(kt, kts, NB, ahead < range.end);
+            if (behind == NB - 2) wait_loads<(NB - 2) * (QL + WL)>();
+            else wait_but(behind);
         }
         meet();
         operands(next, kt + 1 < kts ? kt + 1 : kt, 0);         // (behind a tile's last K-tile: anything, nobody uses it)
         int from = kt + NB;
         if (from >= kts) {                                     // the next tile's K-tile of this buffer
-            if (from == kts || (kts < NB && kt == 0)) {
+            if (turns_to_next(kt, kts, NB)) {
                 ahead += range.step;
                 if (ahead < range.end) aim(ahead);
             }
-            from = kt % NB;
+            from = copied_behind(kt, kts, NB);
         }
         if (ahead < range.end) copy(buf, from);
         __builtin_amdgcn_sched_barrier(0);
