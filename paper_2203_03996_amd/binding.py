@@ -485,21 +485,21 @@ def _int32(t, name, dev):
 
 
 class RowNorm:
-    """A norm over a row's channels: kind "rms" or "layer", weight and bias [c] (None: ones, zeros), which it keeps."""
+    """A norm over a row's channels: kind "rms" or "layer", weight and bias [c] (None: ones, zeros), which it keeps.
+
+    Each call reads the parameters where they lie then: a module's may move or change their type between calls."""
 
     def __init__(self, kind: str, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5):
         self.kind, self.weight, self.bias, self.eps = NORM_CODES[kind], weight, bias, float(eps)
-        self._fits = {(t.numel(), t.dtype, t.get_device()) for t in (weight, bias) if t is not None}
         for t in (weight, bias):
             if t is not None and (t.dim() != 1 or not t.is_contiguous()):
                 raise ValueError(f"a norm's parameters must be contiguous vectors, got {tuple(t.shape)} strides {t.stride()}")
-        self._pointers = (self.kind, self.eps, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr())
 
     def pointers(self, c: int, dt, dev):
         """(kind, eps, address of the weight, address of the bias) for rows of c channels."""
-        if not self._fits <= {(c, dt, dev)}:
-            raise ValueError(f"a norm's parameters must be [{c}] {dt} on GPU {dev}, got {self._fits}")
-        return self._pointers
+        w, b = self.weight, self.bias
+        return (self.kind, self.eps, None if w is None else _vector(w, "a norm's weight", c, dt, dev),
+                None if b is None else _vector(b, "a norm's bias", c, dt, dev))
 
 
 class RowWeights:
@@ -528,7 +528,7 @@ class RowWeights:
                 t.record_stream(ctx.stream)
         if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
             raise ValueError(f"bias must be a contiguous device tensor [{n}]")
-        self.act, self._bias = ACT_CODES[act], _ptr(bias) or None
+        self.act = ACT_CODES[act]
         # scratch for all products of 8-bit rows (partial sums: 8 MB at most) and the linear ones of few rows
         nbytes = max(lib.dcnn_rows_scratch_bytes(_ROWS_MAX, k, n, 0), lib.dcnn_rows_scratch_bytes(_SCRATCH_ROWS, k, n, 1))
         with torch.cuda.stream(ctx.stream):
@@ -538,9 +538,9 @@ class RowWeights:
 
     def _call(self, call, linear, a, rows, dt, count, out):
         ctx = self.ctx
-        if self.bias is not None and self.bias.dtype != dt:
-            raise ValueError(f"the bias is {self.bias.dtype}, the output {dt}")
-        a.dtype, a.k, a.n, a.act, a.packed, a.bias = _row_dtype(dt), self.k, self.n, self.act, self.packed.data_ptr(), self._bias
+        a.dtype, a.k, a.n, a.act, a.packed = _row_dtype(dt), self.k, self.n, self.act, self.packed.data_ptr()
+        if self.bias is not None:                                 # (where it lies now, as the outputs' type is this call's)
+            a.bias = _vector(self.bias, "bias", self.n, dt, ctx.index)
         if count is not None:
             a.count = _int32(count, "count", ctx.index)
         if out is None:

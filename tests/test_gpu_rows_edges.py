@@ -36,3 +36,41 @@ def product_at_some_rows(ctx, dt, rows, k, n):  # noqa: F811
     at = torch.from_numpy(np.unique(np.concatenate([np.arange(min(rows, 70)), rng.integers(0, rows, 130), np.arange(max(0, rows - 70), rows)]))).cuda()
     s = (q[at].double() @ w.double()) * qs[at].double()[:, None] * ws.double()          # (whole numbers below 2^53 before the scales)
     close(y[at], np64(s + bias.double()), dt, np64(4 * U32 * (s.abs() + bias.double().abs())), f"{dt} {rows}x{k}x{n}")
+
+
+# ---- parameters that move ---------------------------------------------------------------------------------------------
+def test_parameters_are_read_where_they_lie_at_each_call(ctx):  # noqa: F811
+    """Norms, biases and gates of a module whose storage is swapped between calls."""
+    c, n, rows = 64, 96, 40
+    rng = np.random.default_rng(1)
+    layer = torch.nn.LayerNorm(c).cuda()
+    bias = torch.nn.Parameter(torch.zeros(n, device="cuda"), requires_grad=False)
+    gate = torch.nn.Parameter(torch.ones(c, device="cuda"), requires_grad=False)
+    norm = pkg.RowNorm("layer", layer.weight, layer.bias)
+    w, ws = q_weights(rng, c, n)
+    weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias)
+    up, down = rand(rng, (c, n), "f32"), rand(rng, (n, c), "f32")
+    block = pkg.RowBlock(ctx, up, down, up_bias=bias, pre=norm, gate=gate)
+    for dt in ("f32", "f16", "f32", "bf16"):
+        for t in (*layer.parameters(), bias, gate):
+            t.data = rand(rng, t.shape, dt, 0.3, 0.5)              # (what lay there before is freed)
+        x = rand(rng, (rows, c), dt)
+        fresh = pkg.RowNorm("layer", layer.weight.data.clone(), layer.bias.data.clone())
+        fresh_weights = pkg.RowWeights(ctx, w, scale=ws, bias=bias.data.clone())
+        fresh_block = pkg.RowBlock(ctx, up, down, up_bias=bias.data.clone(), pre=fresh, gate=gate.data.clone())
+        got, want = weights.linear(x, pre=norm), fresh_weights.linear(x, pre=fresh)
+        z, zw = ctx.rows_norm(x, pre=norm, z=True)[1], ctx.rows_norm(x, pre=fresh, z=True)[1]
+        y, yw = block.step(x, torch.empty_like(x)), fresh_block.step(x, torch.empty_like(x))
+        ctx.sync()
+        assert torch.equal(got, want) and torch.equal(z, zw) and torch.equal(y, yw), dt
+        for other in set(TYPES) - {dt}:
+            xo = x.to(TYPES[other][0])
+            for bad in (lambda: weights.linear(xo), lambda: ctx.rows_norm(xo, pre=norm, z=True), lambda: weights.linear(xo, pre=fresh)):
+                with pytest.raises(ValueError):
+                    bad()
+    bias.data = torch.zeros(n + 1, device="cuda")
+    with pytest.raises(ValueError):
+        weights.linear(rand(rng, (rows, c), "f32"))
+    bias.data = torch.zeros(n)                                     # not on the GPU
+    with pytest.raises(ValueError):
+        weights.linear(rand(rng, (rows, c), "f32"))

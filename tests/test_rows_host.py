@@ -86,3 +86,35 @@ def test_argument_blocks_have_the_layout_of_the_header(tmp_path):
     subprocess.run(["gcc", str(src), "-o", str(tmp_path / "layout")], check=True)
     got = subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True, check=True).stdout.split()
     assert [int(v) for v in got] == want
+
+
+@pytest.mark.parametrize("move", ["half", "half and back", "data", "to"])
+def test_a_norm_reads_its_parameters_where_they_lie_at_each_call(move):
+    """A module's parameters keep their tensors and change what these stand on; the address of a call is the one of that moment."""
+    import torch
+    layer = torch.nn.LayerNorm(64)
+    norm = pkg.RowNorm("layer", layer.weight, layer.bias)
+    assert norm.pointers(64, torch.float32, -1) == (2, norm.eps, layer.weight.data_ptr(), layer.bias.data_ptr())
+    dtype = torch.float32
+    held = layer.weight.data, layer.bias.data                     # (so that the new storage is not the old one's by chance)
+    if move == "half":
+        layer.half()
+        dtype = torch.float16
+    elif move == "half and back":
+        layer.half().float()
+    elif move == "to":
+        layer.to(torch.bfloat16)
+        dtype = torch.bfloat16
+    else:
+        layer.weight.data, layer.bias.data = torch.ones(64), torch.zeros(64)
+    assert norm.pointers(64, dtype, -1)[2:] == (layer.weight.data_ptr(), layer.bias.data_ptr())
+    assert layer.weight.data_ptr() != held[0].data_ptr()
+    for wrong in (t for t in (torch.float32, torch.float16, torch.bfloat16) if t != dtype):
+        with pytest.raises(ValueError):
+            norm.pointers(64, wrong, -1)
+    layer.bias.data = torch.zeros(65, dtype=dtype)
+    with pytest.raises(ValueError):
+        norm.pointers(64, dtype, -1)
+    layer.bias.data = torch.zeros(128, dtype=dtype)[::2]
+    with pytest.raises(ValueError):
+        norm.pointers(64, dtype, -1)
