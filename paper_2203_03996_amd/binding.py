@@ -260,6 +260,13 @@ class Context:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def capturing(self) -> bool:
+        """Whether a graph is being captured on the context's stream, whichever stream torch is on."""
+        if torch._C._cuda_getCurrentRawStream(self.index) == self._raw_stream:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(self.stream):
+            return torch.cuda.is_current_stream_capturing()
+
     def rows_norm(self, x=None, h=None, *, post=None, gate=None, gate_rows=0, scale=1.0, pre=None, idx=None, count=None,
                   y=None, z=None, q=None, q_scale=None):
         """dcnn_rows_norm: y = x + scale * gate * post(h) and z = pre(y), z also in 8 bits (q with q_scale).
@@ -558,7 +565,7 @@ class RowWeights:
 
     def _linear_scratch(self, rows):
         """(address, bytes) of scratch that holds so many 8-bit rows; a larger one takes the place of a smaller one."""
-        capturing = torch.cuda.is_current_stream_capturing()
+        capturing = self.ctx.capturing()
         scratch = self._grown
         if scratch is None or rows > self._grown_rows:
             need = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n, 1)

@@ -74,3 +74,40 @@ def test_parameters_are_read_where_they_lie_at_each_call(ctx):  # noqa: F811
     bias.data = torch.zeros(n)                                     # not on the GPU
     with pytest.raises(ValueError):
         weights.linear(rand(rng, (rows, c), "f32"))
+
+
+# ---- scratch ----------------------------------------------------------------------------------------------------------
+def test_scratch_made_in_a_capture_while_torch_is_on_another_stream():
+    """The context's stream is captured, torch is on a stream that has forked from it: scratch that the graph clears is the graph's alone."""
+    rng = np.random.default_rng(29)
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = pkg.Context(0)  # noqa: F811
+    k, n, rows = 4096, 128, 160                                     # (workgroups that share a tile count themselves in the scratch)
+    w, ws = q_weights(rng, k, n)
+    x = rand(rng, (400, k), "f16")
+    torch.cuda.synchronize()
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    want = pkg.RowWeights(ctx, w, scale=ws).linear(x)
+    out = torch.zeros(rows, n, dtype=torch.float16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        assert ctx.capturing()
+        other.wait_stream(stream)
+        with torch.cuda.stream(other):
+            assert ctx.capturing()
+            weights.linear(x[:rows], out=out)
+        stream.wait_stream(other)
+    assert weights._grown is None and not ctx.capturing()          # (nothing has cleared what the capture made)
+    for eager in (rows, 400, 100):
+        with torch.cuda.stream(other):
+            got = weights.linear(x[:eager])
+        ctx.sync()
+        assert torch.equal(got, want[:eager]), eager
+        with torch.cuda.stream(stream):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[:rows]), eager
+        out.zero_()
+        torch.cuda.synchronize()

@@ -118,3 +118,34 @@ def test_a_norm_reads_its_parameters_where_they_lie_at_each_call(move):
     layer.bias.data = torch.zeros(128, dtype=dtype)[::2]
     with pytest.raises(ValueError):
         norm.pointers(64, dtype, -1)
+
+
+def test_scratch_that_a_graph_clears_is_not_kept(monkeypatch):
+    """What is captured on the context's stream decides, not the stream that torch is on (streams and captures are stood in for)."""
+    import contextlib
+
+    import torch
+    current, captured = ["torch's"], set()
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, current[0] = current[0], stream
+        yield
+        current[0] = before
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: current[0] in captured)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: current[0], raising=False)
+    ctx = pkg.Context.__new__(pkg.Context)
+    ctx.lib, ctx.index, ctx.stream, ctx._raw_stream, ctx.device = pkg.load_library(), 0, "the context's", "the context's", torch.device("cpu")
+    weights = pkg.RowWeights.__new__(pkg.RowWeights)
+    weights.__dict__.update(ctx=ctx, k=64, n=64, _grown=None, _grown_rows=0, _captured=set())
+    captured.add("the context's")
+    weights._linear_scratch(100)                                   # torch is on another stream, which no graph captures
+    assert weights._grown is None
+    captured.clear()
+    captured.add("torch's")
+    weights._linear_scratch(100)                                   # the other way round: the scratch is cleared now
+    assert weights._grown is not None and not weights._captured
+    captured.add("the context's")
+    at, _ = weights._linear_scratch(100)                           # a graph that uses it holds it
+    assert at == weights._grown.data_ptr() and len(weights._captured) == 1
