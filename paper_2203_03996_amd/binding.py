@@ -273,6 +273,9 @@ class Context:
 
         x and y are maps (last dimension c), the rest is [rows, c].  y, z, q: a tensor to write, True for a new one, or
         None where it is not wanted (q_scale: a tensor [rows], or None for a new one).  post, pre: RowNorm or None.
+        Rows that a list does not name are left as they are (in a new y: uninitialised).  Without a count all rows of x,
+        or all that idx names, are wanted: a matrix with fewer is refused.  With a count the smallest of idx, h, z and q
+        is the room of the call, and what the count names beyond it is left as it is too.
         Returns (y, z, q, q_scale)."""
         t = h if x is None else x
         if t is None:
@@ -291,10 +294,7 @@ class Context:
                 rows = map_rows
         if h is not None:
             a.h, a.ldh, n = _as_rows(h, "h", c, dt, dev)
-            if rows is None or (n < rows and idx is not None):
-                rows = n
-            elif n < rows:
-                raise ValueError(f"rows_norm: h has {n} rows, {rows} are wanted")
+            rows = n if rows is None else _room(rows, n, "h", count)
         if y is not None:
             if y is True:
                 y = self.empty((rows, c) if x is None else x.shape, dt)
@@ -315,14 +315,14 @@ class Context:
                 a.z, a.ldz = z.data_ptr(), c
             else:
                 a.z, a.ldz, n = _as_rows(z, "z", c, dt, dev)
-                rows = min(rows, n)
+                rows = _room(rows, n, "z", count)
         if q is not None:
             if q is True:
                 q = self.empty((rows, -(-c // 16) * 16), torch.int8)[:, :c]
             if q_scale is None:
                 q_scale = self.empty(rows, torch.float32)
             a.q, a.q_scale, a.ldq = _check_q(q, q_scale, c, dev)
-            rows = min(rows, q.shape[0])
+            rows = _room(rows, q.shape[0], "q", count)
         if post is not None:
             a.post_kind, a.post_eps, a.post_w, a.post_b = post.pointers(c, dt, dev)
         if pre is not None:
@@ -466,6 +466,15 @@ def _as_rows(t, name, c, dt, dev):
     return t.data_ptr(), ld, n
 
 
+def _room(rows, n, name, count):
+    """Rows of a call with a compact matrix of n rows: it may have fewer than the call where their number is on the GPU, and nowhere else."""
+    if n >= rows:
+        return rows
+    if count is None:
+        raise ValueError(f"{name} has {n} rows, {rows} are wanted")
+    return n
+
+
 def _vector(t, name, c, dt, dev):
     if t.numel() != c or t.dtype is not dt or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{c}] {dt} on GPU {dev}, got {tuple(t.shape)} {t.dtype}")
@@ -555,7 +564,7 @@ class RowWeights:
             a.y, a.ldy = out.data_ptr(), self.n
         else:
             a.y, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.index)
-            rows = min(rows, n)
+            rows = _room(rows, n, "out", count)
         a.rows = rows
         a.scratch, a.scratch_bytes = self._scratch_at if not linear or rows <= _SCRATCH_ROWS else self._linear_scratch(rows)
         st = call(ctx.handle, a)
@@ -578,13 +587,15 @@ class RowWeights:
         return scratch.data_ptr(), scratch.numel()
 
     def matmul(self, q, q_scale, *, dtype=torch.float16, count=None, out=None):
-        """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`."""
+        """dcnn_rows_matmul: the product of 8-bit rows [rows, k] with a scale each, [rows, n] of `dtype`.
+
+        out: a matrix to write, of `rows` rows at least; with a count it may have fewer (what the count names beyond them is not computed)."""
         a = RowsMatmulArgs()
         a.q, a.q_scale, a.ldq = _check_q(q, q_scale, self.k, self.ctx.index)
         return self._call(self.ctx.lib.dcnn_rows_matmul, 0, a, q.shape[0], dtype, count, out)
 
     def linear(self, x, *, pre=None, idx=None, count=None, out=None):
-        """dcnn_rows_linear: rows of the map x (those that idx names), normed with `pre`, quantised and multiplied; [rows, n]."""
+        """dcnn_rows_linear: rows of the map x (those that idx names), normed with `pre`, quantised and multiplied; [rows, n].  out: as in matmul."""
         a, dt, dev = RowsMatmulArgs(), x.dtype, self.ctx.index
         a.x, a.ldx, rows = _as_rows(x, "x", self.k, dt, dev)
         a.map_rows = rows

@@ -111,3 +111,48 @@ def test_scratch_made_in_a_capture_while_torch_is_on_another_stream():
         assert torch.equal(out, want[:rows]), eager
         out.zero_()
         torch.cuda.synchronize()
+
+
+# ---- matrices that are too short --------------------------------------------------------------------------------------
+def test_matrices_with_too_few_rows_are_refused(ctx):  # noqa: F811
+    """Every row of a call without a count is wanted: none is left out because another matrix has no room for it."""
+    rng = np.random.default_rng(3)
+    x, h, y = rand(rng, (8, 32), "f32"), rand(rng, (8, 32), "f32"), torch.full((8, 32), 7.0, device="cuda")
+    short = torch.full((4, 32), 7.0, device="cuda")
+    q, qs = torch.zeros(4, 32, dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
+    w, ws = q_weights(rng, 32, 32)
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    rows, scales = ctx.rows_quantize(x)
+    idx = torch.arange(8, dtype=torch.int32, device="cuda")
+    for listed in (None, idx):
+        for bad in (lambda: ctx.rows_norm(x, h, y=y, z=short, idx=listed), lambda: ctx.rows_norm(x, h, y=y, q=q, q_scale=qs, idx=listed),
+                    lambda: ctx.rows_norm(x, h[:4], y=y, idx=listed), lambda: ctx.rows_norm(x, z=short, idx=listed), lambda: weights.linear(x, out=short, idx=listed),
+                    lambda: weights.matmul(rows, scales, dtype=torch.float32, out=short)):
+            with pytest.raises(ValueError, match="rows"):
+                bad()
+    ctx.sync()
+    assert (np64(y) == 7.0).all() and (np64(short) == 7.0).all(), "a refused call wrote something"
+
+
+@pytest.mark.parametrize("count,m", [(3, 3), (4, 4), (9, 4)])
+def test_a_count_goes_with_matrices_of_less_room(ctx, count, m):  # noqa: F811
+    """A list has room for the whole map and the matrices for the rows that there are: they are the call's room."""
+    rng = np.random.default_rng(3)
+    x, h = rand(rng, (20, 32), "f32"), rand(rng, (4, 32), "f32")
+    w, ws = q_weights(rng, 32, 48)
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    at = torch.from_numpy(rng.permutation(20).astype(np.int32)).cuda()
+    c = torch.tensor([count], dtype=torch.int32, device="cuda")
+    y, z, out, two = (torch.full(s, 7.0, device="cuda") for s in ((20, 32), (4, 32), (4, 48), (4, 48)))
+    q, qs = torch.zeros(4, 32, dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
+    ctx.rows_norm(x, h, y=y, z=z, q=q, q_scale=qs, idx=at, count=c)
+    weights.linear(x, out=out, idx=at, count=c)
+    rows, scales = ctx.rows_quantize(x)
+    weights.matmul(rows, scales, out=two, dtype=torch.float32, count=c)
+    ctx.sync()
+    i = at[:m].long()
+    want = torch.full_like(y, 7.0)
+    want[i] = x[i] + h[:m]
+    assert torch.equal(y, want) and torch.equal(z[:m], want[i]) and (z[m:] == 7.0).all() and (q[m:] == 0).all()
+    assert torch.equal(out[:m], weights.linear(x[i])) and (out[m:] == 7.0).all()
+    assert torch.equal(two[:m], weights.linear(x[:m])) and (two[m:] == 7.0).all()
