@@ -195,9 +195,10 @@ __device__ __forceinline__ void make_panel(const FewRows& n, int t0, int count, 
     static_assert(TOKENS == WAVES * (kWave / L), "a row for each eight lanes");
     const int lane = threadIdx.x % L, r = threadIdx.x / L, c = n.c;
     const float inv_c = 1.0f / (float)c;
-    int turn = 0, i = t0 + r;
-    if (n.idx != nullptr) i = i < count ? n.idx[i] : -1;
-    const bool token = t0 + r < count && i >= 0 && i < n.map_rows;
+    const bool in = in_rows(t0, r, count);
+    int turn = 0, i = in ? t0 + r : -1;
+    if (n.idx != nullptr && in) i = n.idx[i];
+    const bool token = i >= 0 && i < n.map_rows;
     const T* x = static_cast<const T*>(n.x) + (int64_t)(token ? i : 0) * n.ldx;
     u32x4 raw[NV];
 #pragma unroll
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int tw = wave / CW, cw = wave % CW;
     const int count = row_count(a.count, a.rows);
-    const int tiles_t = (count + S::tokens - 1) / S::tokens, tiles_c = (a.n + S::channels - 1) / S::channels;
+    const int tiles_t = tiles_of(count, S::tokens), tiles_c = tiles_of(a.n, S::channels);
     const int blocks_c = (a.n + kPackC - 1) / kPackC;
     const int w_block_bytes = a.kt * kPackK * kPackC;          // 2 MB at most
     // (workgroups that share a tile are neighbours, so on one XCD; the grid has one for each)
@@ -396,14 +397,14 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
 #pragma unroll
             for (int f = 0; f < FC; ++f) acc[t][f] = i32x16{};
         // what the sums are scaled with: a channel's and a row's by each thread, dealt out when the sums are there
-        const int my_ch = c0 + (int)threadIdx.x, my_row = t0 + (int)threadIdx.x;
+        const int my_ch = c0 + (int)threadIdx.x;
         float my_ws = 0.0f, my_bias = 0.0f, my_rs = 0.0f;
         if ((int)threadIdx.x < S::channels && my_ch < a.n) {
             my_ws = a.w_scale[my_ch];
             if (a.bias != nullptr) my_bias = (float)static_cast<const T*>(a.bias)[my_ch];
         }
         if constexpr (MODE != kPanel)
-            if ((int)threadIdx.x < S::tokens && my_row < count) my_rs = a.q_scale[my_row];
+            if ((int)threadIdx.x < S::tokens && in_rows(t0, (int)threadIdx.x, count)) my_rs = a.q_scale[t0 + (int)threadIdx.x];
         int kt = 0;
 #pragma clang loop unroll(disable)
         for (; kt + NB <= kts; kt += NB)
@@ -440,9 +441,9 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
         meet();
         int8_t* mine = out_lds + wave * S::unit;
         constexpr int E = RowVec<T>::E, PW = S::row / 16, UF = PW * E / 32;
-        // this lane's first 16 bytes on their way out: row r0, channel ch0
-        const int r0 = t0 + tw * FT * 32 + lane / PW, ch0 = c0 + cw * FC * 32 + lane % PW * E;
-        T* const y0 = static_cast<T*>(a.y) + (int64_t)r0 * a.ldy + ch0;
+        // this lane's first 16 bytes on their way out: row r0 of the tile, channel ch0
+        const int r0 = tw * FT * 32 + lane / PW, ch0 = c0 + cw * FC * 32 + lane % PW * E;
+        T* const y0 = static_cast<T*>(a.y) + ((int64_t)t0 + r0) * a.ldy + ch0;
         const bool cut = c0 + S::channels > a.n && a.n % E != 0;
         constexpr int kAsk = 2;
         auto leave = [&](auto acts) {                          // 0: no activation, 1: one, kAsk: see there
@@ -470,7 +471,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
                     static_assert(kWave / PW % PW == 0, "whole exchanges of places");
                     T* y = y0 + (int64_t)(t * 32) * a.ldy + u * UF * 32;
                     const auto piece = [&](int i) { return *reinterpret_cast<const AlignedVec<T>*>(from + i * kWave * 16); };
-                    const int ch = ch0 + u * UF * 32, left = count - r0 - t * 32;        // rows from this lane's first one on
+                    const int ch = ch0 + u * UF * 32, left = count - t0 - r0 - t * 32;   // rows from this lane's first one on
                     const int whole = ch + E <= a.n ? left : 0;
 #pragma unroll
                     for (int i = 0; i < 32 * PW / kWave; ++i) {

@@ -156,3 +156,37 @@ def test_a_count_goes_with_matrices_of_less_room(ctx, count, m):  # noqa: F811
     assert torch.equal(y, want) and torch.equal(z[:m], want[i]) and (z[m:] == 7.0).all() and (q[m:] == 0).all()
     assert torch.equal(out[:m], weights.linear(x[i])) and (out[m:] == 7.0).all()
     assert torch.equal(two[:m], weights.linear(x[:m])) and (two[m:] == 7.0).all()
+
+
+# ---- the longest calls ------------------------------------------------------------------------------------------------
+def test_product_of_the_most_rows(ctx):  # noqa: F811
+    """2^31 - 1 rows (34 GB of them): the last tile ends where 32 bits do."""
+    rows, k = 0x7fffffff, 16
+    rng = np.random.default_rng(31)
+    w, ws = q_weights(rng, k, 1)
+    ws.fill_(0.5)
+    q, qs = torch.zeros(rows, k, dtype=torch.int8, device="cuda"), torch.full((rows,), 0.25, device="cuda")
+    at = torch.tensor([0, 1, 127, 128, 1 << 30, rows - 300, rows - 256, rows - 129, rows - 128, rows - 127, rows - 2, rows - 1], device="cuda")
+    q[at] = torch.from_numpy(rng.integers(-8, 9, (len(at), k), dtype=np.int8)).cuda()
+    want = (q[at].double() @ w.double()) * 0.125 + 1.0             # (sums below 2^14, eighths: exact in fp32)
+    weights = pkg.RowWeights(ctx, w, scale=ws, bias=torch.ones(1, device="cuda"))
+    out = torch.empty(rows, 1, device="cuda")
+    for count in (None, rows - 1, rows - 100, rows - 128, rows - 257, 3):
+        out.fill_(-3.0)
+        weights.matmul(q, qs, dtype=torch.float32, out=out, count=None if count is None else torch.tensor([count], dtype=torch.int32, device="cuda"))
+        ctx.sync()
+        n = rows if count is None else count
+        here = at < n
+        assert torch.equal(out[at[here]].double(), want[here]), count
+        for lo in range(0, rows, 1 << 28):                         # rows of zeros are the bias, rows behind the count what they were
+            part, end = out[lo:lo + (1 << 28)], max(0, min(n - lo, 1 << 28))
+            assert int((part[:end] != 1.0).sum()) <= len(at) and bool((part[end:] == -3.0).all()), (count, lo)
+
+
+def test_norm_of_the_most_rows(ctx):  # noqa: F811
+    rows = 0x7fffffff
+    x = torch.full((rows, 1), 0.5, dtype=torch.float16, device="cuda")
+    x[rows - 1], x[rows - 2], x[0] = 3.0, 4.0, 5.0
+    _, z, _, _ = ctx.rows_norm(x, z=True)
+    ctx.sync()
+    assert all(torch.equal(z[lo:lo + (1 << 28)], x[lo:lo + (1 << 28)]) for lo in range(0, rows, 1 << 28))

@@ -58,3 +58,35 @@ def test_k_tiles_are_there_when_they_are_read(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2203_03996_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+ROWS = r"""
+#include <cstdio>
+#include <initializer_list>
+#include "tile_schedule.h"
+using namespace dcnn;
+int main() {
+    int bad = 0;
+    const int tops[] = {0, 1, 2, 31, 32, 63, 64, 65, 127, 128, 255, 256, 257, 1 << 24, 0x7ffffeff, 0x7fffff00, 0x7fffff01, 0x7fffff80, 0x7fffff81, 0x7fffffc1, 0x7ffffffe, 0x7fffffff};
+    for (int per : {32, 64, 128, 256})
+        for (int rows : tops) {
+            const long long tiles = tiles_of(rows, per);
+            if (tiles * per < rows || (tiles - 1) * per >= rows) ++bad, printf("%d rows in tiles of %d: %lld\n", rows, per, tiles);
+            if (rows == 0) continue;
+            const int t0 = (int)((tiles - 1) * per);             // the last tile
+            for (int r = 0; r < per; ++r)
+                if (in_rows(t0, r, rows) != ((long long)t0 + r < rows)) ++bad, printf("%d rows: row %d of the tile at %d\n", rows, r, t0);
+        }
+    return bad != 0;
+}
+"""
+
+
+def test_tiles_of_the_longest_calls(tmp_path):
+    """Up to 2^31 - 1 rows: sums that pass 32 bits would leave a call without tiles, or its last rows' scales to be read from elsewhere."""
+    src = tmp_path / "rows.cpp"
+    src.write_text(ROWS)
+    exe = tmp_path / "rows"
+    subprocess.run(["g++", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", os.path.join(ROOT, "paper_2203_03996_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
