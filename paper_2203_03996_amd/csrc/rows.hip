@@ -1,4 +1,5 @@
 // C entry points of the row operators: checks of arguments, no kernels.
+#include "overlap.h"
 #include "rows.h"
 
 using namespace dcnn;
@@ -48,6 +49,20 @@ void set_norm(const dcnn_row_norm& n, int* kind, float* eps, const void** w, con
     *w = n.kind == DCNN_NORM_NONE ? nullptr : n.w_dev;
     *b = n.kind == DCNN_NORM_NONE ? nullptr : n.b_dev;
 }
+// An output shares no byte with an input or another output: workgroups run in any order, and what one of them reads another may have
+// written over.  (`x` may be `y`, the caller says where: a row is read before it is written.)
+template <int OUTS, int INS>
+dcnn_status check_apart(dcnn_ctx* ctx, const char* what, const Bytes (&outs)[OUTS], const Bytes (&ins)[INS], const Bytes* y = nullptr, const Bytes* x = nullptr) {
+    for (int i = 0; i < OUTS; ++i) {
+        for (int j = i + 1; j < OUTS; ++j)
+            if (overlap(outs[i], outs[j])) return fail(ctx, DCNN_EINVAL, "%s: %s overlaps %s", what, outs[i].name, outs[j].name);
+        for (int j = 0; j < INS; ++j)
+            if (!(&outs[i] == y && &ins[j] == x) && overlap(outs[i], ins[j])) return fail(ctx, DCNN_EINVAL, "%s: %s overlaps %s", what, outs[i].name, ins[j].name);
+    }
+    return DCNN_OK;
+}
+Bytes vector_bytes(const char* name, const void* p, int64_t bytes) { return {name, p, 1, bytes, bytes}; }
+Bytes matrix_bytes(const char* name, const void* p, int64_t rows, int64_t ld, int64_t c, size_t es) { return {name, p, rows, ld * (int64_t)es, c * (int64_t)es}; }
 // Scratch, which grows with the rows: the counts of workgroups that share a tile (at the same place whatever the sizes: they are zero between calls), their
 // partial sums, then the 8-bit rows of a call that makes some: scales, rows
 struct Scratch {
@@ -95,6 +110,17 @@ dcnn_status check_matmul(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul
     return DCNN_OK;
 }
 
+// ... y and scratch from what every product reads and from the rows (`ins`) of this one
+template <int INS> dcnn_status check_product_apart(dcnn_ctx* ctx, const char* what, const dcnn_rows_matmul_args* p, int linear, const Bytes (&ins)[INS]) {
+    const size_t es = rows_dtype_size(p->dtype);
+    const Bytes outs[] = {matrix_bytes("y", p->y_dev, p->list.rows, p->ldy, p->n, es),
+                          vector_bytes("scratch", p->scratch_dev, (int64_t)dcnn_rows_scratch_bytes(p->list.rows, p->k, p->n, linear))};
+    const Bytes all[] = {vector_bytes("the packed weights", p->packed_dev, (int64_t)dcnn_rows_weights_bytes(p->k, p->n)), vector_bytes("bias", p->bias_dev, p->n * es),
+                         vector_bytes("count", p->list.count_dev, 4)};
+    const dcnn_status st = check_apart(ctx, what, outs, all);
+    return st == DCNN_OK ? check_apart(ctx, what, outs, ins) : st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,10 +150,8 @@ dcnn_status dcnn_rows_norm(dcnn_ctx* ctx, const dcnn_rows_norm_args* p) {
     if (st == DCNN_OK) st = check_ld(ctx, what, "gate", p->gate_dev, p->gate_rows ? p->ldg : p->c, p->c, es);
     if (st == DCNN_OK && (p->q_dev != nullptr || p->q_scale_dev != nullptr)) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->c);
     if (st != DCNN_OK) return st;
-    const auto same = [](const void* a, const void* b) { return a != nullptr && a == b; };
-    if (same(p->y_dev, p->h_dev) || same(p->z_dev, p->h_dev) || same(p->z_dev, p->x_dev) || same(p->z_dev, p->y_dev))
-        return fail(ctx, DCNN_EINVAL, "%s: an output in the place of an input or another output (y may be x)", what);
-    if (p->y_dev != nullptr && p->y_dev == p->x_dev && p->ldy != p->ldx && p->list.map_rows > 1)
+    const bool in_place = p->y_dev != nullptr && p->y_dev == p->x_dev;
+    if (in_place && p->ldy != p->ldx && p->list.map_rows > 1)
         return fail(ctx, DCNN_ESHAPE, "%s: in place with leading dimensions %lld and %lld", what, (long long)p->ldx, (long long)p->ldy);
 
     NormArgs a;
@@ -139,6 +163,16 @@ dcnn_status dcnn_rows_norm(dcnn_ctx* ctx, const dcnn_rows_norm_args* p) {
     a.c = p->c, a.scale = p->scale;
     set_norm(p->post, &a.post, &a.post_eps, &a.post_w, &a.post_b);
     set_norm(p->pre, &a.pre, &a.pre_eps, &a.pre_w, &a.pre_b);
+    const int64_t rows = p->list.rows, map_rows = p->list.idx_dev != nullptr ? p->list.map_rows : rows, c = p->c;
+    const Bytes outs[] = {matrix_bytes("y", p->y_dev, map_rows, p->ldy, c, es), matrix_bytes("z", p->z_dev, rows, p->ldz, c, es),
+                          matrix_bytes("q", p->q_dev, rows, p->ldq, align_up((size_t)c, 16), 1), vector_bytes("q_scale", p->q_scale_dev, rows * 4)};
+    const Bytes ins[] = {matrix_bytes("x", p->x_dev, map_rows, p->ldx, c, es), matrix_bytes("h", p->h_dev, rows, p->ldh, c, es),
+                         matrix_bytes("the gate", p->gate_dev, p->gate_rows ? cdiv(map_rows, p->gate_rows) : 1, p->ldg, c, es),
+                         vector_bytes("a norm's weight", a.post_w, c * es), vector_bytes("a norm's bias", a.post_b, c * es),
+                         vector_bytes("a norm's weight", a.pre_w, c * es), vector_bytes("a norm's bias", a.pre_b, c * es),
+                         vector_bytes("idx", a.idx, rows * 4), vector_bytes("count", a.count, 4)};
+    st = check_apart(ctx, what, outs, ins, in_place ? &outs[0] : nullptr, &ins[0]);
+    if (st != DCNN_OK) return st;
     a.gate_div = p->gate_rows ? make_fastdiv((uint32_t)p->gate_rows) : FastDiv{0, 0, 0};
     return launch_rows_norm(ctx, p->dtype, a);
 }
@@ -157,10 +191,14 @@ dcnn_status dcnn_rows_pack(dcnn_ctx* ctx, int32_t dtype, int64_t k, int64_t n, c
     if (need == 0) return fail(ctx, DCNN_EINVAL, "%s: k %lld, n %lld", what, (long long)k, (long long)n);
     if (w_dev == nullptr || packed_dev == nullptr) return fail(ctx, DCNN_EINVAL, "%s: null weights", what);
     if ((scale_dev != nullptr) != (dtype == DCNN_I8)) return fail(ctx, DCNN_EINVAL, "%s: scales come with 8-bit weights and with no others", what);
-    const dcnn_status st = check_ld(ctx, what, "weights", w_dev, ldw, n, rows_dtype_size(dtype));
+    dcnn_status st = check_ld(ctx, what, "weights", w_dev, ldw, n, rows_dtype_size(dtype));
     if (st != DCNN_OK) return st;
     if (!aligned(packed_dev, kAlign) || !aligned(scale_dev, 4)) return fail(ctx, DCNN_EINVAL, "%s: misaligned buffer", what);
     if (packed_bytes < need) return fail(ctx, DCNN_ENOMEM, "%s: %zu bytes, %zu needed", what, packed_bytes, need);
+    const Bytes outs[] = {vector_bytes("packed", packed_dev, (int64_t)need)};
+    const Bytes ins[] = {matrix_bytes("the weights", w_dev, k, ldw, n, rows_dtype_size(dtype)), vector_bytes("scale", scale_dev, n * 4)};
+    st = check_apart(ctx, what, outs, ins);
+    if (st != DCNN_OK) return st;
     int8_t* packed = static_cast<int8_t*>(packed_dev);
     return launch_rows_pack(ctx, dtype, k, n, w_dev, ldw, scale_dev, packed, reinterpret_cast<float*>(packed + packed_scale_offset(k, n)));
 }
@@ -179,7 +217,9 @@ dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     dcnn_status st = check_matmul(ctx, what, p, 0, &m);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK) st = check_q(ctx, what, p->q_dev, p->q_scale_dev, p->ldq, p->k);
-    if (st == DCNN_OK && p->q_dev == p->y_dev) st = fail(ctx, DCNN_EINVAL, "%s: y in the place of q, which other workgroups read", what);
+    if (st != DCNN_OK) return st;
+    const Bytes ins[] = {matrix_bytes("q", p->q_dev, p->list.rows, p->ldq, p->k, 1), vector_bytes("q_scale", p->q_scale_dev, p->list.rows * 4)};
+    st = check_product_apart(ctx, what, p, 0, ins);
     if (st != DCNN_OK) return st;
     m.q = p->q_dev, m.q_scale = p->q_scale_dev, m.ldq = (int)p->ldq;
     return launch_rows_matmul(ctx, p->dtype, matmul_plan(p->list.rows, p->k, p->n, p->list.count_dev != nullptr), m);
@@ -195,7 +235,6 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     if (st == DCNN_OK) st = check_map(ctx, what, p->list);
     if (st == DCNN_OK && p->list.rows == 0) return st;
     if (st == DCNN_OK && p->x_dev == nullptr) st = fail(ctx, DCNN_EINVAL, "%s: x is null", what);
-    if (st == DCNN_OK && p->x_dev == p->y_dev) st = fail(ctx, DCNN_EINVAL, "%s: y in the place of x, which other workgroups read", what);
     if (st == DCNN_OK) st = check_ld(ctx, what, "x", p->x_dev, p->ldx, p->k, rows_dtype_size(p->dtype));
     if (st == DCNN_OK) st = check_norm(ctx, what, p->pre, rows_dtype_size(p->dtype));
     if (st != DCNN_OK) return st;
@@ -209,6 +248,11 @@ dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* p) {
     a.q_scale = reinterpret_cast<float*>(scratch + at.scales);
     a.q = reinterpret_cast<int8_t*>(scratch + at.rows), a.ldq = (int)at.ldq;
     set_norm(p->pre, &a.pre, &a.pre_eps, &a.pre_w, &a.pre_b);
+    const size_t es = rows_dtype_size(p->dtype);
+    const Bytes ins[] = {matrix_bytes("x", p->x_dev, a.idx != nullptr ? a.map_rows : a.rows, p->ldx, p->k, es), vector_bytes("a norm's weight", a.pre_w, p->k * es),
+                         vector_bytes("a norm's bias", a.pre_b, p->k * es), vector_bytes("idx", a.idx, p->list.rows * 4)};
+    st = check_product_apart(ctx, what, p, 1, ins);
+    if (st != DCNN_OK) return st;
     if (rows_linear_fuses(p->dtype, p->list.rows, p->k, p->n, p->list.count_dev != nullptr)) return launch_rows_linear_fused(ctx, p->dtype, a, m);
     st = launch_rows_norm(ctx, p->dtype, a);
     if (st != DCNN_OK) return st;

@@ -190,3 +190,59 @@ def test_norm_of_the_most_rows(ctx):  # noqa: F811
     _, z, _, _ = ctx.rows_norm(x, z=True)
     ctx.sync()
     assert all(torch.equal(z[lo:lo + (1 << 28)], x[lo:lo + (1 << 28)]) for lo in range(0, rows, 1 << 28))
+
+
+# ---- outputs that share bytes with what is read -----------------------------------------------------------------------
+def test_outputs_that_reach_into_inputs_are_refused(ctx):  # noqa: F811
+    """Not only at the same address: a row further on, in the middle, in the gate, in parameters, in one another."""
+    buf = torch.full((40, 64), 2.0, device="cuda")
+    x, h, z, y = buf[0:8], buf[8:16], buf[16:24], buf[24:32]
+    whole = torch.ones(64, 64, device="cuda")
+    weights = pkg.RowWeights(ctx, whole)
+    idx = torch.arange(8, dtype=torch.int32, device="cuda")
+    flat = buf.view(-1)
+    q8 = torch.ones(40, 64, dtype=torch.int8, device="cuda")
+    out8 = q8.view(torch.float32).view(-1)                         # the same bytes as floats
+    scales = torch.ones(8, device="cuda")
+    small = pkg.RowWeights(ctx, whole[:, :8].contiguous())
+    bad = [lambda: ctx.rows_norm(x, h, y=buf[1:9]), lambda: ctx.rows_norm(x, h, y=buf[7:15]), lambda: ctx.rows_norm(x, h, y=flat[3:515].view(8, 64)),
+           lambda: ctx.rows_norm(x, z=buf[1:9]), lambda: ctx.rows_norm(x, h, y=y, z=buf[25:33]), lambda: ctx.rows_norm(x, h, z=buf[9:17]),
+           lambda: ctx.rows_norm(x, h, gate=y[:4], gate_rows=2, y=y), lambda: ctx.rows_norm(x, h, gate=y[5], y=y), lambda: ctx.rows_norm(x, h, gate=x, gate_rows=1, y=x),
+           lambda: ctx.rows_norm(x, h, post=pkg.RowNorm("rms", y[3]), y=y), lambda: ctx.rows_norm(x, pre=pkg.RowNorm("layer", None, z[7]), z=z),
+           lambda: ctx.rows_norm(x, q=buf.view(torch.int8).view(-1)[:8 * 64].view(8, 64), q_scale=scales), lambda: ctx.rows_norm(x, q=q8[:8], q_scale=flat[60:68]),
+           lambda: ctx.rows_norm(x, h, y=y, q=q8[:8], q_scale=y.view(-1)[504:]), lambda: ctx.rows_norm(x, z=buf.view(torch.float32)[4:12], idx=idx),
+           lambda: weights.linear(x, out=buf[1:9]), lambda: weights.linear(x, out=buf[6:14], idx=idx), lambda: weights.linear(x, pre=pkg.RowNorm("rms", z[1]), out=z),
+           lambda: small.matmul(q8[:8], scales, dtype=torch.float32, out=out8[16:80].view(8, 8)),
+           lambda: pkg.RowWeights(ctx, whole, bias=z[0]).linear(x, out=z)]
+    for i, call in enumerate(bad):
+        with pytest.raises(pkg.DcnnError) as e:
+            call()
+        assert e.value.status == 1 and "overlaps" in str(e.value), (i, e.value)
+    need = ctx.lib.dcnn_rows_weights_bytes(64, 64)
+    both = torch.full((need + 64 * 64 * 4,), 5, dtype=torch.uint8, device="cuda")
+    at = both.data_ptr()
+    assert ctx.lib.dcnn_rows_pack(ctx.handle, 0, 64, 64, at + need - 4, 64, None, at, need) == 1
+    assert ctx.lib.dcnn_rows_pack(ctx.handle, 3, 64, 64, at + need, 64, at + need - 256, at, need) == 1
+    ctx.sync()
+    assert (buf == 2.0).all() and (q8 == 1).all() and (both == 5).all(), "a refused call wrote something"
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("c", [64, 61])
+def test_matrices_between_the_columns_of_one_buffer(ctx, dt, c):  # noqa: F811
+    """Views whose rows lie in each other's gaps share no byte: taken, and right."""
+    rng = np.random.default_rng(c)
+    rows = 50
+    wide = rand(rng, (rows, 4 * c), dt)
+    x, h, y, z = (wide[:, i * c:(i + 1) * c] for i in range(4))
+    apart = [t.clone() for t in (x, h)]
+    norm = pkg.RowNorm("rms", rand(rng, c, dt, 0.3, 1.0))
+    want = ctx.rows_norm(*apart, post=norm, pre=norm, y=True, z=True)[:2]
+    ctx.rows_norm(x, h, post=norm, pre=norm, y=y, z=z)
+    assert torch.equal(y, want[0]) and torch.equal(z, want[1]) and torch.equal(x, apart[0]) and torch.equal(h, apart[1])
+    weights = pkg.RowWeights(ctx, rand(rng, (c, c), dt))
+    want = weights.linear(apart[0], pre=norm)
+    weights.linear(x, pre=norm, out=z)
+    assert torch.equal(z, want) and torch.equal(y, ctx.rows_norm(*apart, post=norm, y=True)[0])
+    ctx.rows_norm(x, h, post=norm, y=x)                            # (in place, as before)
+    assert torch.equal(x, y)
