@@ -237,7 +237,7 @@ __device__ __forceinline__ void make_panel(const FewRows& n, int t0, int count, 
 }
 
 // kWhole: workgroups stride through the tiles.  kParts: `splits` workgroups share a tile, each `share` of its K-tiles.  kPanel: a workgroup
-// makes the 8-bit rows of a token tile itself and keeps them; `splits` workgroups share its channel tiles, `share` to each.
+// has one tile and makes the 8-bit rows of its tokens itself.
 template <typename T, int TW, int CW, int FT, int FC, int NB, TileMode MODE>
 __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulArgs a, int splits, int share, std::conditional_t<MODE == kPanel, FewRows, int> n) {
     using S = TileShape<T, TW, CW, FT, FC, NB, MODE>;
@@ -259,16 +259,14 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     const int tiles_t = tiles_of(count, S::tokens), tiles_c = tiles_of(a.n, S::channels);
     const int blocks_c = (a.n + kPackC - 1) / kPackC;
     const int w_block_bytes = a.kt * kPackK * kPackC;          // 2 MB at most
-    // (workgroups that share a tile are neighbours, so on one XCD; the grid has one for each)
-    const WgTileRange mine_of = wg_tile_range(MODE == kPanel ? (int64_t)tiles_t * splits : (int64_t)tiles_t * tiles_c * (MODE == kParts ? splits : 1));
-    if (mine_of.begin >= mine_of.end) return;
-    const int part = MODE != kWhole ? (int)(mine_of.begin % splits) : 0, k0 = MODE == kParts ? part * share : 0;
+    // (workgroups that share a tile, or the rows of one, are neighbours, so on one XCD; the grid has one for each)
+    const WgTileRange range = wg_tile_range((int64_t)tiles_t * tiles_c * (MODE == kParts ? splits : 1));
+    if (range.begin >= range.end) return;
+    const int part = MODE == kParts ? (int)(range.begin % splits) : 0, k0 = MODE == kParts ? part * share : 0;
     const int kts = MODE == kParts ? (a.kt - k0 < share ? a.kt - k0 : share) : a.kt;
-    const int panel_t = MODE == kPanel ? (int)(mine_of.begin / splits) : 0;
-    const WgTileRange range = MODE == kPanel ? WgTileRange{(int64_t)part * share, (part + 1) * share < tiles_c ? (part + 1) * share : tiles_c, 1} : mine_of;
-    if (MODE == kPanel && range.begin >= range.end) return;
+    const TileAt only = MODE == kPanel ? TileAt{(int)((uint32_t)range.begin / (uint32_t)tiles_c), (int)((uint32_t)range.begin % (uint32_t)tiles_c)} : TileAt{};
     auto place_of = [&](int64_t tile) -> TileAt {
-        if constexpr (MODE == kPanel) return {panel_t, (int)tile};
+        if constexpr (MODE == kPanel) return only;
         else return tile_at((int)(MODE == kParts ? tile / splits : tile), tiles_t, tiles_c);
     };
     extern __shared__ __align__(16) int8_t panel[];
@@ -378,7 +376,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     if constexpr (MODE == kPanel) {
         float* const scales = reinterpret_cast<float*>(panel + kts * (S::tokens * kPackK));
         constexpr int X = 8 / RowVec<T>::E;                    // (vectors of a lane: twice as many in fp32)
-        const int t0 = panel_t * S::tokens;
+        const int t0 = only.t * S::tokens;
         if (n.c <= 64) make_panel<T, X, S::tokens, S::waves>(n, t0, count, panel, scales);
         else if (n.c <= 128) make_panel<T, 2 * X, S::tokens, S::waves>(n, t0, count, panel, scales);
         else make_panel<T, 4 * X, S::tokens, S::waves>(n, t0, count, panel, scales);
@@ -501,7 +499,7 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
 template <typename T, int TW, int CW, int FT, int FC, int NB, TileMode MODE = kWhole>
 static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 1, int share = 0, const FewRows* rows = nullptr) {
     using S = TileShape<T, TW, CW, FT, FC, NB, MODE>;
-    const int64_t tiles = cdiv(a.rows, S::tokens) * (MODE == kPanel ? 1 : cdiv(a.n, S::channels)) * splits;
+    const int64_t tiles = cdiv(a.rows, S::tokens) * cdiv(a.n, S::channels) * splits;
     const int64_t most = MODE != kWhole ? tiles : (int64_t)ctx->num_cu * (int64_t)(ctx->max_lds / S::lds);
     const int64_t grid = cdiv(tiles < most ? tiles : most, kXcd) * kXcd;   // (tile_range deals out to whole rounds of XCDs)
     if constexpr (MODE == kPanel) {
@@ -694,10 +692,7 @@ bool rows_linear_fuses(int dtype, int64_t rows, int64_t k, int64_t n, bool count
 }
 
 template <typename T> static dcnn_status launch_linear_t(dcnn_ctx* ctx, const FewRows& n, const MatmulArgs& a) {
-    if (!fuses_few(sizeof(T) == 4 ? DCNN_F32 : DCNN_F16, a.rows, n.c)) {
-        const int64_t tiles_c = cdiv(a.n, 128);
-        return launch_tile<T, 2, 4, 1, 1, 2, kPanel>(ctx, a, (int)tiles_c, 1, &n);
-    }
+    if (!fuses_few(sizeof(T) == 4 ? DCNN_F32 : DCNN_F16, a.rows, n.c)) return launch_tile<T, 2, 4, 1, 1, 2, kPanel>(ctx, a, 1, 0, &n);
     const bool one = (int64_t)cdiv(n.c, 64) * 64 <= kFewWaves * kWave * RowVec<T>::E;
     if (a.rows == 1) return one ? launch_few<T, 1, 1, 1, 1>(ctx, a, n) : launch_few<T, 1, 1, 1, 2>(ctx, a, n);
     return one ? launch_few<T, 1, 1, kFewNorm, 1>(ctx, a, n) : launch_few<T, 1, 1, kFewNorm, 2>(ctx, a, n);

@@ -148,8 +148,9 @@ template <typename T, bool BLOCK> static dcnn_status launch_norm_t(dcnn_ctx* ctx
     if (v <= 512) return launch_norm_shape<T, 256, 2, BLOCK>(ctx, a);
     if (v <= 1024) return launch_norm_shape<T, 512, 2, BLOCK>(ctx, a);
     if (v <= 2048) return launch_norm_shape<T, 1024, 2, BLOCK>(ctx, a);
-    if (v <= 4096) return launch_norm_shape<T, 1024, 4, BLOCK>(ctx, a);
-    return launch_norm_shape<T, 1024, 8, BLOCK>(ctx, a);
+    if constexpr (kRowsMaxC / RowVec<T>::E > 4096)             // (fp32 alone)
+        if (v > 4096) return launch_norm_shape<T, 1024, 8, BLOCK>(ctx, a);
+    return launch_norm_shape<T, 1024, 4, BLOCK>(ctx, a);
 }
 template <typename T> static dcnn_status launch_norm_any(dcnn_ctx* ctx, const NormArgs& a) {
     return a.h != nullptr ? launch_norm_t<T, true>(ctx, a) : launch_norm_t<T, false>(ctx, a);
