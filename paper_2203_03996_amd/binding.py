@@ -197,6 +197,7 @@ class Context:
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
         self.stream = torch.cuda.current_stream(self.device)
         self.index, self._raw_stream = self.stream.device_index, self.stream.cuda_stream
+        self._gpu = torch.device("cuda", self.index)
         h = C.c_void_p()
         st = self.lib.dcnn_ctx_create(C.c_void_p(self.stream.cuda_stream), C.c_void_p(_ptr(self.workspace)),
                                       nbytes, C.byref(h))
@@ -253,16 +254,16 @@ class Context:
                                                      _ptr(mask_out), _ptr(idx), _ptr(count)))
 
     def empty(self, shape, dtype):
-        """An uninitialised device tensor that belongs to the context's stream, whichever stream torch is on."""
+        """An uninitialised device tensor that belongs to the context's GPU and stream, whichever torch is on."""
         # (torch.cuda.current_stream builds an object, 3 us; the calls that allocate their outputs take 8 in all)
         if torch._C._cuda_getCurrentRawStream(self.index) == self._raw_stream:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty(shape, dtype=dtype, device=self._gpu)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty(shape, dtype=dtype, device=self._gpu)
 
     def capturing(self) -> bool:
         """Whether a graph is being captured on the context's stream, whichever stream torch is on."""
-        if torch._C._cuda_getCurrentRawStream(self.index) == self._raw_stream:
+        if torch._C._cuda_getCurrentRawStream(self.index) == self._raw_stream and torch.cuda.current_device() == self.index:
             return torch.cuda.is_current_stream_capturing()
         with torch.cuda.stream(self.stream):
             return torch.cuda.is_current_stream_capturing()
@@ -525,13 +526,13 @@ class RowWeights:
 
     def __init__(self, ctx: Context, weights: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None, act="none"):
         self.ctx, lib = ctx, ctx.lib
-        if weights.dim() != 2 or weights.stride(1) != 1 or not weights.is_cuda:
-            raise ValueError("weights must be a device matrix [k, n] with its rows side by side")
+        if weights.dim() != 2 or weights.stride(1) != 1 or weights.get_device() != ctx.index:
+            raise ValueError(f"weights must be a matrix [k, n] on GPU {ctx.index}, the elements of a row side by side")
         k, n = weights.shape
         code = I8 if weights.dtype == torch.int8 else _row_dtype(weights.dtype)
         if (scale is not None) != (code == I8) or (scale is not None and (scale.shape != (n,) or scale.dtype != torch.float32 or
-                                                                          not scale.is_contiguous() or not scale.is_cuda)):
-            raise ValueError(f"8-bit weights come with a float32 scale [{n}] on the device, others without one")
+                                                                          not scale.is_contiguous() or scale.get_device() != ctx.index)):
+            raise ValueError(f"8-bit weights come with a float32 scale [{n}] on GPU {ctx.index}, others without one")
         self.k, self.n, self.bias = k, n, bias
         nbytes = lib.dcnn_rows_weights_bytes(k, n)
         if nbytes == 0:
@@ -542,13 +543,13 @@ class RowWeights:
         for t in (weights, scale):                                # (their memory is theirs until the stream has read them)
             if t is not None:
                 t.record_stream(ctx.stream)
-        if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or not bias.is_cuda):
-            raise ValueError(f"bias must be a contiguous device tensor [{n}]")
+        if bias is not None and (bias.shape != (n,) or not bias.is_contiguous() or bias.get_device() != ctx.index):
+            raise ValueError(f"bias must be a contiguous tensor [{n}] on GPU {ctx.index}")
         self.act = ACT_CODES[act]
         # scratch for all products of 8-bit rows (partial sums: 8 MB at most) and the linear ones of few rows
         nbytes = max(lib.dcnn_rows_scratch_bytes(_ROWS_MAX, k, n, 0), lib.dcnn_rows_scratch_bytes(_SCRATCH_ROWS, k, n, 1))
         with torch.cuda.stream(ctx.stream):
-            self._scratch = torch.zeros(nbytes, dtype=torch.uint8, device=ctx.device)
+            self._scratch = torch.zeros(nbytes, dtype=torch.uint8, device=ctx._gpu)
         self._scratch_at = self._scratch.data_ptr(), nbytes
         self._grown, self._grown_rows, self._captured = None, 0, set()         # _captured: what graphs hold the address of
 
@@ -579,7 +580,7 @@ class RowWeights:
         if scratch is None or rows > self._grown_rows:
             need = self.ctx.lib.dcnn_rows_scratch_bytes(rows, self.k, self.n, 1)
             with torch.cuda.stream(self.ctx.stream):
-                scratch = torch.zeros(need, dtype=torch.uint8, device=self.ctx.device)
+                scratch = torch.zeros(need, dtype=torch.uint8, device=self.ctx._gpu)
             if not capturing:                                     # (else it is the graph's: the kernel that clears it runs when the graph does)
                 self._grown, self._grown_rows = scratch, rows
         elif capturing:

@@ -246,3 +246,15 @@ def test_matrices_between_the_columns_of_one_buffer(ctx, dt, c):  # noqa: F811
     assert torch.equal(z, want) and torch.equal(y, ctx.rows_norm(*apart, post=norm, y=True)[0])
     ctx.rows_norm(x, h, post=norm, y=x)                            # (in place, as before)
     assert torch.equal(x, y)
+
+
+# ---- the context's GPU ------------------------------------------------------------------------------------------------
+def test_weights_of_another_gpu_are_refused(ctx, monkeypatch):  # noqa: F811
+    """(the context says that it is on another one)"""
+    w, ws = q_weights(np.random.default_rng(0), 32, 8)
+    x = torch.zeros(4, 32, device="cuda")
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    monkeypatch.setattr(ctx, "index", 1)
+    for bad in (lambda: pkg.RowWeights(ctx, w, scale=ws), lambda: pkg.RowWeights(ctx, w.float()), lambda: weights.linear(x), lambda: ctx.rows_norm(x, z=True)):
+        with pytest.raises(ValueError, match="GPU 1"):
+            bad()

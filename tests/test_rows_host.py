@@ -135,8 +135,9 @@ def test_scratch_that_a_graph_clears_is_not_kept(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: current[0] in captured)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     ctx = pkg.Context.__new__(pkg.Context)
-    ctx.lib, ctx.index, ctx.stream, ctx._raw_stream, ctx.device = pkg.load_library(), 0, "the context's", "the context's", torch.device("cpu")
+    ctx.lib, ctx.index, ctx.stream, ctx._raw_stream, ctx._gpu = pkg.load_library(), 0, "the context's", "the context's", torch.device("cpu")
     weights = pkg.RowWeights.__new__(pkg.RowWeights)
     weights.__dict__.update(ctx=ctx, k=64, n=64, _grown=None, _grown_rows=0, _captured=set())
     captured.add("the context's")
@@ -149,3 +150,26 @@ def test_scratch_that_a_graph_clears_is_not_kept(monkeypatch):
     captured.add("the context's")
     at, _ = weights._linear_scratch(100)                           # a graph that uses it holds it
     assert at == weights._grown.data_ptr() and len(weights._captured) == 1
+
+
+def test_new_tensors_and_captures_are_those_of_the_contexts_gpu(monkeypatch):
+    """Two GPUs whose streams have the same handle (the default one, 0), and torch is on the other (both are stood in for)."""
+    import contextlib
+
+    import torch
+    made, entered = [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        entered.append(stream)
+        yield
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: made.append(device))
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: bool(entered))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    ctx = pkg.Context.__new__(pkg.Context)
+    ctx.device, ctx._gpu, ctx.index, ctx.stream, ctx._raw_stream = torch.device("cuda"), torch.device("cuda", 0), 0, "the context's", 0
+    ctx.empty((3, 4), torch.float32)
+    assert made == [torch.device("cuda", 0)]
+    assert ctx.capturing() and entered == ["the context's"]        # asked of the context's stream, not of the other GPU's
