@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from dataclasses import dataclass
 
 import numpy as np
@@ -522,7 +523,12 @@ class RowNorm:
 class RowWeights:
     """Weights [k, n] of a product, in 8 bits with a scale per output channel, laid out once for the matrix cores (dcnn_rows_pack).
 
-    weights: floating point (quantised here), or int8 with `scale` [n].  bias: [n] of the outputs' type, or None."""
+    weights: floating point (quantised here), or int8 with `scale` [n].  bias: [n] of the outputs' type, or None; each call reads
+    it where it lies then.
+
+    The object holds scratch that its calls share, as large as the 8-bit rows of its largest linear call (a list's: as many rows
+    as the list has room for).  Calls follow each other on the context's stream, and threads take turns.  Graphs hold the scratch
+    too: two that were captured from one object must not run at the same time, and the object has to outlive them."""
 
     def __init__(self, ctx: Context, weights: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None, act="none"):
         self.ctx, lib = ctx, ctx.lib
@@ -552,6 +558,7 @@ class RowWeights:
             self._scratch = torch.zeros(nbytes, dtype=torch.uint8, device=ctx._gpu)
         self._scratch_at = self._scratch.data_ptr(), nbytes
         self._grown, self._grown_rows, self._captured = None, 0, set()         # _captured: what graphs hold the address of
+        self._one_call = threading.Lock()
 
     def _call(self, call, linear, a, rows, dt, count, out):
         ctx = self.ctx
@@ -567,10 +574,11 @@ class RowWeights:
             a.y, a.ldy, n = _as_rows(out, "out", self.n, dt, ctx.index)
             rows = _room(rows, n, "out", count)
         a.rows = rows
-        a.scratch, a.scratch_bytes = self._scratch_at if not linear or rows <= _SCRATCH_ROWS else self._linear_scratch(rows)
-        st = call(ctx.handle, a)
-        if st:
-            ctx.check(st)
+        with self._one_call:                                      # (a call's kernels follow each other: both use the scratch)
+            a.scratch, a.scratch_bytes = self._scratch_at if not linear or rows <= _SCRATCH_ROWS else self._linear_scratch(rows)
+            st = call(ctx.handle, a)
+            if st:
+                ctx.check(st)
         return out
 
     def _linear_scratch(self, rows):

@@ -258,3 +258,27 @@ def test_weights_of_another_gpu_are_refused(ctx, monkeypatch):  # noqa: F811
     for bad in (lambda: pkg.RowWeights(ctx, w, scale=ws), lambda: pkg.RowWeights(ctx, w.float()), lambda: weights.linear(x), lambda: ctx.rows_norm(x, z=True)):
         with pytest.raises(ValueError, match="GPU 1"):
             bad()
+
+
+def test_threads_share_weights(ctx):  # noqa: F811
+    """Linear calls of several sizes from several threads: each has its own rows' results."""
+    import threading
+    rng = np.random.default_rng(41)
+    k, n = 512, 128
+    w, ws = q_weights(rng, k, n)
+    x = [rand(rng, (rows, k), "f16") for rows in (80, 300, 900, 2500)]
+    want = [pkg.RowWeights(ctx, w, scale=ws).linear(t) for t in x]
+    weights = pkg.RowWeights(ctx, w, scale=ws)
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        got = [weights.linear(x[i]) for _ in range(40)]
+        torch.cuda.synchronize()
+        wrong.extend(i for y in got if not torch.equal(y, want[i]))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

@@ -173,3 +173,37 @@ def test_new_tensors_and_captures_are_those_of_the_contexts_gpu(monkeypatch):
     ctx.empty((3, 4), torch.float32)
     assert made == [torch.device("cuda", 0)]
     assert ctx.capturing() and entered == ["the context's"]        # asked of the context's stream, not of the other GPU's
+
+
+def test_threads_take_turns_at_the_scratch_of_a_product(monkeypatch):
+    """A call is two launches that share scratch: no other call may come between its choice of scratch and its last launch (the library stood in for)."""
+    import threading
+    import time
+
+    import torch
+    inside, together, used = [], [], []
+
+    def call(handle, a):
+        inside.append(a)
+        time.sleep(0.002)                                          # (the interpreter's lock is not held in the library either)
+        together.append(len(inside))
+        used.append((a.rows, a.scratch_bytes))
+        inside.remove(a)
+        return 0
+
+    class Row(pkg.binding.RowsMatmulArgs):
+        __hash__ = object.__hash__
+    weights = pkg.RowWeights.__new__(pkg.RowWeights)
+    ctx = pkg.Context.__new__(pkg.Context)
+    ctx.lib, ctx.index, ctx.handle, ctx._gpu, ctx.stream = pkg.load_library(), -1, None, torch.device("cpu"), None
+    monkeypatch.setattr(ctx, "empty", lambda shape, dtype: torch.empty(shape, dtype=dtype), raising=False)
+    monkeypatch.setattr(ctx, "capturing", lambda: False, raising=False)
+    weights.__dict__.update(ctx=ctx, k=64, n=64, bias=None, act=0, packed=torch.zeros(1), _grown=None, _grown_rows=0, _captured=set(), _scratch_at=(0, 0),
+                            _one_call=threading.Lock())
+    threads = [threading.Thread(target=lambda r=r: [weights._call(call, 1, Row(), r, torch.float16, None, None) for _ in range(5)]) for r in (70, 200, 500, 900)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(used) == 20 and set(together) == {1}
+    assert all(size >= ctx.lib.dcnn_rows_scratch_bytes(rows, 64, 64, 1) for rows, size in used)
