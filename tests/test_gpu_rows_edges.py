@@ -282,3 +282,36 @@ def test_threads_share_weights(ctx):  # noqa: F811
     for t in threads:
         t.join()
     assert not wrong
+
+
+# ---- bits ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dt,ks", [("f16", (5, 77, 256, 300, 511, 512)), ("bf16", (8, 500, 512)), ("f32", (5, 77, 129, 255, 256))])
+def test_rows_of_a_wave_have_the_same_bits_alone_and_among_many(ctx, dt, ks, kind):  # noqa: F811
+    """Rows of up to 64 vectors of 16 bytes: normed by the kernel of one to four rows, by a tile's, or by the norm's own."""
+    for k in ks:
+        rng = np.random.default_rng(k)
+        x = rand(rng, (700, k), dt, 1.5, 0.5)
+        weights, norm = pkg.RowWeights(ctx, rand(rng, (k, 200), "f32")), pkg.RowNorm(kind, rand(rng, k, dt), rand(rng, k, dt))
+        whole = weights.linear(x, pre=norm)
+        q, qs = ctx.rows_quantize(x, pre=norm)
+        assert torch.equal(whole, weights.matmul(q, qs, dtype=TYPES[dt][0])), k
+        for r in (1, 2, 4, 40):
+            assert torch.equal(weights.linear(x[:r], pre=norm), whole[:r]), (k, r)
+
+
+@pytest.mark.parametrize("c", [1000, 2100, 4096])
+def test_a_list_with_the_room_of_the_map_has_the_bits_of_the_map(ctx, c):  # noqa: F811
+    """Long rows too: a list of the map's room takes the kernels that the map takes, or others with the same bits."""
+    rng = np.random.default_rng(c)
+    for px, m in ((4, 3), (60, 30), (900, 100)):
+        x, h = rand(rng, (px, c), "f16"), rand(rng, (px, c), "f16")
+        norm = pkg.RowNorm("layer", rand(rng, c, "f16"), rand(rng, c, "f16"))
+        weights = pkg.RowWeights(ctx, rand(rng, (c, 300), "f16"))
+        idx = torch.from_numpy(rng.permutation(px).astype(np.int32)).cuda()
+        count = torch.tensor([m], dtype=torch.int32, device="cuda")
+        at = idx[:m].long()
+        assert torch.equal(weights.linear(x, pre=norm, idx=idx, count=count)[:m], weights.linear(x, pre=norm)[at])
+        listed = ctx.rows_norm(x, h[idx.long()].contiguous(), post=norm, pre=norm, idx=idx, count=count, y=x.clone(), z=True)
+        whole = ctx.rows_norm(x, h, post=norm, pre=norm, y=True, z=True)
+        assert torch.equal(listed[0][at], whole[0][at]) and torch.equal(listed[1][:m], whole[1][at])
