@@ -351,9 +351,9 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
             __builtin_amdgcn_sched_barrier(0);
         }
         if (kt + 1 >= arrived) {                               // K-tile kt + 1: those behind it may be on their way
-            const int behind = may_be_in_flight(kt, kts, NB, ahead < range.end);
-            if (behind == NB - 2) wait_loads<(NB - 2) * (QL + WL)>();
-            else wait_but(behind);
+            static_assert(NB == 2 || NB == 3, "none or one");
+            if (may_be_in_flight(kt, kts, NB, ahead < range.end) == NB - 2) wait_loads<(NB - 2) * (QL + WL)>();
+            else wait_loads<0>();
         }
         meet();
         operands(next, kt + 1 < kts ? kt + 1 : kt, 0);         // (behind a tile's last K-tile: anything, nobody uses it)

@@ -20,8 +20,9 @@ constexpr bool turns_to_next(int kt, int kts, int nb) { return kt + nb == kts ||
 // Copied K-tiles that may still be on their way in a workgroup's first tile when K-tile kt + 1 has to be there (in later tiles: from
 // kt + 1 = nb on, those before have been waited for): the ones issued behind it.  A tile of fewer than nb K-tiles has fewer on their way.
 constexpr int may_be_in_flight(int kt, int kts, int nb, bool more) {
-    const int behind = more ? (kts < nb ? kts : nb) - 2 : kts - 2 - kt;
-    return behind <= 0 ? 0 : (behind < nb - 2 ? behind : nb - 2);          // (never more than nb - 2: said for the compiler)
+    if (nb == 2) return 0;
+    const int behind = more && kts >= nb ? nb - 2 : kts - 2 - kt;          // (a tile of fewer than nb: the first wait is at kt = 0, later ones need less)
+    return behind > 0 ? behind : 0;
 }
 
 }  // namespace dcnn
