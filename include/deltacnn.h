@@ -283,11 +283,14 @@ dcnn_status dcnn_net_stats(dcnn_net* net, dcnn_stats* stats_host);
  * the size of a call), so each operator takes a list as layers hand it out:
  *   idx_dev    NULL: row r of the operator is row r of the maps.  Else entry r names the map row (dcnn_delta.idx).
  *              An entry outside 0 .. map_rows-1 is a row without a token: nothing of a map is read or written for it,
- *              its compact outputs are zero.  Entries that are written through (y) must be distinct.
+ *              its compact outputs are those of a row of zeros behind the norm (z and q zero, a product act(bias)).
+ *              Entries that are written through (y) must be distinct.
  *   count_dev  NULL: `rows` rows.  Else the number of rows is min(*count_dev, rows), read on the GPU.
  * Maps (x, y) are addressed through idx, compact matrices (h, z, q, outputs of products) by r; compact rows at and
  * beyond the number of rows are neither read nor written.  Leading dimensions (ld*) count elements; rows of maps and
- * matrices need no alignment beyond their element's, except 8-bit rows (below).  Arithmetic is fp32 (products: exact
+ * matrices need no alignment beyond their element's, except 8-bit rows (below).  An output that shares a byte with an
+ * input or another output is refused (of whole maps, listed rows or not; matrices may lie in the gaps between each
+ * other's rows).  Arithmetic is fp32 (products: exact
  * 32-bit integers), with one rounding to the storage type at each store.  No call needs a workspace of the context. */
 typedef struct {
     int64_t        rows;        /* rows at most (0: nothing is launched)             */
@@ -311,8 +314,8 @@ typedef struct {
  * x NULL: 0; h NULL: y is x (and y_dev must be NULL); gate NULL: 1.  z is formed from y before y is rounded.
  * q / q_scale: z in 8 bits, q[r] = round_half_even(z[r] * (127 / max|z[r]|)) with q_scale[r] = max|z[r]| / 127.  A row
  * whose largest magnitude is below 1e-36 becomes zeros with scale 0, a row that holds a NaN or an infinity zeros with
- * scale NaN (products of it are NaN).  At least one of y, z, q is wanted; y_dev may equal x_dev (in place, ldy = ldx), outputs
- * overlap nothing else.  c <= 32768. */
+ * scale NaN (products of it are NaN).  At least one of y, z, q is wanted; y_dev may equal x_dev (in place, ldy = ldx).
+ * c <= 32768. */
 typedef struct {
     dcnn_row_list list;
     int32_t       dtype;        /* of x, h, gate, y, z and the norms' w and b: F32, F16, BF16 */
@@ -353,7 +356,7 @@ typedef struct {
     int64_t       k, n;
     const void*   packed_dev;   /* of dcnn_rows_pack with the same k and n              */
     const void*   bias_dev;     /* [n] or NULL                                         */
-    void*         y_dev;        /* [rows, n] compact; overlaps no input                */
+    void*         y_dev;        /* [rows, n] compact                                   */
     int64_t       ldy;
     const int8_t* q_dev;        /* matmul: [rows, k], aligned and spaced as in dcnn_rows_norm_args (the bytes behind k may hold anything; up to a
                                  * multiple of 16 they are read) */

@@ -2,7 +2,12 @@
 
 A block takes every pixel by itself -- norm, expansion, activation, projection, norm, gated residual -- so run on the
 flagged pixels alone it gives what it would give on the whole map: the list and the count that a layer leaves with an
-update are all it needs, and they never travel to the host.  Its products run in 8-bit integers.
+update are all it needs, and they never travel to the host.  (Bit for bit where the list has room for the map, as those
+of layers have, or the channels of a row are at most 64 vectors of 16 bytes; a list of one to four longer rows is normed
+by another kernel, whose sums are in another order.)  Its products run in 8-bit integers.
+
+Between its two products a block holds the hidden rows of as many pixels as the list has room for, and each of its two
+weights the 8-bit rows of as many.
 """
 from __future__ import annotations
 
@@ -36,7 +41,10 @@ class RowBlock:
 
 
 class TokenStack:
-    """Blocks one behind the other on an accumulated map, with the tokens of every block kept from frame to frame."""
+    """Blocks one behind the other on an accumulated map, with the tokens of every block kept from frame to frame.
+
+    init and step return the last block's tokens themselves, not a copy: the next step writes into them, and a caller that
+    changes them changes what later frames start from."""
 
     def __init__(self, blocks: list[RowBlock]):
         self.blocks, self.maps = blocks, None

@@ -71,8 +71,10 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 // and the tokens their columns: a lane ends with four consecutive channels of one token.
 //
 // K-tiles go from memory straight into one of NB LDS buffers, NB - 1 K-tiles ahead of their use, the first ones of the workgroup's next
-// tile behind the last ones of this; the operands of a step of 32 k are read from LDS one step ahead, the first ones of the next K-tile
-// behind the one barrier, which stands a step before the tile's end.  So the matrix cores wait neither for memory nor for LDS.
+// tile behind the last ones of this (which and when: tile_schedule.h); the operands of a step of 32 k are read from LDS one step ahead, the
+// first ones of the next K-tile behind the one barrier, which stands a step before the tile's end.  So the matrix cores wait for memory and
+// LDS only where a K-tile takes longer to come than to multiply: with two buffers a K-tile has the time of one on its way.  Three buffers
+// give it the time of two, but at every third K-tile, where the first buffer is read, the compiler waits for all copies.
 // Weights lie in LDS as they are packed (an operand load of a wave is 1 KB in a row).  A row's eight chunks of 16 k are exchanged by bits
 // of its number: the 16 lanes of a quarter of an operand load, 16 rows at one k, then cover all 64 banks.
 //
@@ -81,12 +83,12 @@ dcnn_status launch_rows_pack(dcnn_ctx* ctx, int dtype, int64_t k, int64_t n, con
 // 8.4 -> 6.9; 4096 -> 4096 the same, or 4 % at 60000 rows).  An output costs three and a half instructions and an activation two more: that,
 // and not the matrix cores, is what a short k waits for.
 //
-// 16384 x 4096 -> 4096 in bf16: 244-250 us, 2.2 POP/s; 8192 x 8192 -> 4096: 230, 2.4 (a library's 8-bit product that leaves its 32-bit sums:
-// 248 and 226).  Power bounds these: the same product of zeros takes 183 us in place of 230; the clock is at 1.8 GHz, and the matrix cores are
-// busy 60 % of its cycles.  Per tile of 256 x 256 about 5 us of 60 are the outputs'.  What it took, us for
-// the first of them: one K-tile staged through registers behind a barrier 328; loads two K-tiles and operands a step ahead 295; copies
-// straight into LDS 272; scales and bias by one load each, dealt out in LDS, and no wait for stores 250.  26214 x 256 -> 1024 in fp16 is bound
-// by its outputs: 17.1 us, 3.9 TB/s behind the launch.
+// 16384 x 4096 -> 4096 in bf16: 237-247 us in a row (the same matrices again, or others from memory), 2.2-2.3 POP/s; 8192 x 8192 -> 4096:
+// 225-245, 2.2-2.4 (a library's 8-bit product that leaves its 32-bit sums: 248 and 226).  Power bounds these: the same product of zeros takes
+// 183 us in place of 230; the clock is at 1.8 GHz, and the matrix cores are busy 60 % of its cycles.  Per tile of 256 x 256 about 5 us of 60
+// are the outputs'.  What it took, us for the first of them: one K-tile staged through registers behind a barrier 328; loads two K-tiles and
+// operands a step ahead 295; copies straight into LDS 272; scales and bias by one load each, dealt out in LDS, and no wait for stores 250.
+// 26214 x 256 -> 1024 in fp16 is bound by its outputs: 17-18 us in a row where the rows are in the caches, 25 where all comes from memory.
 constexpr int kChunks = kPackK / 16, kSteps = kPackK / 32;
 constexpr int kPlanCus = 256;                  // compute units of an MI355X: what a plan counts on
 constexpr int kPanelTiles = 2;                 // K-tiles of rows that a workgroup makes for itself and keeps
@@ -244,7 +246,8 @@ __global__ __launch_bounds__(TW * CW * kWave, 2) void rows_matmul_kernel(MatmulA
     constexpr int QL = S::copied / 8 / S::waves, WL = S::channels / 8 / S::waves;        // copies of 1 KB per K-tile and wave
     static_assert(S::threads >= S::channels && S::threads >= S::tokens && (2 * S::channels + S::tokens) * 4 <= S::waves * S::unit, "a thread for each factor");
     static_assert(QL * 8 * S::waves == S::copied && WL * 8 * S::waves == S::channels, "whole rounds of copies");
-    // (an array each: what is read from one buffer does not wait for copies into the others)
+    // (an array each: what is read from the second and third does not wait for copies into the others; of the first the compiler is not so
+    // sure, and waits for every copy before it is read)
     __shared__ __align__(1024) int8_t buf0[S::stage], buf1[S::stage], buf2[NB > 2 ? S::stage : 16], out_lds[S::waves * S::unit];
     static_assert(NB == 2 || NB == 3, "an array for each buffer");
     auto buffer = [&](auto i) -> int8_t* {
@@ -527,8 +530,8 @@ static dcnn_status launch_tile(dcnn_ctx* ctx, const MatmulArgs& a, int splits = 
 // NORM > 0: up to NORM tokens are normed and quantised on the spot, by every workgroup for itself (a row is 8 KB that the caches hold, a
 // launch of its own takes longer), while the first weights are on their way.
 //
-// Bound by the weights' bytes and the launch (3.2 us): 1 x 4096 -> 4096 5.8 us in a row (6.5 TB/s behind the launch), 16 rows 7.0, 32 rows
-// 9.1 (their 8-bit rows from L2, as many bytes as the weights); 1 x 8192 -> 1024 5.5.
+// Bound by the weights' bytes and the launch (3.2 us): 1 x 4096 -> 4096 6.2 us in a row with weights from memory (3.7 where the caches hold
+// them), 16 rows 7.4, 32 rows 9.1 to 10.9 (their 8-bit rows from L2 or memory, as many bytes as the weights); 1 x 8192 -> 1024 5.5 to 7.0.
 constexpr int kFewWaves = 8, kAhead = 8;
 template <int G, int F> struct FewShape {
     static constexpr int sums = kFewWaves * G * F * kWave * 16;
@@ -706,7 +709,7 @@ dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& n
 }
 
 // ---- which kernel ------------------------------------------------------------------------------------------------------
-// us, in a row on the GPU, weights from memory (rows, k -> n); a launch alone is 3.2:
+// us, in a row on the GPU, weights from memory, rows that the caches hold (rows, k -> n); a launch alone is 3.2:
 //   17 to 32 rows: few / tiles of 64   24, 4096 -> 4096: 8.9 / 11.1   24, 1024 -> 256: 4.6 / 5.1   32, 8192 -> 1024: 11.3 / 10.9   32, 16384 -> 512: 19.5 / 12.5
 //   tiles of 64 / 128 deep / 128 / 256   500, 4096 -> 4096 (128 tiles of 128): 20 / 23 / 32 / 50   1000, 4096 -> 4096 (256): 35 / 25 / 33 / 50
 //                                        2000, 4096 -> 4096 (512): 67 / 46 / 40 / 50   4000, 4096 -> 4096 (1024; 256 of 256): 128 / 94 / 78 / 63
@@ -716,11 +719,14 @@ dcnn_status launch_rows_linear_fused(dcnn_ctx* ctx, int dtype, const NormArgs& n
 //   pairs of 128 / 256                   26214, 256 -> 1024: 17.9 / 19.4   16384, 512 -> 2048: 29.5 / 27.5   16384, 1000 -> 1531: 43 / 53   8000, 4096 -> 4096: 150 / 132
 //   k of a tile of 64 in one / in parts  64, 8192 -> 1024: 22 / 10.9 (8)   64, 4096 -> 4096: 17 / 11.0 (4)   200, 8192 -> 1024: 22 / 12.5 (4), 14.4 (8)
 //                                        500, 8192 -> 1024: 24 / 18.2 (2), 16.4 (4)   64, 1024 -> 256: 5.1 / 6.7 (2)
+// A list's length is on the GPU: its plan is that of a quarter of its room, a guess that was measured only afterwards.  Product behind a count
+// of 3, 10, 30 and 100 % of the room / of as many rows without one, the same matrices again:
+//   262144, 256 -> 1024: 7.0 / 7.0, 19.8 / 17.7, 49 / 47, 156 / 152      65536, 512 -> 512: 6.0 / 4.4, 6.6 / 6.4, 11.5 / 11.5, 32 / 29
+//   16384, 1024 -> 4096: 15.6 / 6.6, 16.4 / 11.8, 34 / 28, 80 / 78       16384, 256 -> 1024: 4.8 / 3.6, 5.1 / 4.3, 7.7 / 6.1, 14.1 / 10.9
 MatmulPlan matmul_plan(int64_t rows, int64_t k, int64_t n, bool counted) {
     MatmulPlan p{kFewRows, 1, 0};
     const int64_t kt = packed_k(k) / kPackK;
     if (rows <= 16 || (rows <= 32 && kt < 64)) return p;
-    // a list's length is on the GPU; its room is that of the whole map, and few maps are flagged all over
     const int64_t likely = counted ? cdiv(rows, 4) : rows;
     const int64_t tiles64 = cdiv(rows, 64) * cdiv(n, 64), tiles128 = cdiv(likely, 128) * cdiv(n, 128), tiles256 = cdiv(likely, 256) * cdiv(n, 256);
     if (tiles128 <= kPlanCus / 2) {

@@ -5,16 +5,18 @@
 // One pass: a row of c channels lives in the registers of its L lanes (8 to 64 lanes of a wave, or a workgroup of 256 to 1024), NV vectors
 // of 16 bytes to a lane, so its mean, its variance (from the centred values, not from a difference of squares) and its largest magnitude
 // are reductions over registers and nothing is read twice.  Few vectors and many lanes: with four vectors to a lane (what y needs, what
-// the parameters hold) registers left one wave to a SIMD, 8192 rows of 8192 in 8 bits took 116 us in place of 48.
+// the parameters hold) registers left one wave to a SIMD, 8192 rows of 8192 in 8 bits took 116 us in place of 40.
 // fp32 all through; y, z and q are rounded once each, z and q from the unrounded y.
 // y and z are stored past the L2 (non-temporal; see row_store): 5 to 20 % of the time.  x and h are not read so: 5 to 15 % more.
 //
 // Bound by HBM, 2 * c elements read and up to 2 * c written a row, and by the launch (3 us) below some 10 MB:
-//   16384 x 4096 bf16, both norms, gate, y and z     104 us, inputs from memory (5.2 TB/s; a copy of 2 GB: 4.94); 90 on the same rows again
-//   16384 x 1024 bf16                                28           4.8
-//   26214 of 262144 x 256 fp16 by a list             12           4.4    20000 x 500 fp16 19, x 512 19 (rows at odd addresses cost little)
-//   4099 x 1037 fp32                                 17           4.0    1 x 2048 fp16 4.7 us
-//   8192 x 8192 fp16 to 8 bits                       48           4.2    26214 x 256 by a list 9.4
+// (us in a row on the GPU: all matrices from memory / the same ones again, which the caches hold in part; a copy of 2 GB: 4.94 TB/s)
+//   16384 x 4096 bf16, both norms, gate, y and z     104 (5.2 TB/s) / 90
+//   16384 x 1024 bf16                                31  (4.4) / 25
+//   26214 of 262144 x 256 fp16 by a list             13  (4.1)
+//   4099 x 1037 fp32                                 22  (3.0) / 18     20000 x 500 fp16 19, x 512 19 (rows at odd addresses cost little)
+//   8192 x 8192 fp16 to 8 bits                       40  (5.0) / 33     26214 x 256 by a list 9.6
+//   1 x 2048 fp16                                    3.7
 #include "rows_device.h"
 
 namespace dcnn {
@@ -23,7 +25,7 @@ template <typename T, int L> struct NormShape {
     static constexpr int threads = L > 256 ? L : 256, rows = threads / L;
 };
 
-// BLOCK: there is an h.  (Without one six waves fit a SIMD: 8192 rows of 8192 in 8 bits 48 us, with five of them 62.)  HOLD: a lane's part of the parameters stays in registers from row to row.
+// BLOCK: there is an h.  (Without one six waves fit a SIMD; with five of them 8192 rows of 8192 in 8 bits took 30 % longer.)  HOLD: a lane's part of the parameters stays in registers from row to row.
 template <typename T, int L, int NV, bool BLOCK>
 __global__ __launch_bounds__((NormShape<T, L>::threads), !BLOCK && NV <= 2 ? 6 : 4) void rows_norm_kernel(NormArgs a) {
     constexpr int E = RowVec<T>::E, R = NormShape<T, L>::rows;
