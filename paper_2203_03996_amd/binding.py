@@ -186,7 +186,10 @@ class Delta:
 
 
 class Context:
-    """dcnn_ctx on torch's current stream, with a torch-allocated workspace."""
+    """dcnn_ctx on torch's current stream, with a torch-allocated workspace.
+
+    All calls run on that stream, whichever torch is on later: tensors made on another one are the caller's to wait for.  Calls
+    on one context follow each other (one thread at a time), with its GPU as torch's current one."""
 
     def __init__(self, max_pixels: int, device="cuda"):
         """max_pixels = 0 creates the context without a workspace (enough for mask_compact_static)."""
