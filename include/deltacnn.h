@@ -372,6 +372,118 @@ size_t      dcnn_rows_scratch_bytes(int64_t rows, int64_t k, int64_t n, int32_t 
 dcnn_status dcnn_rows_matmul(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
 dcnn_status dcnn_rows_linear(dcnn_ctx* ctx, const dcnn_rows_matmul_args* args);
 
+/* ---- tokens: heads, a cache in 4 bits, attention over it ------------------------------------------- */
+/* What mixes tokens.  A stream is a sequence of tokens: the pixels of one map of a batch, or a text.  A call works on rows
+ * as the row operators do (a list of map rows, or all of them), and each row is a token with a stream and a position:
+ *   i        = list.idx_dev ? idx[r] : r                  (an entry outside 0 .. map_rows-1 is a row without a token)
+ *   stream   = stream_dev ? stream[i] : i / period
+ *   position = pos_dev ? pos[i] : i % period
+ * Maps of `period` pixels, one to a stream, need neither array; one token for each stream (period 1) positions alone.
+ * Matrices of heads ([rows, heads * dim], the values of a head side by side) are compact: addressed by r. */
+typedef struct {
+    dcnn_row_list  list;
+    int64_t        period;      /* tokens of a stream in the maps; read where an array is NULL (1 at least) */
+    const int32_t* stream_dev;  /* [map_rows] or NULL */
+    const int32_t* pos_dev;     /* [map_rows] or NULL */
+} dcnn_row_tokens;
+
+/* Rotation by position: pair j < rot / 2 of a head, (a, b), becomes (a cos - b sin, b cos + a sin) with the cosine and sine
+ * of table[position][j].  The pairs are (j, j + rot/2), or neighbours (2j, 2j+1); the values from rot on stay as they are. */
+typedef enum { DCNN_ROT_HALVES = 0, DCNN_ROT_PAIRS = 1 } dcnn_rot_style;
+typedef struct {
+    const float* table_dev;     /* [positions][rot / 2][2], NULL: no rotation            */
+    int64_t      positions;     /* a row with a position outside of it has no token       */
+    int32_t      rot;           /* multiple of 16, dim at most                           */
+    int32_t      style;         /* dcnn_rot_style                                        */
+} dcnn_rotation;
+
+/* Queries and keys, each head normed by itself (w and b of a norm: [dim]) and rotated by its row's position, in one pass:
+ * out[r][h] = rotate(norm(in[r][h])).  Arithmetic is fp32 with one rounding at the store.  Rows without a token become
+ * zeros.  k_heads 0: queries alone (k may be NULL).  An output may be its input (same leading dimension).
+ * dim: 32, 64, 96, 128, 192 or 256; rows * (q_heads + k_heads) at most 2^31 - 1. */
+typedef struct {
+    dcnn_row_tokens tokens;     /* (streams are not looked at; positions are, where there is a rotation) */
+    int32_t         dtype;      /* of q, k, their outputs and the norms' w and b: F32, F16, BF16 */
+    int32_t         dim;
+    int32_t         q_heads, k_heads;
+    const void     *q_dev, *k_dev;
+    void           *q_out_dev, *k_out_dev;
+    int64_t         ldq, ldk, ldq_out, ldk_out;
+    dcnn_row_norm   q_norm, k_norm;
+    dcnn_rotation   rotation;
+} dcnn_rows_heads_args;
+dcnn_status dcnn_rows_heads(dcnn_ctx* ctx, const dcnn_rows_heads_args* args);
+
+/* A paged cache of keys and values in 4 bits, memory of the caller's.  Each 32 values of a head are 4-bit floating-point
+ * codes -- a sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 -- and one power of two that they are
+ * multiplied with: a byte, the exponent with a bias of 127 (255: the values are NaN).
+ *   codes   [num_pages][2: keys, values][heads][page][dim / 2], the value of an even place in the low half of its byte
+ *   scales  [num_pages][2][heads][page][dim / 32]
+ * Token p of stream s lies in slot p % page of page pages[s][p / page].  A page whose number is outside 0 .. num_pages-1 is
+ * none: nothing is written there, and its tokens do not count. */
+typedef struct {
+    int32_t        dtype;       /* of q, k, v and outputs: F32, F16, BF16                 */
+    int32_t        heads;       /* of keys and values                                    */
+    int32_t        dim;         /* 32, 64, 96, 128, 192 or 256                           */
+    int32_t        page;        /* tokens of a page: a power of two, 16 to 4096           */
+    int64_t        streams;
+    int64_t        length;      /* tokens of a stream at most (2^30 at most)              */
+    int64_t        num_pages;
+    uint8_t       *codes_dev, *scales_dev;   /* 16-byte aligned                          */
+    const int32_t* pages_dev;   /* [streams][ceil(length / page)], or NULL: page j of stream s is s * ceil(length / page) + j */
+} dcnn_cache;
+
+/* Writes the keys (normed and rotated first) and values of rows into the cache.  The scale of 32 values is the smallest
+ * power of two with max|v| <= 6 * scale (2^-126 at least), and each becomes the code next to v / scale, ties to the even
+ * one (a zero keeps its sign); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
+ * order of a sum.  Rows without a token, or with a position outside 0 .. length-1, write nothing.  The (stream, position)
+ * of rows must be distinct.  rows * heads at most 2^30. */
+typedef struct {
+    dcnn_cache      cache;
+    dcnn_row_tokens tokens;
+    const void     *k_dev, *v_dev;
+    int64_t         ldk, ldv;
+    dcnn_row_norm   k_norm;
+    dcnn_rotation   rotation;   /* of the keys */
+} dcnn_cache_append_args;
+dcnn_status dcnn_cache_append(dcnn_ctx* ctx, const dcnn_cache_append_args* args);
+
+/* What the cache holds for the tokens of rows, as numbers of its dtype (fp16: a held magnitude of 65536 or more is infinite);
+ * zeros for a row without a token.  Either output may be NULL. */
+typedef struct {
+    dcnn_cache      cache;
+    dcnn_row_tokens tokens;
+    void           *k_out_dev, *v_out_dev;
+    int64_t         ldk, ldv;
+} dcnn_cache_read_args;
+dcnn_status dcnn_cache_read(dcnn_ctx* ctx, const dcnn_cache_read_args* args);
+
+/* Attention of rows of queries over the cache of their stream:
+ *   y[r][h] = sum_t softmax_t(scale * q[r][h] . k[t][h / (q_heads / heads)]) v[t][h / (q_heads / heads)]
+ * over the tokens t of the row's stream with t < len (lens_dev[stream], cut to 0 .. length; NULL: length), t <= position if
+ * `causal`, and |position - t| < window if window > 0.  Rows that see no token, or have none, become zeros.  Queries and
+ * keys meet exactly, sums and the softmax's statistics are fp32; the weights of a row, relative to the largest, are rounded
+ * to the dtype before they meet the values (F32: kept), and the result once more.  F16 holds keys and values rounded to
+ * fp16 (see dcnn_cache_read).
+ * scratch_dev: dcnn_cache_scratch_bytes(...) bytes of the cache's and the call's sizes, 256-byte aligned, whatever it holds;
+ * calls may share it one after the other.  rows * q_heads at most 2^30. */
+typedef struct {
+    dcnn_cache      cache;
+    dcnn_row_tokens tokens;
+    const void*     q_dev;      /* [rows, q_heads * dim]                                 */
+    void*           y_dev;      /* [rows, q_heads * dim]                                 */
+    int64_t         ldq, ldy;
+    int32_t         q_heads;    /* a multiple of cache.heads                             */
+    float           scale;
+    int32_t         causal;
+    int64_t         window;     /* 0: none                                               */
+    const int32_t*  lens_dev;   /* [streams] or NULL                                     */
+    void*           scratch_dev;
+    size_t          scratch_bytes;
+} dcnn_cache_attend_args;
+size_t      dcnn_cache_scratch_bytes(int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length);
+dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* args);
+
 #ifdef __cplusplus
 }
 #endif

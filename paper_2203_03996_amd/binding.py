@@ -25,6 +25,7 @@ ACT_CODES = {"none": ACT_NONE, None: ACT_NONE, "relu": ACT_RELU, "relu6": ACT_RE
 TORCH_DTYPE = {F32: torch.float32, F16: torch.float16}
 ROW_DTYPE_CODE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 NORM_CODES = {"none": 0, None: 0, "rms": 1, "layer": 2}
+ROT_CODES = {"halves": 0, "pairs": 1}
 DTYPE_CODE = {"f32": F32, "f16": F16}
 STATUS_NAMES = ["OK", "EINVAL", "ESHAPE", "EDTYPE", "ESTATE", "ENOMEM", "EHIP", "EUNSUPPORTED"]
 
@@ -36,7 +37,7 @@ EXPORTS = [
     "dcnn_net_bind", "dcnn_net_init", "dcnn_net_step", "dcnn_net_reset", "dcnn_net_output",
     "dcnn_net_num_layers", "dcnn_net_layer", "dcnn_net_stats",
     "dcnn_rows_norm", "dcnn_rows_weights_bytes", "dcnn_rows_pack", "dcnn_rows_scratch_bytes", "dcnn_rows_matmul",
-    "dcnn_rows_linear",
+    "dcnn_rows_linear", "dcnn_rows_heads", "dcnn_cache_append", "dcnn_cache_read", "dcnn_cache_scratch_bytes", "dcnn_cache_attend",
 ]
 
 
@@ -93,6 +94,33 @@ class RowsMatmulArgs(C.Structure):
         ("bias", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("q", C.c_void_p), ("q_scale", C.c_void_p),
         ("ldq", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64)] + _row_norm("pre") + [
         ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
+_TOKENS = _ROW_LIST + [("period", C.c_int64), ("stream", C.c_void_p), ("pos", C.c_void_p)]
+_ROTATION = [("table", C.c_void_p), ("positions", C.c_int64), ("rot", C.c_int32), ("style", C.c_int32)]
+_CACHE = [("dtype", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("page", C.c_int32), ("streams", C.c_int64), ("length", C.c_int64),
+          ("num_pages", C.c_int64), ("codes", C.c_void_p), ("scales", C.c_void_p), ("pages", C.c_void_p)]
+
+
+class RowsHeadsArgs(C.Structure):
+    _fields_ = _TOKENS + [
+        ("dtype", C.c_int32), ("dim", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("q", C.c_void_p), ("k", C.c_void_p),
+        ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldq_out", C.c_int64),
+        ("ldk_out", C.c_int64)] + _row_norm("q_norm") + _row_norm("k_norm") + _ROTATION
+
+
+class CacheAppendArgs(C.Structure):
+    _fields_ = _CACHE + _TOKENS + [("k", C.c_void_p), ("v", C.c_void_p), ("ldk", C.c_int64), ("ldv", C.c_int64)] + _row_norm("k_norm") + _ROTATION
+
+
+class CacheReadArgs(C.Structure):
+    _fields_ = _CACHE + _TOKENS + [("k_out", C.c_void_p), ("v_out", C.c_void_p), ("ldk", C.c_int64), ("ldv", C.c_int64)]
+
+
+class CacheAttendArgs(C.Structure):
+    _fields_ = _CACHE + _TOKENS + [
+        ("q", C.c_void_p), ("y", C.c_void_p), ("ldq", C.c_int64), ("ldy", C.c_int64), ("q_heads", C.c_int32), ("scale", C.c_float),
+        ("causal", C.c_int32), ("_pad", C.c_int32), ("window", C.c_int64), ("lens", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
 
 
 class DcnnError(RuntimeError):
@@ -163,6 +191,12 @@ def load_library() -> C.CDLL:
     lib.dcnn_rows_scratch_bytes.restype = sz
     lib.dcnn_rows_matmul.argtypes = [vp, P(RowsMatmulArgs)]
     lib.dcnn_rows_linear.argtypes = [vp, P(RowsMatmulArgs)]
+    lib.dcnn_rows_heads.argtypes = [vp, P(RowsHeadsArgs)]
+    lib.dcnn_cache_append.argtypes = [vp, P(CacheAppendArgs)]
+    lib.dcnn_cache_read.argtypes = [vp, P(CacheReadArgs)]
+    lib.dcnn_cache_scratch_bytes.argtypes = [C.c_int64, i32, i32, i32, C.c_int64, C.c_int64]
+    lib.dcnn_cache_scratch_bytes.restype = sz
+    lib.dcnn_cache_attend.argtypes = [vp, P(CacheAttendArgs)]
     _lib = lib
     return lib
 
@@ -337,6 +371,42 @@ class Context:
         if st:
             self.check(st)
         return y, z, q, q_scale
+
+    def rows_heads(self, q, k=None, *, dim, q_norm=None, k_norm=None, rotation=None, positions=None, idx=None, count=None, q_out=None, k_out=None):
+        """dcnn_rows_heads: queries q [rows, heads * dim] and keys k, each head normed by itself and rotated by the row's position.
+
+        A row's token is map row i = idx[r] (r without a list); its position is positions[i], or i counted round and round the
+        rotation's table (maps of as many pixels).  q_norm, k_norm: RowNorm over `dim` values, or None; rotation: Rotation or
+        None.  q_out, k_out: a matrix to write (q and k themselves: in place), or None for a new one.  Without a count every row
+        that idx names is wanted; with one the smallest matrix is the room of the call.  Returns (q_out, k_out), or q_out alone
+        without keys."""
+        a, dt, dev = RowsHeadsArgs(), q.dtype, self.index
+        a.dtype, a.dim = _row_dtype(dt), dim
+        a.q, a.ldq, rows, a.q_heads = _as_heads(q, "q", dim, dt, dev)
+        if idx is None and positions is not None:
+            _whole(positions, rows, "positions", "q")
+        rows = _set_tokens(a, rows, rows, None, positions, rotation.positions if rotation is not None else 1, idx, count, dev)
+        if k is not None:
+            a.k, a.ldk, n, a.k_heads = _as_heads(k, "k", dim, dt, dev)
+            rows = _room(rows, n, "k", count)
+        q_out = self.empty((rows, a.q_heads * dim), dt) if q_out is None else q_out
+        a.q_out, a.ldq_out, n = _as_rows(q_out, "q_out", a.q_heads * dim, dt, dev)
+        rows = _room(rows, n, "q_out", count)
+        if k is not None:
+            k_out = self.empty((rows, a.k_heads * dim), dt) if k_out is None else k_out
+            a.k_out, a.ldk_out, n = _as_rows(k_out, "k_out", a.k_heads * dim, dt, dev)
+            rows = _room(rows, n, "k_out", count)
+        if q_norm is not None:
+            a.q_norm_kind, a.q_norm_eps, a.q_norm_w, a.q_norm_b = q_norm.pointers(dim, dt, dev)
+        if k_norm is not None:
+            a.k_norm_kind, a.k_norm_eps, a.k_norm_w, a.k_norm_b = k_norm.pointers(dim, dt, dev)
+        if rotation is not None:
+            a.table, a.positions, a.rot, a.style = rotation.pointers(dev)
+        a.rows = rows
+        st = self.lib.dcnn_rows_heads(self.handle, a)
+        if st:
+            self.check(st)
+        return q_out if k is None else (q_out, k_out)
 
     def rows_quantize(self, x, *, pre=None, idx=None, count=None):
         """Rows of x (normed with `pre`, or as they are) in 8 bits: (q [rows, c], q_scale [rows])."""
@@ -616,6 +686,204 @@ class RowWeights:
         if pre is not None:
             a.pre_kind, a.pre_eps, a.pre_w, a.pre_b = pre.pointers(self.k, dt, dev)
         return self._call(self.ctx.lib.dcnn_rows_linear, 1, a, rows, dt, count, out)
+
+
+def _as_heads(t, name, dim, dt, dev):
+    """(address, leading dimension, rows, heads) of a matrix of heads of `dim` values."""
+    if t.dim() != 2 or t.shape[1] == 0 or t.shape[1] % dim:
+        raise ValueError(f"{name} must be a matrix [rows, heads * {dim}], got {tuple(t.shape)}")
+    return *_as_rows(t, name, t.shape[1], dt, dev), t.shape[1] // dim
+
+
+def _whole(t, rows, name, of):
+    if t.numel() < rows:
+        raise ValueError(f"{name} has {t.numel()} entries, {of} {rows} rows")
+
+
+def _set_tokens(a, n, map_rows, streams, positions, period, idx, count, dev):
+    """Fills in which tokens the rows of an n-row matrix are; returns the rows of the call so far."""
+    a.period, rows = period, n
+    if streams is not None:
+        a.stream, map_rows = _int32(streams, "streams", dev), streams.numel()
+    if positions is not None:
+        a.pos = _int32(positions, "positions", dev)
+        map_rows = positions.numel() if streams is None else min(map_rows, positions.numel())
+    if idx is not None:
+        a.idx, rows = _int32(idx, "idx", dev), idx.numel()
+        if streams is None and positions is None:
+            map_rows = _ROWS_MAX
+    if count is not None:
+        a.count = _int32(count, "count", dev)
+    a.map_rows = map_rows
+    return _room(rows, n, "a matrix of rows", count)
+
+
+class Rotation:
+    """Rotation of heads by position: `table` [positions, rot / 2, 2] float32, the cosine and sine of each pair's angle.
+
+    style "halves": pair j is the values j and j + rot / 2 of a head; "pairs": 2 j and 2 j + 1.  Values from rot on are left alone."""
+
+    def __init__(self, table: torch.Tensor, style: str = "halves"):
+        if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or table.shape[1] % 8 or not table.numel():
+            raise ValueError(f"a rotation's table must be contiguous float32 [positions, a multiple of 8, 2], got {tuple(table.shape)} {table.dtype}")
+        self.table, self.style, self.positions, self.rot = table, ROT_CODES[style], table.shape[0], 2 * table.shape[1]
+
+    @classmethod
+    def of_angles(cls, angles: torch.Tensor, style: str = "halves"):
+        """From angles [positions, rot / 2] (float64: those of far positions need it)."""
+        a = angles.double()
+        return cls(torch.stack([a.cos(), a.sin()], 2).float().contiguous(), style)
+
+    @classmethod
+    def of_positions(cls, positions: int, rot: int, base: float = 10000.0, style: str = "halves", device="cuda"):
+        """Pair j turns by position * base ^ (-2 j / rot)."""
+        p = torch.arange(positions, dtype=torch.float64, device=device)[:, None]
+        return cls.of_angles(p * base ** (-torch.arange(rot // 2, dtype=torch.float64, device=device) * 2 / rot), style)
+
+    @classmethod
+    def of_pixels(cls, h: int, w: int, rot: int, base: float = 100.0, style: str = "halves", device="cuda"):
+        """Pixels of an h x w map: the first half of the pairs turns by the row, the second by the column (rot a multiple of 16)."""
+        f = base ** (-torch.arange(rot // 4, dtype=torch.float64, device=device) * 4 / rot)
+        y, x = (torch.arange(n, dtype=torch.float64, device=device)[:, None] * f for n in (h, w))
+        return cls.of_angles(torch.cat([y[:, None].expand(h, w, -1), x[None].expand(h, w, -1)], 2).reshape(h * w, -1), style)
+
+    def pointers(self, dev):
+        if self.table.get_device() != dev:
+            raise ValueError(f"the rotation's table is on {self.table.device}, the call on GPU {dev}")
+        return self.table.data_ptr(), self.positions, self.rot, self.style
+
+
+class TokenCache:
+    """Keys and values of the tokens of `streams` streams, up to `length` each, in 4 bits (dcnn_cache), and attention over them.
+
+    heads, dim: of keys and values; dtype: of queries, keys, values and outputs.  page: tokens of a page.  pages: int32
+    [streams, ceil(length / page)], the number of each page, read at every call (the caller may hand pages out anew), or
+    None where every stream has its own, one behind the other.  codes, scales: the memory (see dcnn_cache), or None for
+    new, zeroed memory of `num_pages` pages (as many as all streams need where it is not given).
+
+    Calls name tokens as rows: map row i = idx[r] (r without a list) is a token of streams[i] at positions[i].  Without both
+    the maps are pixels, `length` to a stream: stream i / length, position i % length; with positions alone row i is the
+    token of stream i.  Matrices are compact; without a count every row that idx names is wanted.
+
+    The object holds scratch that its attend calls share.  They follow each other on the context's stream, and threads take
+    turns.  Graphs hold the scratch too: two that were captured from one object must not run at the same time, and the object
+    has to outlive them."""
+
+    def __init__(self, ctx: Context, streams: int, length: int, heads: int, dim: int, *, dtype=torch.float16, page: int = 64, pages=None,
+                 num_pages: int | None = None, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None):
+        self.ctx, self.streams, self.length, self.heads, self.dim, self.page = ctx, streams, length, heads, dim, page
+        self.dtype, self._code = dtype, _row_dtype(dtype)
+        if min(streams, length, heads, dim) < 1 or page < 16 or page > 4096 or page & (page - 1) or dim % 32:
+            raise ValueError(f"a cache of {streams} streams of {length} tokens, {heads} heads of {dim}, pages of {page}")
+        per_stream = -(-length // page)
+        if (codes is None) != (scales is None):
+            raise ValueError("codes and scales come together")
+        if codes is None:
+            num_pages = streams * per_stream if num_pages is None else num_pages
+            with torch.cuda.stream(ctx.stream):
+                codes, scales = (torch.zeros((num_pages, 2, heads, page, n), dtype=torch.uint8, device=ctx._gpu) for n in (dim // 2, dim // 32))
+        elif num_pages is not None and num_pages != codes.shape[0]:
+            raise ValueError(f"{num_pages} pages, codes of {codes.shape[0]}")
+        self.num_pages = codes.shape[0]
+        for name, t, n in (("codes", codes, dim // 2), ("scales", scales, dim // 32)):
+            if t.shape != (self.num_pages, 2, heads, page, n) or t.dtype != torch.uint8 or not t.is_contiguous() or t.get_device() != ctx.index:
+                raise ValueError(f"{name} must be contiguous uint8 [pages, 2, {heads}, {page}, {n}] on GPU {ctx.index}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+        if pages is not None and (pages.shape != (streams, per_stream) or pages.dtype != torch.int32 or not pages.is_contiguous() or pages.get_device() != ctx.index):
+            raise ValueError(f"pages must be contiguous int32 [{streams}, {per_stream}] on GPU {ctx.index}, got {tuple(pages.shape)} {pages.dtype}")
+        if pages is None and self.num_pages < streams * per_stream:
+            raise ValueError(f"{self.num_pages} pages for {streams} streams of {per_stream}")
+        self.codes, self.scales, self.pages = codes, scales, pages
+        self._scratch, self._captured, self._one_call = None, set(), threading.Lock()
+
+    def _args(self, a, n, streams, positions, idx, count):
+        """Fills in the cache and the tokens of a call with an n-row matrix; returns its rows."""
+        dev = self.ctx.index
+        a.dtype, a.heads, a.dim, a.page = self._code, self.heads, self.dim, self.page
+        a.streams, a.length, a.num_pages = self.streams, self.length, self.num_pages
+        a.codes, a.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        if self.pages is not None:
+            a.pages = self.pages.data_ptr()
+        if streams is not None and positions is None:
+            raise ValueError("streams come with positions")
+        if idx is None:
+            for name, t in (("streams", streams), ("positions", positions)):
+                if t is not None:
+                    _whole(t, n, name, "a matrix of")
+        return _set_tokens(a, n, n, streams, positions, self.length if positions is None else 1, idx, count, dev)
+
+    def append(self, k, v, *, norm: RowNorm | None = None, rotation: Rotation | None = None, streams=None, positions=None, idx=None, count=None):
+        """dcnn_cache_append: keys k [rows, heads * dim] (normed and rotated on the way) and values v into their tokens' places,
+        which must be distinct."""
+        a, dev, c = CacheAppendArgs(), self.ctx.index, self.heads * self.dim
+        a.k, a.ldk, n = _as_rows(k, "k", c, self.dtype, dev)
+        rows = self._args(a, n, streams, positions, idx, count)
+        a.v, a.ldv, n = _as_rows(v, "v", c, self.dtype, dev)
+        a.rows = _room(rows, n, "v", count)
+        if norm is not None:
+            a.k_norm_kind, a.k_norm_eps, a.k_norm_w, a.k_norm_b = norm.pointers(self.dim, self.dtype, dev)
+        if rotation is not None:
+            a.table, a.positions, a.rot, a.style = rotation.pointers(dev)
+        st = self.ctx.lib.dcnn_cache_append(self.ctx.handle, a)
+        if st:
+            self.ctx.check(st)
+
+    def read(self, *, streams=None, positions=None, idx=None, count=None, rows: int | None = None):
+        """dcnn_cache_read: (keys, values) [rows, heads * dim] that the cache holds for tokens, zeros for those it has no place for.
+
+        The tokens are those that idx names, else as many as positions has, else the first `rows` of all (None: all)."""
+        if idx is not None:
+            n = idx.numel()
+        elif positions is not None:
+            n = positions.numel()
+        else:
+            n = self.streams * self.length if rows is None else rows
+        a, c = CacheReadArgs(), self.heads * self.dim
+        a.rows = self._args(a, n, streams, positions, idx, count)
+        k, v = (self.ctx.empty((n, c), self.dtype) for _ in range(2))
+        a.k_out, a.v_out, a.ldk, a.ldv = k.data_ptr(), v.data_ptr(), c, c
+        st = self.ctx.lib.dcnn_cache_read(self.ctx.handle, a)
+        if st:
+            self.ctx.check(st)
+        return k, v
+
+    def attend(self, q, *, lens=None, causal=False, window: int = 0, scale: float | None = None, streams=None, positions=None, idx=None, count=None, out=None):
+        """dcnn_cache_attend: attention of queries q [rows, q_heads * dim] over the tokens of their streams, [rows, q_heads * dim].
+
+        q_heads is a multiple of the cache's heads; consecutive query heads share one.  lens: int32 [streams], the tokens that
+        count (None: `length`).  causal: none behind the row's position; window: only those nearer to it than so many (0: all).
+        scale: of the products, 1 / sqrt(dim) where it is None.  out: a matrix to write."""
+        a, dev = CacheAttendArgs(), self.ctx.index
+        a.q, a.ldq, n, a.q_heads = _as_heads(q, "q", self.dim, self.dtype, dev)
+        rows = self._args(a, n, streams, positions, idx, count)
+        if out is None:
+            out = self.ctx.empty((rows, a.q_heads * self.dim), self.dtype)
+            a.y, a.ldy = out.data_ptr(), a.q_heads * self.dim
+        else:
+            a.y, a.ldy, n = _as_rows(out, "out", a.q_heads * self.dim, self.dtype, dev)
+            rows = _room(rows, n, "out", count)
+        if lens is not None:
+            a.lens = _int32(lens, "lens", dev)
+            _whole(lens, self.streams, "lens", "the cache's streams are")
+        a.rows, a.causal, a.window = rows, 1 if causal else 0, window
+        a.scale = self.dim ** -0.5 if scale is None else scale
+        with self._one_call:                                      # (a call's kernels follow each other: both use the scratch)
+            a.scratch, a.scratch_bytes = self._scratch_for(rows, a.q_heads)
+            st = self.ctx.lib.dcnn_cache_attend(self.ctx.handle, a)
+            if st:
+                self.ctx.check(st)
+        return out
+
+    def _scratch_for(self, rows, q_heads):
+        """(address, bytes) of scratch for a call; a larger one takes the place of a smaller one."""
+        need = self.ctx.lib.dcnn_cache_scratch_bytes(rows, q_heads, self.heads, self.dim, self.streams, self.length)
+        scratch, capturing = self._scratch, self.ctx.capturing()
+        if scratch is None or scratch.numel() < need:
+            scratch = self.ctx.empty(max(need, 256), torch.uint8)
+            if not capturing:                                     # (else it is the graph's)
+                self._scratch = scratch
+        elif capturing:
+            self._captured.add(scratch)
+        return scratch.data_ptr(), scratch.numel()
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

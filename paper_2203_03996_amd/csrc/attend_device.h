@@ -1,0 +1,96 @@
+// Device-side helpers of attention: operands of the matrix cores in the types of a cache.
+#pragma once
+
+#include "cache_device.h"
+
+namespace dcnn {
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef f16 f16x8v __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x8v __attribute__((ext_vector_type(8)));
+
+// What a type's queries, weights, keys and values are on the matrix cores: TERMS operands whose sum is the number.  Codes times a power of two are
+// exact in bf16 (and, from 2^-24 to 2^16, in fp16), fp32 numbers are three bf16 ones.
+template <typename T> struct Operand {
+    typedef f16x8v type;
+    static constexpr int TERMS = 1;
+    static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[0][e] = (f16)v[e];
+    }
+    template <int SEL> static __device__ __forceinline__ uint32_t pair(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, SEL)); }
+    static __device__ __forceinline__ f32x4 mfma16(type a, type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Operand<bf16> {
+    typedef bf16x8v type;
+    static constexpr int TERMS = 1;
+    static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[0][e] = (bf16)v[e];
+    }
+    template <int SEL> static __device__ __forceinline__ uint32_t pair(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL)); }
+    static __device__ __forceinline__ f32x4 mfma16(type a, type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Operand<float> : Operand<bf16> {
+    static constexpr int TERMS = 3;
+    static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float rest = v[e];
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+                o[t][e] = (bf16)rest;
+                rest -= (float)o[t][e];
+            }
+        }
+    }
+};
+// Eight codes of a word, one scale.
+template <typename T> __device__ __forceinline__ typename Operand<T>::type decode8(uint32_t w, float s) {
+    typedef Operand<T> O;
+    const u32x4 v = {O::template pair<0>(w, s), O::template pair<1>(w, s), O::template pair<2>(w, s), O::template pair<3>(w, s)};
+    return __builtin_bit_cast(typename O::type, v);
+}
+// Eight codes of a word, a scale for each: a pair is converted with both, and halves of the two are put together.
+template <typename T> __device__ __forceinline__ typename Operand<T>::type decode8(uint32_t w, const float (&s)[8]) {
+    typedef Operand<T> O;
+    const u32x4 v = {__builtin_amdgcn_perm(O::template pair<0>(w, s[1]), O::template pair<0>(w, s[0]), 0x07060100u),
+                     __builtin_amdgcn_perm(O::template pair<1>(w, s[3]), O::template pair<1>(w, s[2]), 0x07060100u),
+                     __builtin_amdgcn_perm(O::template pair<2>(w, s[5]), O::template pair<2>(w, s[4]), 0x07060100u),
+                     __builtin_amdgcn_perm(O::template pair<3>(w, s[7]), O::template pair<3>(w, s[6]), 0x07060100u)};
+    return __builtin_bit_cast(typename O::type, v);
+}
+// Eight queries' values as the type holds them, as operands.
+template <typename T> __device__ __forceinline__ void load_operand(const T* p, typename Operand<T>::type (&o)[Operand<T>::TERMS]) {
+    if constexpr (sizeof(T) == 2) {
+        o[0] = __builtin_bit_cast(typename Operand<T>::type, *reinterpret_cast<const typename RowVec<T>::type*>(p));
+    } else {
+        float v[8];
+        const typename RowVec<T>::type a = *reinterpret_cast<const typename RowVec<T>::type*>(p), b = *reinterpret_cast<const typename RowVec<T>::type*>(p + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+        Operand<T>::split(v, o);
+    }
+}
+
+// Tokens that a row sees: lo .. hi-1.
+struct Span { int lo, hi; };
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const Token& t) {
+    if (!t.here || (uint32_t)t.stream >= (uint32_t)a.cache.streams) return {0, 0};
+    int lo = 0, hi = a.cache.length;
+    if (a.lens != nullptr) {
+        const int n = a.lens[t.stream];
+        hi = n < 0 ? 0 : (n < hi ? n : hi);
+    }
+    // (in 64 bits: positions may be any number)
+    if (a.causal != 0 && (int64_t)t.pos + 1 < hi) hi = t.pos + 1;
+    if (a.window > 0) {
+        const int64_t first = (int64_t)t.pos - a.window + 1, end = (int64_t)t.pos + a.window;
+        if (end < hi) hi = (int)end;
+        if (first > lo) lo = first < hi ? (int)first : hi;
+    }
+    if (hi <= lo) return {0, 0};
+    return {lo, hi};
+}
+
+}  // namespace dcnn

@@ -1,0 +1,337 @@
+// Attention over the cache for rows that share no stream: one token of each.
+//
+//   S = K q,  p = exp2(S * scale log2(e) - max),  y = V^T p / sum p, the maximum and the sums kept up to date from tile to tile
+//
+// The cache is read once and nothing else is large: HBM bounds it, so every step serves to keep loads in flight.  A workgroup has one row, one
+// head of keys and up to 16 query heads of it (the columns of an operand), and every `splits`-th part of the row's tokens; its four waves go
+// through tiles of 64 tokens in turn, each with its own sums, which are joined at the end.  A tile:
+//   * lane (g, i), g = lane / 16, i = lane % 16.  Operand rows are tokens in the order that puts the products of tokens 16 g .. 16 g + 15
+//     into lane group g: row i of the kt-th sixteen is token 16 (i / 4) + 4 kt + i % 4.  Group g multiplies the words [g NB, (g + 1) NB) of a
+//     token's codes: one wide load, mostly one scale.
+//   * values lie in LDS as they came (rows of D / 2 bytes, columns of 16 bytes permuted against bank conflicts) and are read transposed: 16
+//     tokens of a channel to a lane, the ones whose weights the lane has.  Their 16 scales come straight from the cache.
+//   * codes become operands by conversions that take the scale: one instruction for two values.
+// The next tile's codes and scales are in flight meanwhile.
+#include "attend_device.h"
+
+namespace dcnn {
+
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+// A tile's part of a lane.
+template <int NB> struct KvTile {
+    uint32_t k[4][NB];
+    uint32_t ks[4][2];                         // scale bytes of a word's block: the first and the last word's
+    u32x4 v[NB];
+    u32x4 vs[NB];                              // 16 tokens, NB bytes each
+    bool page;                                 // the lane's sixteen tokens have a page
+};
+
+template <int NB> __device__ __forceinline__ int value_column(int row, int col) {
+    if constexpr (NB == 2 || NB == 6) return col ^ (row >> 3 & 1);
+    if constexpr (NB == 4) return col ^ (row >> 2 & 3);
+    if constexpr (NB == 8) return col ^ (row >> 1 & 7);
+    return col;
+}
+
+// The page of the sixteen tokens `lane % 4` of a tile.
+__device__ __forceinline__ int tile_page(const CacheArgs& c, int stream, int first, int lane) { return page_of(c, stream, (first + 16 * (lane & 3)) >> c.page_shift); }
+
+template <int NB> __device__ __forceinline__ void load_tile(KvTile<NB>& t, const CacheArgs& c, int page, int head, int first, int lane) {
+    constexpr int ROW = NB * 16;
+    const int g = lane / 16, i = lane % 16, mask = (1 << c.page_shift) - 1;
+    const int64_t page_tokens = (int64_t)c.heads << c.page_shift;      // tokens of a page's keys, or values
+    const auto token_at = [&](int p, int group, int which) {
+        return ((int64_t)(p < 0 ? 0 : p) * 2 + which) * page_tokens + ((int64_t)head << c.page_shift) + ((first + 16 * group) & mask);
+    };
+    const int k_page = __shfl(page, i / 4, kWave);
+    const int64_t k_at = token_at(k_page, i / 4, 0) + i % 4;
+    const uint32_t* kp = reinterpret_cast<const uint32_t*>(c.codes + k_at * ROW) + g * NB;
+    const uint8_t* sp = c.scales + k_at * NB;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) t.k[kt][j] = kp[kt * 4 * (ROW / 4) + j];
+        t.ks[kt][0] = sp[kt * 4 * NB + g * NB / 4];
+        if constexpr (NB % 4 != 0 && NB > 2) t.ks[kt][1] = sp[kt * 4 * NB + (g * NB + NB - 1) / 4];
+        if constexpr (NB == 8) t.ks[kt][1] = sp[kt * 4 * NB + g * 2 + 1];
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int chunk = lane + 64 * n, group = chunk / (16 * NB), within = chunk % (16 * NB);
+        const int64_t at = token_at(__shfl(page, group, kWave), group, 1);
+        t.v[n] = *reinterpret_cast<const u32x4*>(c.codes + at * ROW + within * 16);
+    }
+    const int v_page = __shfl(page, g, kWave);
+    t.page = v_page >= 0;
+    const u32x4* vp = reinterpret_cast<const u32x4*>(c.scales + token_at(v_page, g, 1) * NB);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) t.vs[n] = vp[n];
+}
+
+// Scale of token e and block b among a lane's value scales, as a conversion takes it.
+template <int NB> __device__ __forceinline__ float value_scale(const u32x4 (&vs)[NB], int e, int b) {
+    const int byte = e * NB + b, word = byte / 4, at = byte % 4;
+    const uint32_t w = vs[word / 4][word % 4];
+    return __builtin_bit_cast(float, at == 3 ? w >> 1 : w << (23 - 8 * at));
+}
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
+    typedef Operand<T> O;
+    typedef typename O::type Op;
+    constexpr int D = NB * 32, ROW = NB * 16, TERMS = O::TERMS;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * 64 * ROW];         // values of the waves' tiles, then sums
+    __shared__ float stat[4][16][2];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16;
+    uint8_t* const mine = lds + wave * 64 * ROW;
+    const int count = row_count(a.tokens.count, a.tokens.rows);
+    const int units = count * a.cache.heads * a.blocks;
+    for (int64_t item = blockIdx.x; item < (int64_t)units * a.splits; item += gridDim.x) {
+        const int unit = (int)(item / a.splits), part = (int)(item % a.splits);
+        const int block = unit % a.blocks, rest = unit / a.blocks, head = rest % a.cache.heads, r = rest / a.cache.heads;
+        const Token token = token_of(a.tokens, r);
+        const Span span = span_of(a, token);
+        const int start = span.lo & ~63, tiles = (span.hi - start + 63) / 64, share = (tiles + a.splits - 1) / a.splits;
+        const int from = part * share, to = from + share < tiles ? from + share : tiles;
+        // this lane's query head, and its values that meet the lane's part of a key
+        const int column = block * 16 + i;
+        const bool asks = column < a.group;
+        const T* q = static_cast<const T*>(a.q) + (int64_t)r * a.ldq + ((int64_t)head * a.group + (asks ? column : 0)) * D + g * NB * 8;
+        Op qo[NB][TERMS];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            load_operand<T>(q + j * 8, qo[j]);
+            if (!asks) {
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) qo[j][t] = Op{};
+            }
+        }
+        f32x4 o[2 * NB];
+#pragma unroll
+        for (int d = 0; d < 2 * NB; ++d) o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float top = -INFINITY, sum = 0.0f;
+
+        int tile = from + wave;
+        KvTile<NB> next;
+        int page = -1;
+        if (tile < to) {
+            page = tile_page(a.cache, token.stream, start + tile * 64, lane);
+            load_tile<NB>(next, a.cache, page, head, start + tile * 64, lane);
+            if (tile + 4 < to) page = tile_page(a.cache, token.stream, start + (tile + 4) * 64, lane);
+        }
+        for (; tile < to; tile += 4) {
+            const KvTile<NB> now = next;
+            const int first = start + tile * 64;
+            // (a wave's accesses to LDS follow each other: what it reads of the tile before has been read)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int chunk = lane + 64 * n, row = chunk / NB, col = chunk % NB;
+                *reinterpret_cast<u32x4*>(mine + row * ROW + value_column<NB>(row, col) * 16) = now.v[n];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            if (tile + 4 < to) {
+                load_tile<NB>(next, a.cache, page, head, first + 256, lane);
+                if (tile + 8 < to) page = tile_page(a.cache, token.stream, first + 512, lane);
+            }
+            float p[16];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+                const float s0 = scale_of_byte(now.ks[kt][0]), s1 = NB % 4 != 0 && NB <= 2 ? s0 : NB == 4 ? s0 : scale_of_byte(now.ks[kt][1]);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const float sj = (NB == 8 ? j < 4 : (g * NB + j) / 4 == g * NB / 4) ? s0 : s1;
+                    const Op k = decode8<T>(now.k[kt][j], sj);
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) s = O::mfma16(k, qo[j][t], s);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[kt * 4 + e] = s[e] * a.factor;
+            }
+            // the lane's column, tokens first + 16 g + 0 .. 15
+            uint32_t seen = 0xffffu;
+            const bool ragged = first < span.lo || first + 64 > span.hi || !__all(now.page);
+            if (ragged) {
+                const int t = first + 16 * g;
+                seen = 0;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) seen |= now.page && t + e >= span.lo && t + e < span.hi ? 1u << e : 0u;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) p[e] = seen >> e & 1 ? p[e] : -INFINITY;
+            }
+            float m = p[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) m = fmaxf(m, p[e]);
+            m = fmaxf(m, __shfl_xor(m, 16, kWave));
+            m = fmaxf(m, __shfl_xor(m, 32, kWave));
+            m = fmaxf(m, top);
+            if (__any(m > top)) {
+                const float factor = m > top ? __builtin_amdgcn_exp2f(top - m) : 1.0f;        // (top may be -inf: 0)
+                top = m;
+                sum *= factor;
+#pragma unroll
+                for (int d = 0; d < 2 * NB; ++d) o[d] *= factor;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(p[e] - base);
+                sum += p[e];
+            }
+            Op w[2][TERMS];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) O::split(*reinterpret_cast<const float(*)[8]>(p + 8 * s), w[s]);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float vs[2][8];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) vs[e / 8][e % 8] = value_scale<NB>(now.vs, e, b);
+                if (ragged) {                                          // (what lies in masked places may be anything, and a zero times NaN is one)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) vs[e / 8][e % 8] = seen >> e & 1 ? vs[e / 8][e % 8] : 0.0f;
+                }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int d = 2 * b + half;
+                    const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(mine + lane * ROW + value_column<NB>(lane, b) * 16 + half * 8));
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const Op k = decode8<T>((uint32_t)v[s], vs[s]);
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t) o[d] = O::mfma16(k, w[s][t], o[d]);
+                    }
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        }
+
+        // the waves' sums as one: those of waves 2 and 3 to waves 0 and 1, then wave 1's to wave 0
+        sum += __shfl_xor(sum, 16, kWave);
+        sum += __shfl_xor(sum, 32, kWave);
+        if (g == 0) stat[wave][i][0] = top, stat[wave][i][1] = sum;
+        __syncthreads();
+        float all = stat[0][i][0], total = 0.0f;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) all = fmaxf(all, stat[w][i][0]);
+        const float base = all == -INFINITY ? 0.0f : all;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) total += stat[w][i][1] * (all == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(stat[w][i][0] - base));
+        const float factor = all == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - base);
+#pragma unroll
+        for (int d = 0; d < 2 * NB; ++d) o[d] *= factor;
+        f32x4* const sums = reinterpret_cast<f32x4*>(lds);
+        if (wave >= 2) {
+#pragma unroll
+            for (int d = 0; d < 2 * NB; ++d) sums[((wave - 2) * 2 * NB + d) * kWave + lane] = o[d];
+        }
+        __syncthreads();
+        if (wave < 2) {
+#pragma unroll
+            for (int d = 0; d < 2 * NB; ++d) o[d] += sums[(wave * 2 * NB + d) * kWave + lane];
+        }
+        __syncthreads();
+        if (wave == 1) {
+#pragma unroll
+            for (int d = 0; d < 2 * NB; ++d) sums[d * kWave + lane] = o[d];
+        }
+        __syncthreads();
+        if (wave == 0 && asks) {
+#pragma unroll
+            for (int d = 0; d < 2 * NB; ++d) o[d] += sums[d * kWave + lane];
+            if (a.splits == 1) {
+                T* y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + ((int64_t)head * a.group + column) * D + 4 * g;
+                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+                for (int d = 0; d < 2 * NB; ++d) {
+                    typename RowQuad<T>::type v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = (T)(total == 0.0f ? 0.0f : o[d][e] * inv);
+                    *reinterpret_cast<typename RowQuad<T>::type*>(y + d * 16) = v;
+                }
+            } else {
+                const int64_t at = item * 16 + i;
+#pragma unroll
+                for (int d = 0; d < 2 * NB; ++d) *reinterpret_cast<f32x4*>(a.part + at * D + d * 16 + 4 * g) = o[d];
+                if (g == 0) a.stat[at * 2] = all, a.stat[at * 2 + 1] = total;
+            }
+        }
+        __syncthreads();                                               // (the sums have been read: the next row's values may come)
+    }
+}
+
+// The parts of a row and head as one.
+template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    constexpr int E = (D + 63) / 64;
+    __shared__ float sums[4][D];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int count = row_count(a.tokens.count, a.tokens.rows);
+    const int q_heads = a.cache.heads * a.group;
+    for (int unit = blockIdx.x; unit < count * q_heads; unit += gridDim.x) {
+        const int r = unit / q_heads, q_head = unit % q_heads, head = q_head / a.group, in_group = q_head % a.group;
+        const int64_t first = ((((int64_t)r * a.cache.heads + head) * a.blocks + in_group / 16) * a.splits) * 16 + in_group % 16;
+        float top = -INFINITY;
+        for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.stat[(first + (int64_t)s * 16) * 2]);
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+        const float base = top == -INFINITY ? 0.0f : top;
+        float total = 0.0f, o[E] = {};
+#pragma unroll 4
+        for (int s = wave; s < a.splits; s += 4) {
+            const int64_t at = first + (int64_t)s * 16;
+            const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
+            total += a.stat[at * 2 + 1] * w;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (lane + 64 * e < D) o[e] += a.part[at * D + lane + 64 * e] * w;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
+        __shared__ float totals[4];
+        if (lane == 0) totals[wave] = total;
+        __syncthreads();
+        total = totals[0] + totals[1] + totals[2] + totals[3];
+        if ((int)threadIdx.x < D) {
+            const int d = threadIdx.x;
+            const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
+            static_cast<T*>(a.y)[(int64_t)r * a.ldy + (int64_t)q_head * D + d] = (T)(total == 0.0f ? 0.0f : v / total);
+        }
+        __syncthreads();
+    }
+}
+
+AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t length) {
+    AttendPlan p;
+    p.units = rows * heads * cdiv(q_heads / heads, 16);
+    const int64_t wanted = cdiv(2048, p.units < 1 ? 1 : p.units), most = cdiv(length, 256);
+    p.splits = (int)(wanted < most ? wanted : most);
+    return p;
+}
+
+template <typename T, int NB> static dcnn_status launch_few(dcnn_ctx* ctx, const AttendArgs& a) {
+    const int64_t units = (int64_t)a.tokens.rows * a.cache.heads * a.blocks * a.splits, most = (int64_t)ctx->num_cu * 16;
+    hipLaunchKernelGGL((attend_few_kernel<T, NB>), dim3((unsigned)(units < most ? units : most)), dim3(256), 0, ctx->stream, a);
+    dcnn_status st = check_hip(ctx, hipGetLastError(), "attend_few_kernel launch");
+    if (st != DCNN_OK || a.splits == 1) return st;
+    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group;
+    hipLaunchKernelGGL((attend_join_kernel<T, NB * 32>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);
+    return check_hip(ctx, hipGetLastError(), "attend_join_kernel launch");
+}
+template <typename T> static dcnn_status launch_few_t(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
+    switch (dim) {
+        case 32: return launch_few<T, 1>(ctx, a);
+        case 64: return launch_few<T, 2>(ctx, a);
+        case 96: return launch_few<T, 3>(ctx, a);
+        case 128: return launch_few<T, 4>(ctx, a);
+        case 192: return launch_few<T, 6>(ctx, a);
+        default: return launch_few<T, 8>(ctx, a);
+    }
+}
+dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a) {
+    if (dtype == DCNN_F16) return launch_few_t<f16>(ctx, dim, a);
+    if (dtype == DCNN_BF16) return launch_few_t<bf16>(ctx, dim, a);
+    return launch_few_t<float>(ctx, dim, a);
+}
+
+}  // namespace dcnn

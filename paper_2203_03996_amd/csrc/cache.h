@@ -1,0 +1,70 @@
+// Heads, the cache in 4 bits and attention over it: what their translation units share (internal).
+#pragma once
+
+#include "rows.h"
+
+namespace dcnn {
+
+constexpr int64_t kCacheMaxLength = 1 << 30;   // positions, with a tile of tokens behind them, fit 31 bits
+constexpr int64_t kMaxHeadRows = 1 << 30;      // rows * heads of a call
+constexpr int64_t kMaxPageBytes = 0xffffffff;  // of a page's codes: the factor of a page's number fits 32 bits
+constexpr int kMxBlock = 32;                   // values that share a scale
+
+inline bool cache_dim(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
+
+// Which token a row is (see dcnn_row_tokens).
+struct TokenArgs {
+    const int32_t *idx, *count, *stream, *pos;
+    int rows, map_rows;
+    FastDiv period;
+};
+struct CacheArgs {
+    uint8_t *codes, *scales;
+    const int32_t* pages;
+    int heads, dim, page_shift, num_pages;
+    int streams, length, per_stream;           // per_stream: pages of a stream
+};
+struct RotationArgs {
+    const float* table;                        // null: none
+    int positions, rot, style;
+};
+// One matrix of heads of a call.
+struct HeadJob {
+    const void *in, *w, *b;
+    void* out;
+    int64_t ld_in, ld_out;
+    int heads, norm;
+    float eps;
+};
+enum HeadsOp { kTurnHeads, kAppendHeads, kReadHeads };
+struct HeadsArgs {
+    TokenArgs tokens;
+    CacheArgs cache;                           // append, read
+    RotationArgs rotation;                     // of both jobs' heads (kTurnHeads), of the keys (kAppendHeads)
+    HeadJob job[2];                            // queries and keys, or keys and values
+    int chunk, chunks[2];                      // heads that a workgroup takes one after the other, and how many such parts a job has
+};
+dcnn_status launch_heads(dcnn_ctx* ctx, int dtype, int dim, HeadsOp op, HeadsArgs a);
+
+struct AttendArgs {
+    TokenArgs tokens;
+    CacheArgs cache;
+    const void* q;
+    void* y;
+    int64_t ldq, ldy;
+    int group;                                 // query heads of a head of keys
+    int blocks;                                // sixteens of them
+    float factor;                              // scale * log2(e)
+    int causal, window;
+    const int32_t* lens;
+    int splits;                                // workgroups that share a row's tokens
+    float *part, *stat;                        // with splits: sums [unit][split][16][dim], maxima and sums of weights [unit][split][16][2]
+};
+struct AttendPlan {
+    int splits;
+    int64_t units;                             // rows (at most) * heads * blocks
+};
+AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t length);
+dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);
+
+}  // namespace dcnn

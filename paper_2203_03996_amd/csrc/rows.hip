@@ -1,6 +1,6 @@
 // C entry points of the row operators: checks of arguments, no kernels.
-#include "overlap.h"
 #include "rows.h"
+#include "rows_check.h"
 
 using namespace dcnn;
 
@@ -8,27 +8,6 @@ namespace {
 
 constexpr int64_t kLdqMax = 1 << 22;       // 8-bit rows of a tile are addressed in 32 bits
 
-bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-
-dcnn_status check_list(dcnn_ctx* ctx, const char* what, const dcnn_row_list& l) {
-    if (l.rows < 0 || l.rows > kRowsMax) return fail(ctx, DCNN_EINVAL, "%s: %lld rows", what, (long long)l.rows);
-    if (!aligned(l.idx_dev, 4) || !aligned(l.count_dev, 4)) return fail(ctx, DCNN_EINVAL, "%s: idx or count not 4-byte aligned", what);
-    return DCNN_OK;
-}
-// the part of the list that maps need
-dcnn_status check_map(dcnn_ctx* ctx, const char* what, const dcnn_row_list& l) {
-    if (l.map_rows < 0 || l.map_rows > kRowsMax) return fail(ctx, DCNN_EINVAL, "%s: maps of %lld rows", what, (long long)l.map_rows);
-    if (l.idx_dev == nullptr && l.map_rows < l.rows)
-        return fail(ctx, DCNN_ESHAPE, "%s: %lld rows of maps that have %lld", what, (long long)l.rows, (long long)l.map_rows);
-    return DCNN_OK;
-}
-dcnn_status check_ld(dcnn_ctx* ctx, const char* what, const char* name, const void* p, int64_t ld, int64_t c, size_t es) {
-    if (p == nullptr) return DCNN_OK;
-    if (ld < c) return fail(ctx, DCNN_ESHAPE, "%s: leading dimension %lld of %s is less than its %lld columns", what, (long long)ld, name, (long long)c);
-    if (ld > kLdMax) return fail(ctx, DCNN_EUNSUPPORTED, "%s: leading dimension %lld of %s", what, (long long)ld, name);
-    if (!aligned(p, es)) return fail(ctx, DCNN_EINVAL, "%s: %s is not aligned to its elements", what, name);
-    return DCNN_OK;
-}
 dcnn_status check_q(dcnn_ctx* ctx, const char* what, const void* q, const void* scale, int64_t ld, int64_t c) {
     if (q == nullptr || scale == nullptr) return fail(ctx, DCNN_EINVAL, "%s: 8-bit rows need q and q_scale", what);
     if (!aligned(q, 16) || ld % 16 != 0) return fail(ctx, DCNN_EINVAL, "%s: 8-bit rows must start at multiples of 16 bytes (ldq %lld)", what, (long long)ld);
@@ -36,33 +15,6 @@ dcnn_status check_q(dcnn_ctx* ctx, const char* what, const void* q, const void* 
     if (!aligned(scale, 4)) return fail(ctx, DCNN_EINVAL, "%s: q_scale not 4-byte aligned", what);
     return check_ld(ctx, what, "q", q, ld, c, 1);
 }
-dcnn_status check_norm(dcnn_ctx* ctx, const char* what, const dcnn_row_norm& n, size_t es) {
-    if (n.kind < DCNN_NORM_NONE || n.kind > DCNN_NORM_LAYER) return fail(ctx, DCNN_EINVAL, "%s: norm %d", what, n.kind);
-    if (n.kind == DCNN_NORM_NONE) return DCNN_OK;
-    if (!(n.eps >= 0.0f) || n.eps > 3.0e38f) return fail(ctx, DCNN_EINVAL, "%s: a norm's eps must be finite and not negative", what);
-    if (!aligned(n.w_dev, es) || !aligned(n.b_dev, es)) return fail(ctx, DCNN_EINVAL, "%s: a norm's parameters are not aligned to their elements", what);
-    return DCNN_OK;
-}
-void set_norm(const dcnn_row_norm& n, int* kind, float* eps, const void** w, const void** b) {
-    *kind = n.kind;
-    *eps = n.eps;
-    *w = n.kind == DCNN_NORM_NONE ? nullptr : n.w_dev;
-    *b = n.kind == DCNN_NORM_NONE ? nullptr : n.b_dev;
-}
-// An output shares no byte with an input or another output: workgroups run in any order, and what one of them reads another may have
-// written over.  (`x` may be `y`, the caller says where: a row is read before it is written.)
-template <int OUTS, int INS>
-dcnn_status check_apart(dcnn_ctx* ctx, const char* what, const Bytes (&outs)[OUTS], const Bytes (&ins)[INS], const Bytes* y = nullptr, const Bytes* x = nullptr) {
-    for (int i = 0; i < OUTS; ++i) {
-        for (int j = i + 1; j < OUTS; ++j)
-            if (overlap(outs[i], outs[j])) return fail(ctx, DCNN_EINVAL, "%s: %s overlaps %s", what, outs[i].name, outs[j].name);
-        for (int j = 0; j < INS; ++j)
-            if (!(&outs[i] == y && &ins[j] == x) && overlap(outs[i], ins[j])) return fail(ctx, DCNN_EINVAL, "%s: %s overlaps %s", what, outs[i].name, ins[j].name);
-    }
-    return DCNN_OK;
-}
-Bytes vector_bytes(const char* name, const void* p, int64_t bytes) { return {name, p, 1, bytes, bytes}; }
-Bytes matrix_bytes(const char* name, const void* p, int64_t rows, int64_t ld, int64_t c, size_t es) { return {name, p, rows, ld * (int64_t)es, c * (int64_t)es}; }
 // Scratch, which grows with the rows: the counts of workgroups that share a tile (at the same place whatever the sizes: they are zero between calls), their
 // partial sums, then the 8-bit rows of a call that makes some: scales, rows
 struct Scratch {

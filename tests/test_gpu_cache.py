@@ -1,0 +1,639 @@
+"""Heads with norm and rotation, the cache in 4 bits and attention over it, against plain forms in 64 bits.
+
+Tolerances follow from the arithmetic.  U32 and U are the unit round-offs of fp32 and of the storage type:
+* heads: a head's sum is eight numbers to a lane and five steps between lanes, so it is good to 13 U32 of its magnitudes and a norm's factor to half
+  of that; mean, centring, factor, weight, bias, two products and a sum of the rotation are a few more: 32 U32 of the magnitudes that meet, U of the result.
+* the cache: codes and scales are equal to those of 64 bits.
+* attention: see attend64, and U of the result.
+* results below the storage type's normal range are good to half of its smallest step."""
+import pytest
+import torch
+
+import paper_2203_03996_amd as pkg
+from tests import cache_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+TYPES = {"f32": (torch.float32, 2.0 ** -24, 2.0 ** -149), "f16": (torch.float16, 2.0 ** -11, 2.0 ** -24), "bf16": (torch.bfloat16, 2.0 ** -8, 2.0 ** -133)}
+TERMS = {"f32": 3, "f16": 1, "bf16": 1}
+DIMS = [32, 64, 96, 128, 192, 256]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return pkg.Context(0)
+
+
+def seeded(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def rand(gen, *shape, dt="f32", scale=1.0, mean=0.0):
+    return (torch.randn(*shape, device="cuda", generator=gen) * scale + mean).to(TYPES[dt][0])
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def close(got, want, dt, slack, what):
+    _, u, tiny = TYPES[dt]
+    got = got.double().view(want.shape)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
+    err = (got - want).abs() - (u * want.abs() + slack + 0.5 * tiny)
+    err = torch.where(torch.isfinite(want), err, torch.zeros_like(err))
+    worst = err.max() if err.numel() else torch.tensor(0.0)
+    assert worst <= 0, f"{what}: off by {worst:.3e} more than the arithmetic allows (at {(err == worst).nonzero()[0].tolist()})"
+
+
+def norm_of(gen, kind, dim, dt, params=True):
+    """(RowNorm or None, what heads64 takes)."""
+    if kind == "none":
+        return None, {}
+    w = rand(gen, dim, dt=dt, scale=0.3, mean=1.0) if params else None
+    b = rand(gen, dim, dt=dt, scale=0.3) if params and kind == "layer" else None
+    return pkg.RowNorm(kind, w, b, 1e-5), dict(kind=kind, w=w, b=b, eps=float(torch.tensor(1e-5, dtype=torch.float32)))
+
+
+# ---- heads ----------------------------------------------------------------------------------------------------------
+def check_heads(ctx, dt, dim, rows, q_heads, k_heads, kind, rot, style, seed=0, params=True, pad=0, positions=None):
+    gen = seeded(seed)
+    wide = rand(gen, rows, (q_heads + k_heads) * dim + pad, dt=dt, scale=2.0, mean=0.5)
+    q, k = wide[:, :q_heads * dim], wide[:, q_heads * dim:(q_heads + k_heads) * dim]
+    (qn, qp), (kn, kp) = norm_of(gen, kind, dim, dt, params), norm_of(gen, kind, dim, dt, params)
+    rotation = pkg.Rotation.of_positions(97, rot, style=style) if rot else None
+    pos = torch.randint(0, 97, (rows,), dtype=torch.int32, device="cuda", generator=gen) if positions is None else positions
+    got = ctx.rows_heads(q, k if k_heads else None, dim=dim, q_norm=qn, k_norm=kn, rotation=rotation, positions=pos)
+    ctx.sync()
+    for x, y, p in ((q, got[0] if k_heads else got, qp), (k, got[1] if k_heads else None, kp)):
+        if y is not None:
+            want, mag = plain.heads64(x, dim, table=rotation and rotation.table, style=style, pos=pos, **p)
+            close(y, want, dt, 32 * U32 * mag, f"{dt} dim {dim} {kind} {style} rot {rot}")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("kind", ["none", "rms", "layer"])
+def test_heads(ctx, dt, dim, kind):
+    for style, rot in (("halves", dim), ("pairs", dim), ("halves", 16), ("pairs", dim // 32 * 16), ("halves", 0)):
+        check_heads(ctx, dt, dim, 37, 5, 3, kind, rot, style)
+    check_heads(ctx, dt, dim, 1, 1, 0, kind, dim, "halves", params=False)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 63, 64, 65, 1000, 5000])
+def test_heads_rows(ctx, dt, rows):
+    check_heads(ctx, dt, 64, rows, 8, 2, "rms", 64, "halves", seed=rows)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("pad", [1, 3, 8])
+def test_heads_of_columns_at_any_address(ctx, dt, pad):
+    check_heads(ctx, dt, 96, 21, 3, 2, "layer", 64, "pairs", pad=pad)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_heads_in_place(ctx, dt):
+    gen = seeded(4)
+    x = rand(gen, 33, 12 * 64, dt=dt)
+    q, k = x[:, :8 * 64], x[:, 8 * 64:10 * 64]
+    rest = x[:, 10 * 64:].clone()
+    qn, _ = norm_of(gen, "rms", 64, dt)
+    rotation, pos = pkg.Rotation.of_positions(50, 64), torch.arange(33, dtype=torch.int32, device="cuda")
+    want = ctx.rows_heads(q, k, dim=64, q_norm=qn, k_norm=qn, rotation=rotation, positions=pos)
+    got = ctx.rows_heads(q, k, dim=64, q_norm=qn, k_norm=qn, rotation=rotation, positions=pos, q_out=q, k_out=k)
+    ctx.sync()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(x[:, 10 * 64:], rest)
+
+
+def test_heads_of_listed_pixels(ctx):
+    gen = seeded(5)
+    h, w, m = 6, 7, 20
+    rotation = pkg.Rotation.of_pixels(h, w, 32)
+    assert rotation.table.shape == (h * w, 16, 2)
+    # pixel (row 2, column 5): eight pairs turned by 2, eight by 5
+    f = 100.0 ** (-torch.arange(8, dtype=torch.float64) * 4 / 32)
+    want = torch.cat([2 * f, 5 * f])
+    assert torch.allclose(rotation.table[2 * w + 5].double().cpu(), torch.stack([want.cos(), want.sin()], 1), atol=2 ** -24)
+    idx = torch.full((m + 9,), 1 << 30, dtype=torch.int32, device="cuda")
+    idx[:m] = torch.randperm(3 * h * w, device="cuda", generator=gen)[:m].sort().values.to(torch.int32)
+    idx[3] = -5                                         # no token
+    q = rand(gen, m + 9, 2 * 32, dt="f16")
+    out = torch.full_like(q, 7.0)
+    ctx.rows_heads(q, dim=32, rotation=rotation, idx=idx, count=ints(m), q_out=out)
+    ctx.sync()
+    want, mag = plain.heads64(q[:m], 32, table=rotation.table, pos=idx[:m].clamp(min=0) % (h * w))
+    want[3], mag[3] = 0.0, 0.0
+    close(out[:m], want, "f16", 32 * U32 * mag, "listed pixels")
+    assert (out[m:] == 7.0).all()
+
+
+def test_heads_at_positions_that_the_table_lacks_are_zeros(ctx):
+    q = rand(seeded(6), 5, 64, dt="bf16")
+    out = ctx.rows_heads(q, dim=64, rotation=pkg.Rotation.of_positions(10, 64), positions=ints(0, 10, -1, 9, 2 ** 31 - 1))
+    ctx.sync()
+    assert (out[[1, 2, 4]] == 0).all() and (out[[0, 3]] != 0).any(1).all()
+
+
+def test_heads_of_broken_rows_stay_in_the_head(ctx):
+    q = rand(seeded(7), 4, 3 * 64, dt="f32")
+    q[1, 64 + 5], q[2, 3] = float("nan"), float("inf")
+    clean = q.clone()
+    clean[1, 64 + 5] = clean[2, 3] = 1.0
+    norm, rotation, pos = pkg.RowNorm("rms"), pkg.Rotation.of_positions(10, 32), ints(1, 2, 3, 4)
+    got, want = (ctx.rows_heads(x, dim=64, q_norm=norm, rotation=rotation, positions=pos).view(4, 3, 64) for x in (q, clean))
+    ctx.sync()
+    broken = torch.zeros(4, 3, dtype=torch.bool, device="cuda")
+    broken[1, 1] = broken[2, 0] = True
+    assert torch.isnan(got[1, 1]).all() and torch.isnan(got[2, 0, 3]) and torch.equal(got[~broken], want[~broken])
+
+
+# ---- the cache ------------------------------------------------------------------------------------------------------
+def new_cache(ctx, streams, length, heads, dim, dt, page=16, shuffled=True, spare=3, garbage=True, seed=1):
+    gen = seeded(seed)
+    per_stream = -(-length // page)
+    num = streams * per_stream + spare
+    codes = torch.randint(0, 256, (num, 2, heads, page, dim // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.full((num, 2, heads, page, dim // 32), 255 if garbage else 127, dtype=torch.uint8, device="cuda")
+    pages = torch.randperm(num, device="cuda", generator=gen)[:streams * per_stream].to(torch.int32).view(streams, per_stream) if shuffled else None
+    return pkg.TokenCache(ctx, streams, length, heads, dim, dtype=TYPES[dt][0], page=page, pages=pages, codes=codes, scales=scales)
+
+
+def places(cache, stream, pos):
+    """(page, slot) of tokens."""
+    stream, pos = stream.long(), pos.long()
+    block = pos // cache.page
+    per_stream = -(-cache.length // cache.page)
+    page = stream * per_stream + block if cache.pages is None else cache.pages[stream, block].long()
+    return page, pos % cache.page
+
+
+def check_append(ctx, cache, k, v, stream, pos, dt, kind="rms", rot=None, style="halves", seed=2, **tokens):
+    """Appends, and compares codes, scales, what is read, and what must not have changed."""
+    gen = seeded(seed)
+    norm, p = norm_of(gen, kind, cache.dim, dt)
+    rotation = pkg.Rotation.of_positions(cache.length, rot, style=style) if rot else None
+    codes, scales = cache.codes.clone(), cache.scales.clone()
+    cache.append(k, v, norm=norm, rotation=rotation, **tokens)
+    m = len(stream)
+    read_k, read_v = cache.read(**tokens)
+    ctx.sync()
+    page, slot = places(cache, stream, pos)
+    for which, x in ((0, plain.heads64(k[:m], cache.dim, table=rotation and rotation.table, style=style, pos=pos, **p)[0]), (1, plain.heads64(v[:m], cache.dim)[0])):
+        c, s = plain.quantised(x)
+        assert torch.equal(cache.scales[page, which, :, slot], s), f"{dt} scales {which}"
+        assert torch.equal(cache.codes[page, which, :, slot], plain.pack(c)), f"{dt} codes {which}"
+        codes[page, which, :, slot], scales[page, which, :, slot] = plain.pack(c), s
+        held = plain.values(plain.pack(c), s).to(TYPES[dt][0])
+        got = (read_k, read_v)[which][:m].view(held.shape)
+        assert torch.equal(torch.nan_to_num(got, 5.0), torch.nan_to_num(held, 5.0)), f"{dt} read {which}"
+    assert torch.equal(cache.codes, codes) and torch.equal(cache.scales, scales), "other places of the cache have changed"
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("dim", DIMS)
+def test_append(ctx, dt, dim):
+    for kind, rot, style in (("rms", dim, "halves"), ("layer", dim // 32 * 16, "pairs"), ("none", dim, "pairs"), ("none", 0, "halves")):
+        cache = new_cache(ctx, 3, 45, 2, dim, dt)
+        gen = seeded(dim)
+        stream, pos = ints(0, 0, 2, 1, 1, 2, 0), ints(0, 44, 15, 16, 17, 31, 1)
+        k, v = (rand(gen, 7, 2 * dim, dt=dt, scale=3.0) for _ in range(2))
+        check_append(ctx, cache, k, v, stream, pos, dt, kind, rot, style, streams=stream, positions=pos)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("page", [16, 64, 4096])
+def test_append_many_rows(ctx, dt, page):
+    cache = new_cache(ctx, 2, 700, 3, 64, dt, page=page)
+    gen = seeded(page)
+    at = torch.randperm(1400, device="cuda", generator=gen)[:1111].to(torch.int32)
+    stream, pos = (at // 700).contiguous(), (at % 700).contiguous()
+    wide = rand(gen, 1111, 2 * 3 * 64 + 5, dt=dt)
+    check_append(ctx, cache, wide[:, :192], wide[:, 193:385], stream, pos, dt, "rms", 64, streams=stream, positions=pos)
+
+
+def test_append_one_token_of_each_stream(ctx):
+    cache = new_cache(ctx, 5, 100, 2, 128, "bf16", page=32)
+    gen = seeded(8)
+    pos = ints(0, 99, 31, 32, 64)
+    k, v = (rand(gen, 5, 256, dt="bf16") for _ in range(2))
+    check_append(ctx, cache, k, v, torch.arange(5, device="cuda"), pos, "bf16", "rms", 128, positions=pos)
+
+
+def test_append_listed_pixels(ctx):
+    cache = new_cache(ctx, 4, 49, 2, 32, "f16", shuffled=False, spare=0)
+    gen = seeded(9)
+    idx = torch.full((80,), 1 << 30, dtype=torch.int32, device="cuda")
+    idx[:33] = torch.randperm(196, device="cuda", generator=gen)[:33].sort().values.to(torch.int32)
+    k, v = (rand(gen, 80, 64, dt="f16") for _ in range(2))
+    check_append(ctx, cache, k, v, idx[:33] // 49, idx[:33] % 49, "f16", "rms", 32, idx=idx, count=ints(33))
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_codes_of_values_between_two(ctx, dt):
+    """Every border of two codes, the numbers next to it on both sides, at scales of many sizes; blocks whose largest magnitude is at the border of two scales."""
+    t = TYPES[dt][0]
+    eps = torch.finfo(t).eps
+    border = torch.tensor([0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0], dtype=torch.float64)
+    rows = []
+    for e in (-20, -13, -3, 0, 1, 5, 12) if dt == "f16" else (-120, -60, -1, 0, 3, 60, 120):
+        for nudge in (0.0, eps, -eps / 2):
+            x = border * (1.0 + nudge)
+            x[-1] = 6.0
+            for top in (6.0, 6.0 * (1 + eps), 3.0, 3.0 * (1 + eps), 5.0):
+                block = torch.zeros(32, dtype=torch.float64)
+                block[:15], block[15:30], block[31] = x * min(1.0, top / 6.0), -x * min(1.0, top / 6.0), -top
+                rows.append(block * 2.0 ** e)
+    x = torch.stack(rows).to(t).cuda()
+    cache = new_cache(ctx, 1, len(x), 1, 32, dt)
+    pos = torch.arange(len(x), dtype=torch.int32, device="cuda")
+    check_append(ctx, cache, x, x.flip(0).contiguous(), torch.zeros_like(pos), pos, dt, "none", streams=torch.zeros_like(pos), positions=pos)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_blocks_of_zeros_tiny_huge_and_broken_values(ctx, dt):
+    t = TYPES[dt][0]
+    info = torch.finfo(t)
+    small = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}[dt]
+    x = rand(seeded(10), 12, 64, dt=dt)
+    x[0] = 0
+    x[1, :32], x[2, :32] = small, info.tiny
+    x[3] = info.max
+    x[4, 5], x[5, 40], x[6, 63] = float("nan"), float("inf"), -float("inf")
+    x[7, 0], x[8, 0], x[9, 0] = info.max, -info.max, info.max / 8
+    cache = new_cache(ctx, 1, 12, 1, 64, dt)
+    pos = torch.arange(12, dtype=torch.int32, device="cuda")
+    check_append(ctx, cache, x, x.flip(0).contiguous(), torch.zeros_like(pos), pos, dt, "none", streams=torch.zeros_like(pos), positions=pos)
+
+
+def test_append_leaves_rows_without_a_place_out(ctx):
+    cache = new_cache(ctx, 2, 40, 1, 32, "f16", page=16)
+    cache.pages[1, 0], cache.pages[1, 1] = -1, cache.num_pages
+    before = cache.codes.clone(), cache.scales.clone()
+    stream, pos = ints(0, 0, -1, 2, 1, 1, 0), ints(-1, 40, 0, 0, 3, 20, 2 ** 31 - 1)
+    k = rand(seeded(11), 7, 32, dt="f16")
+    cache.append(k, k, streams=stream, positions=pos)
+    got = cache.read(streams=stream, positions=pos)
+    ctx.sync()
+    assert torch.equal(cache.codes, before[0]) and torch.equal(cache.scales, before[1])
+    assert all((g == 0).all() for g in got)
+    cache.append(k, k, rotation=pkg.Rotation.of_positions(5, 32), streams=ints(0, 0, 0, 0, 0, 0, 0), positions=ints(5, 6, 7, 8, 9, 10, 39))
+    ctx.sync()
+    assert torch.equal(cache.codes, before[0]), "rows that the rotation has no angles for"
+
+
+def test_pages_behind_four_gigabytes(ctx):
+    """Offsets of far pages pass 32 bits: 2^15 pages of 2^17 bytes."""
+    heads, dim, page = 8, 128, 128
+    num = (1 << 15) + 1200
+    codes = torch.zeros((num, 2, heads, page, dim // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.full((num, 2, heads, page, dim // 32), 127, dtype=torch.uint8, device="cuda")
+    pages = torch.tensor([[num - 1, 3], [num - 2, num - 700]], dtype=torch.int32, device="cuda")
+    cache = pkg.TokenCache(ctx, 2, 256, heads, dim, dtype=torch.float16, page=page, pages=pages, codes=codes, scales=scales)
+    gen = seeded(12)
+    stream = torch.arange(2, dtype=torch.int32, device="cuda").repeat_interleave(256)
+    pos = torch.arange(256, dtype=torch.int32, device="cuda").repeat(2)
+    k, v = (rand(gen, 512, heads * dim, dt="f16") for _ in range(2))
+    cache.append(k, v, streams=stream, positions=pos)
+    q = rand(gen, 2, 2 * heads * dim, dt="f16")
+    out = cache.attend(q, positions=ints(255, 200), causal=True)
+    ctx.sync()
+    c, s = plain.quantised(k.double().view(512, heads, dim))
+    assert torch.equal(codes[num - 1, 0], plain.pack(c)[:128].transpose(0, 1)) and torch.equal(codes[num - 700, 0], plain.pack(c)[384:].transpose(0, 1))
+    assert int((codes.view(num, -1) != 0).any(1).sum()) == 4
+    want, slack = plain.attend64(q, codes, scales, pages, page, [0, 1], [255, 200], [256, 256], dim ** -0.5, causal=True, tiny=2.0 ** -25)
+    close(out, want, "f16", slack, "far pages")
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+def filled(ctx, streams, length, heads, dim, dt, page=16, seed=3, written=None):
+    """A cache of random keys and values; places at and behind `written` tokens of a stream hold NaN scales."""
+    cache = new_cache(ctx, streams, length, heads, dim, dt, page=page, seed=seed)
+    gen = seeded(seed)
+    written = [length] * streams if written is None else written
+    for s in range(streams):
+        n = written[s]
+        if n:
+            pos = torch.arange(n, device="cuda")
+            at, slot = places(cache, torch.full((n,), s, device="cuda"), pos)
+            for which in (0, 1):
+                c, b = plain.quantised(rand(gen, n, heads, dim, scale=1.0 + which))
+                cache.codes[at, which, :, slot], cache.scales[at, which, :, slot] = plain.pack(c), b
+    return cache
+
+
+def check_attend(cache, dt, q, stream, pos, lens, causal=False, window=0, scale=None, what="", out=None, **tokens):
+    ctx = cache.ctx
+    got = cache.attend(q, lens=None if lens is None else ints(*lens), causal=causal, window=window, scale=scale, out=out, **tokens)
+    ctx.sync()
+    m = len(stream)
+    counts = [cache.length] * cache.streams if lens is None else [max(0, min(n, cache.length)) for n in lens]
+    per_stream = -(-cache.length // cache.page)
+    pages = cache.pages if cache.pages is not None else torch.arange(cache.streams * per_stream, device="cuda").view(cache.streams, -1)
+    want, slack = plain.attend64(q[:m], cache.codes, cache.scales, pages, cache.page, stream, pos, counts, cache.dim ** -0.5 if scale is None else scale, causal, window,
+                                 TERMS[dt], TYPES[dt][1], 2.0 ** -25 if dt == "f16" else 0.0)
+    close(got[:m], want, dt, slack, f"{dt} dim {cache.dim} {what}")
+    return got
+
+
+LENGTHS = [0, 1, 15, 16, 17, 63, 64, 65, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("dim", DIMS)
+def test_attend_one_row_of_each_stream(ctx, dt, dim):
+    """All lengths about a tile's and a part's; what lies behind them is NaN."""
+    cache = filled(ctx, len(LENGTHS), 300, 2, dim, dt, written=LENGTHS)
+    q = rand(seeded(dim), len(LENGTHS), 2 * 3 * dim, dt=dt, scale=1.5)
+    check_attend(cache, dt, q, range(len(LENGTHS)), [0] * len(LENGTHS), LENGTHS, positions=ints(*[max(0, n - 1) for n in LENGTHS]))
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("group", [1, 2, 4, 7, 15, 16, 17, 33])
+def test_attend_groups_of_query_heads(ctx, dt, group):
+    cache = filled(ctx, 2, 130, 3, 64, dt, written=[130, 77])
+    q = rand(seeded(group), 2, 3 * group * 64, dt=dt, scale=1.5)
+    check_attend(cache, dt, q, [0, 1], [0, 0], [130, 77], positions=ints(129, 76), what=f"group {group}")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("page", [16, 32, 64, 256, 4096])
+def test_attend_pages(ctx, dt, page):
+    cache = filled(ctx, 2, 333, 1, 128, dt, page=page, written=[333, 200])
+    q = rand(seeded(page), 2, 4 * 128, dt=dt)
+    check_attend(cache, dt, q, [0, 1], [0, 0], [333, 200], positions=ints(332, 199), what=f"page {page}")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 2, 31, 32, 33, 70, 129, 200])
+@pytest.mark.parametrize("group", [1, 4])
+def test_attend_rows_of_one_stream(ctx, dt, rows, group):
+    cache = filled(ctx, 1, 300, 2, 64, dt)
+    gen = seeded(rows)
+    q = rand(gen, rows, 2 * group * 64, dt=dt, scale=1.5)
+    pos = torch.arange(300 - rows, 300, dtype=torch.int32, device="cuda")
+    zero = torch.zeros_like(pos)
+    check_attend(cache, dt, q, zero, pos, [300], causal=True, streams=zero, positions=pos, what="causal")
+    check_attend(cache, dt, q, zero, pos, [300], causal=True, window=50, streams=zero, positions=pos, what="causal window")
+    check_attend(cache, dt, q, zero, pos, [290], window=33, streams=zero, positions=pos, what="window")
+    check_attend(cache, dt, q, zero, pos, None, streams=zero, positions=pos, what="all")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("dim", DIMS)
+def test_attend_rows_of_several_streams(ctx, dt, dim):
+    """Rows in any order, streams of all lengths, rows without a token and rows that see nothing."""
+    lens = [200, 0, 64, 129, 1]
+    cache = filled(ctx, 5, 200, 2, dim, dt, written=lens)
+    gen = seeded(dim + 1)
+    rows = 91
+    stream = torch.randint(-1, 6, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    pos = torch.randint(-5, 205, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    q = rand(gen, rows, 2 * 2 * dim, dt=dt, scale=1.5)
+    for causal, window in ((True, 0), (False, 0), (True, 17), (False, 40)):
+        check_attend(cache, dt, q, stream, pos, lens, causal, window, streams=stream, positions=pos, what=f"causal {causal} window {window}")
+    order = torch.argsort(stream, stable=True)
+    stream, pos = stream[order].contiguous(), pos[order].contiguous()
+    check_attend(cache, dt, q, stream, pos, lens, True, 0, streams=stream, positions=pos, what="in order")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("listed", [1, 40, 150])
+def test_attend_listed_pixels(ctx, dt, listed):
+    streams, n = 6, 100
+    cache = filled(ctx, streams, n, 2, 32, dt)
+    gen = seeded(listed)
+    idx = torch.full((streams * n,), 1 << 30, dtype=torch.int32, device="cuda")
+    idx[:listed] = torch.randperm(streams * n, device="cuda", generator=gen)[:listed].sort().values.to(torch.int32)
+    q = rand(gen, streams * n, 2 * 2 * 32, dt=dt, scale=1.5)
+    out = torch.full_like(q, 7.0)
+    check_attend(cache, dt, q, idx[:listed] // n, idx[:listed] % n, None, idx=idx, count=ints(listed), out=out, what=f"{listed} pixels")
+    assert (out[listed:] == 7.0).all(), "rows behind the list were written"
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [3, 100])
+def test_attend_strided_queries_and_outputs(ctx, dt, rows):
+    cache = filled(ctx, 2, 80, 2, 96, dt)
+    gen = seeded(13)
+    wide = rand(gen, rows, 5 * 192 + 3, dt=dt)
+    q = wide[:, 192:576]
+    out = torch.full((rows, 500), 7.0, dtype=TYPES[dt][0], device="cuda")
+    stream = (torch.arange(rows, dtype=torch.int32, device="cuda") * 2 // rows).to(torch.int32)
+    pos = torch.full_like(stream, 60)
+    check_attend(cache, dt, q, stream, pos, [80, 70], True, streams=stream, positions=pos, out=out[:, 3:387])
+    assert (out[:, :3] == 7.0).all() and (out[:, 387:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+def test_attend_scales(ctx, dt, scale):
+    cache = filled(ctx, 1, 100, 1, 64, dt)
+    for rows in (1, 40):
+        q = rand(seeded(14), rows, 3 * 64, dt=dt)
+        zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        check_attend(cache, dt, q, zero, zero, None, scale=scale, streams=zero, positions=zero, what=f"scale {scale}")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 70])
+def test_attend_products_far_apart(ctx, dt, rows):
+    """Logits of hundreds, the largest in any tile: weights that vanish, maxima that grow from tile to tile, and ones that only fall."""
+    for seed, order in ((15, 1), (16, -1)):
+        cache = filled(ctx, 1, 400, 1, 64, dt, seed=seed)
+        grow = torch.linspace(-3, 3, 400, device="cuda")[::1] * order
+        at, slot = places(cache, torch.zeros(400, device="cuda"), torch.arange(400, device="cuda"))
+        c, b = plain.quantised(grow[:, None, None].double().expand(400, 1, 64))
+        cache.codes[at, 0, :, slot], cache.scales[at, 0, :, slot] = plain.pack(c), b
+        q = rand(seeded(seed), rows, 2 * 64, dt=dt, scale=1.0, mean=8.0)
+        zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        check_attend(cache, dt, q, zero, zero, None, scale=0.7, streams=zero, positions=zero, what="far apart")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_values_of_different_sizes(ctx, dt, rows):
+    """Channels whose values are thousands of times smaller than others', tokens far larger than the rest."""
+    cache = filled(ctx, 1, 150, 1, 128, dt)
+    at, slot = places(cache, torch.zeros(150, device="cuda"), torch.arange(150, device="cuda"))
+    v = rand(seeded(17), 150, 1, 128).double() * torch.tensor([1.0, 2.0 ** -12, 2.0 ** 9, 2.0 ** -6], device="cuda").repeat_interleave(32)
+    v[7] *= 16.0
+    c, b = plain.quantised(v)
+    cache.codes[at, 1, :, slot], cache.scales[at, 1, :, slot] = plain.pack(c), b
+    q = rand(seeded(18), rows, 128, dt=dt)
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    check_attend(cache, dt, q, zero, zero, None, streams=zero, positions=zero, what="sizes")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 50])
+def test_attend_broken_tokens(ctx, dt, rows):
+    """A NaN key or value reaches the rows that see it, and no other: not those before it, nor other heads or streams."""
+    cache = filled(ctx, 2, 128, 2, 64, dt)
+    at, slot = places(cache, torch.zeros(2, device="cuda"), torch.tensor([90, 100], device="cuda"))
+    cache.scales[at[0], 0, 0, slot[0], 1] = 255         # a key of head 0, token 90 of stream 0
+    cache.scales[at[1], 1, 1, slot[1], 0] = 255         # channels 0 to 31 of a value of head 1, token 100
+    q = rand(seeded(19), 2 * rows, 2 * 2 * 64, dt=dt)
+    stream = torch.arange(2, dtype=torch.int32, device="cuda").repeat_interleave(rows)
+    pos = torch.linspace(60, 127, rows, device="cuda").to(torch.int32).repeat(2)
+    got = check_attend(cache, dt, q, stream, pos, None, causal=True, streams=stream, positions=pos).view(2 * rows, 2, 2, 64)
+    first = stream == 0
+    assert torch.equal(torch.isnan(got[:, 0]).all(2).all(1), first & (pos >= 90)) and not torch.isnan(got[~first]).any()
+    assert torch.equal(torch.isnan(got[:, 1, :, :32]).all(2).all(1), first & (pos >= 100)) and not torch.isnan(got[:, 1, :, 32:]).any()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_without_some_pages(ctx, dt, rows):
+    """Tokens of pages that are none do not count, wherever they lie in a tile."""
+    cache = filled(ctx, 1, 150, 1, 32, dt)
+    cache.pages[0, 2], cache.pages[0, 5], cache.pages[0, 9] = -1, cache.num_pages, -(2 ** 31)
+    q = rand(seeded(20), rows, 32, dt=dt)
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    check_attend(cache, dt, q, zero, zero, None, streams=zero, positions=zero, what="pages missing")
+    cache.pages.fill_(-1)
+    assert (cache.attend(q, streams=zero, positions=zero) == 0).all()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_attend_long_cache_in_parts(ctx, dt):
+    cache = filled(ctx, 1, 20000, 1, 64, dt, page=64)
+    for rows in (1, 40):
+        q = rand(seeded(21), rows, 4 * 64, dt=dt)
+        zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        pos = zero + 19990
+        check_attend(cache, dt, q, zero, pos, [19987], causal=True, streams=zero, positions=pos, what=f"{rows} rows")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_the_same_call_gives_the_same_bits(ctx, dt):
+    cache = filled(ctx, 3, 500, 2, 128, dt)
+    gen = seeded(22)
+    for rows in (3, 200):
+        q = rand(gen, rows, 8 * 128, dt=dt)
+        stream = torch.arange(rows, dtype=torch.int32, device="cuda") % 3
+        pos = torch.full_like(stream, 450)
+        a, b = (cache.attend(q, streams=stream, positions=pos, causal=True) for _ in range(2))
+        ctx.sync()
+        assert torch.equal(a, b)
+
+
+def test_calls_of_no_rows(ctx):
+    cache = new_cache(ctx, 2, 20, 1, 32, "f16")
+    none = torch.empty(0, 32, dtype=torch.float16, device="cuda")
+    where = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert ctx.rows_heads(none, dim=32).shape == (0, 32)
+    cache.append(none, none, streams=where, positions=where)
+    assert cache.attend(none, streams=where, positions=where).shape == (0, 32)
+    assert [t.shape for t in cache.read(streams=where, positions=where)] == [(0, 32)] * 2
+    q = rand(seeded(23), 4, 32, dt="f16")
+    out = torch.full_like(q, 7.0)
+    cache.attend(q, idx=ints(0, 1, 2, 3), count=ints(0), out=out)
+    ctx.rows_heads(q, dim=32, idx=ints(0, 1, 2, 3), count=ints(-3), q_out=out)
+    ctx.sync()
+    assert (out == 7.0).all()
+
+
+# ---- together, as a program uses them -------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_a_text_token_by_token_is_the_text_at_once(ctx, dt):
+    """Prompt and decode steps: keys and values appended token by token are those of one call, and so are the outputs."""
+    heads, dim, n, streams = 2, 64, 70, 2
+    gen = seeded(24)
+    qkv = rand(gen, streams * n, (4 + 2 * heads) * dim, dt=dt)
+    q, k, v = qkv[:, :4 * dim], qkv[:, 4 * dim:6 * dim], qkv[:, 6 * dim:]
+    stream = torch.arange(streams, dtype=torch.int32, device="cuda").repeat_interleave(n)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(streams)
+    norm, rotation = pkg.RowNorm("rms", rand(gen, dim, dt=dt, scale=0.1, mean=1.0)), pkg.Rotation.of_positions(n, dim)
+    at_once, by_token = (pkg.TokenCache(ctx, streams, n, heads, dim, dtype=TYPES[dt][0], page=16) for _ in range(2))
+    turned = ctx.rows_heads(q, dim=dim, q_norm=norm, rotation=rotation, positions=pos)
+    at_once.append(k, v, norm=norm, rotation=rotation, streams=stream, positions=pos)
+    whole = at_once.attend(turned, causal=True, streams=stream, positions=pos)
+    ctx.sync()
+    lens = torch.zeros(streams, dtype=torch.int32, device="cuda")
+    for t in range(n):
+        rows = torch.arange(streams, device="cuda") * n + t
+        p = lens.clone()
+        step = ctx.rows_heads(q[rows], dim=dim, q_norm=norm, rotation=rotation, positions=p)
+        by_token.append(k[rows], v[rows], norm=norm, rotation=rotation, positions=p)
+        lens += 1
+        out = by_token.attend(step, lens=lens, positions=p)
+        ctx.sync()
+        assert torch.equal(step, turned[rows])
+        want, slack = plain.attend64(step, by_token.codes, by_token.scales, torch.arange(10, device="cuda").view(2, 5), 16, [0, 1], [t, t], [t + 1] * 2, dim ** -0.5, True, 0,
+                                     TERMS[dt], TYPES[dt][1], 2.0 ** -25 if dt == "f16" else 0.0)
+        close(out, want, dt, slack, f"token {t}")
+        close(whole[rows], want, dt, slack, f"token {t} at once")
+    assert torch.equal(at_once.codes, by_token.codes) and torch.equal(at_once.scales, by_token.scales)
+
+
+def test_captured_steps_replayed_with_other_lengths(ctx):
+    """A decode step as a graph: replayed with new tokens and lengths, with eager work and synchronisations between, it gives the eager step's results."""
+    heads, dim, n, streams = 2, 128, 400, 3
+    gen = seeded(25)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        own = pkg.Context(0)
+        cache = filled(own, streams, n, heads, dim, "f16", page=32)
+        rotation, norm = pkg.Rotation.of_positions(n, dim), pkg.RowNorm("rms")
+        x = rand(gen, streams, (4 + 2 * heads) * dim, dt="f16")
+        pos, lens = ints(5, 100, 390), ints(6, 101, 391)
+
+        def step():
+            q = own.rows_heads(x[:, :4 * dim], dim=dim, q_norm=norm, rotation=rotation, positions=pos)
+            cache.append(x[:, 4 * dim:6 * dim], x[:, 6 * dim:], norm=norm, rotation=rotation, positions=pos)
+            return cache.attend(q, lens=lens, positions=pos)
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured = step()
+        for i in range(4):
+            x.copy_(rand(gen, streams, (4 + 2 * heads) * dim, dt="f16"))
+            pos += 1
+            lens += 1
+            graph.replay()
+            side.synchronize()
+            got = captured.clone()
+            want = step()
+            side.synchronize()
+            assert torch.equal(got, want), f"replay {i}"
+
+
+def test_calls_run_on_the_contexts_stream(ctx):
+    """With torch on another stream: new outputs belong to the context's stream, whose work waits for nothing else."""
+    cache = filled(ctx, 2, 100, 1, 64, "bf16")
+    q = rand(seeded(26), 2, 64, dt="bf16")
+    where = ints(50, 60)
+    want = cache.attend(q, positions=where)
+    ctx.sync()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        got = cache.attend(q, positions=where)
+        turned = ctx.rows_heads(q, dim=64)
+    ctx.sync()
+    assert torch.equal(got, want) and torch.equal(turned, q)
+
+
+# ---- refusals -------------------------------------------------------------------------------------------------------
+def test_outputs_that_share_bytes_are_refused(ctx):
+    cache = new_cache(ctx, 2, 64, 2, 64, "f16")
+    x = rand(seeded(27), 4, 512, dt="f16")
+    where = ints(1, 2)
+    with pytest.raises(pkg.DcnnError):
+        ctx.rows_heads(x[:, :128], dim=64, q_out=x[:, 64:192])
+    with pytest.raises(pkg.DcnnError):
+        ctx.rows_heads(x[:, :128], x[:, 128:256], dim=64, q_out=x[:, 128:256])
+    with pytest.raises(pkg.DcnnError):
+        cache.attend(x[:2, :128], positions=where, out=x[:2, 64:192])
+    with pytest.raises(pkg.DcnnError):
+        cache.attend(x[:2, :128], positions=where, out=cache.codes.view(-1)[:512].view(torch.float16).view(2, 128))
+    with pytest.raises(pkg.DcnnError):
+        cache.append(cache.codes.view(-1)[:512].view(torch.float16).view(2, 128), x[:2, :128], positions=where)
+    out = torch.empty(4, 512, dtype=torch.float16, device="cuda")
+    ctx.rows_heads(x[:, :128], x[:, 128:256], dim=64, q_out=out[:, :128], k_out=out[:, 300:428])
+    ctx.sync()
+    assert torch.equal(out[:, :128], x[:, :128]) and torch.equal(out[:, 300:428], x[:, 128:256])
