@@ -416,7 +416,8 @@ dcnn_status dcnn_rows_heads(dcnn_ctx* ctx, const dcnn_rows_heads_args* args);
 
 /* A paged cache of keys and values in 4 bits, memory of the caller's.  Each 32 values of a head are 4-bit floating-point
  * codes -- a sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 -- and one power of two that they are
- * multiplied with: a byte, the exponent with a bias of 127 (255: the values are NaN).
+ * multiplied with: a byte, the exponent with a bias of 127 (255: the values are NaN; calls on a cache whose products are out of
+ * its dtype's range, which dcnn_cache_append does not make, give infinities or NaN).
  *   codes   [num_pages][2: keys, values][heads][page][dim / 2], the value of an even place in the low half of its byte
  *   scales  [num_pages][2][heads][page][dim / 32]
  * Token p of stream s lies in slot p % page of page pages[s][p / page].  A page whose number is outside 0 .. num_pages-1 is
@@ -434,8 +435,9 @@ typedef struct {
 } dcnn_cache;
 
 /* Writes the keys (normed and rotated first) and values of rows into the cache.  The scale of 32 values is the smallest
- * power of two with max|v| <= 6 * scale (2^-126 at least), and each becomes the code next to v / scale, ties to the even
- * one (a zero keeps its sign); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
+ * power of two with max|v| <= 6 * scale (2^-126 at least; at most 2^13 in fp16 and 2^125 else, so that what is held is
+ * finite: larger magnitudes are held as 6 * scale), and each becomes the code next to v / scale, ties to the even one (a
+ * zero keeps its sign); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
  * order of a sum.  Rows without a token, or with a position outside 0 .. length-1, write nothing.  The (stream, position)
  * of rows must be distinct.  rows * heads at most 2^30. */
 typedef struct {
@@ -448,8 +450,7 @@ typedef struct {
 } dcnn_cache_append_args;
 dcnn_status dcnn_cache_append(dcnn_ctx* ctx, const dcnn_cache_append_args* args);
 
-/* What the cache holds for the tokens of rows, as numbers of its dtype (fp16: a held magnitude of 65536 or more is infinite);
- * zeros for a row without a token.  Either output may be NULL. */
+/* What the cache holds for the tokens of rows, as numbers of its dtype; zeros for a row without a token.  Either output may be NULL. */
 typedef struct {
     dcnn_cache      cache;
     dcnn_row_tokens tokens;
@@ -463,8 +464,8 @@ dcnn_status dcnn_cache_read(dcnn_ctx* ctx, const dcnn_cache_read_args* args);
  * over the tokens t of the row's stream with t < len (lens_dev[stream], cut to 0 .. length; NULL: length), t <= position if
  * `causal`, and |position - t| < window if window > 0.  Rows that see no token, or have none, become zeros.  Queries and
  * keys meet exactly, sums and the softmax's statistics are fp32; the weights of a row, relative to the largest, are rounded
- * to the dtype before they meet the values (F32: kept), and the result once more.  F16 holds keys and values rounded to
- * fp16 (see dcnn_cache_read).
+ * to the dtype before they meet the values (F32: kept), and the result once more.  Keys and values are what
+ * dcnn_cache_read gives.
  * scratch_dev: dcnn_cache_scratch_bytes(...) bytes of the cache's and the call's sizes, 256-byte aligned, whatever it holds;
  * calls may share it one after the other.  rows * q_heads at most 2^30. */
 typedef struct {

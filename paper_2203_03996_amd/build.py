@@ -13,7 +13,8 @@ LIB = os.path.join(LIBDIR, "libdeltacnn.so")
 SOURCES = [("ctx.hip", "ctx.o", []), ("mask_kernels.hip", "mask_kernels.o", []), ("tile_kernels.hip", "tile_kernels.o", []),
            ("conv_kernels.hip", "conv_kernels.o", []), ("conv_first.hip", "conv_first.o", []), ("conv_unit.hip", "conv_unit.o", []), ("layer.hip", "layer.o", []), ("net.hip", "net.o", []),
            ("rows.hip", "rows.o", []), ("rows_norm.hip", "rows_norm.o", []), ("rows_matmul.hip", "rows_matmul.o", []),
-           ("cache.hip", "cache.o", []), ("cache_heads.hip", "cache_heads.o", []), ("attend_few.hip", "attend_few.o", [])]
+           ("cache.hip", "cache.o", []), ("cache_heads.hip", "cache_heads.o", []), ("attend.hip", "attend.o", []), ("attend_few.hip", "attend_few.o", []),
+           ("attend_tile.hip", "attend_tile.o", [])]
 # the MFMA convolution kernels: one object per (element type, accumulator block count), built in parallel
 for _t, _tn in (("f16", "f16"), ("float", "f32")):
     for _nb in (4, 3, 2, 1):

@@ -20,6 +20,7 @@ template <typename T> struct Operand {
     }
     template <int SEL> static __device__ __forceinline__ uint32_t pair(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, SEL)); }
     static __device__ __forceinline__ f32x4 mfma16(type a, type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma32(type a, type b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<bf16> {
     typedef bf16x8v type;
@@ -30,6 +31,7 @@ template <> struct Operand<bf16> {
     }
     template <int SEL> static __device__ __forceinline__ uint32_t pair(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL)); }
     static __device__ __forceinline__ f32x4 mfma16(type a, type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma32(type a, type b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<float> : Operand<bf16> {
     static constexpr int TERMS = 3;
@@ -60,15 +62,17 @@ template <typename T> __device__ __forceinline__ typename Operand<T>::type decod
                      __builtin_amdgcn_perm(O::template pair<3>(w, s[7]), O::template pair<3>(w, s[6]), 0x07060100u)};
     return __builtin_bit_cast(typename O::type, v);
 }
-// Eight queries' values as the type holds them, as operands.
-template <typename T> __device__ __forceinline__ void load_operand(const T* p, typename Operand<T>::type (&o)[Operand<T>::TERMS]) {
+// Eight values of queries as operands, or their opposites.
+template <typename T> __device__ __forceinline__ void load_operand(const T* p, int negate, typename Operand<T>::type (&o)[Operand<T>::TERMS]) {
     if constexpr (sizeof(T) == 2) {
-        o[0] = __builtin_bit_cast(typename Operand<T>::type, *reinterpret_cast<const typename RowVec<T>::type*>(p));
+        u32x4 v = __builtin_bit_cast(u32x4, *reinterpret_cast<const typename RowVec<T>::type*>(p));
+        v ^= negate ? 0x80008000u : 0u;
+        o[0] = __builtin_bit_cast(typename Operand<T>::type, v);
     } else {
         float v[8];
         const typename RowVec<T>::type a = *reinterpret_cast<const typename RowVec<T>::type*>(p), b = *reinterpret_cast<const typename RowVec<T>::type*>(p + 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+        for (int e = 0; e < 4; ++e) v[e] = negate ? -a[e] : a[e], v[4 + e] = negate ? -b[e] : b[e];
         Operand<T>::split(v, o);
     }
 }

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
         Op qo[NB][TERMS];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            load_operand<T>(q + j * 8, qo[j]);
+            load_operand<T>(q + j * 8, a.negate, qo[j]);
             if (!asks) {
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) qo[j][t] = Op{};
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
                     *reinterpret_cast<typename RowQuad<T>::type*>(y + d * 16) = v;
                 }
             } else {
-                const int64_t at = item * 16 + i;
+                const int64_t at = ((int64_t)r * a.cache.heads * a.group + head * a.group + column) * a.splits + part;
 #pragma unroll
                 for (int d = 0; d < 2 * NB; ++d) *reinterpret_cast<f32x4*>(a.part + at * D + d * 16 + 4 * g) = o[d];
                 if (g == 0) a.stat[at * 2] = all, a.stat[at * 2 + 1] = total;
@@ -260,63 +260,10 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
     }
 }
 
-// The parts of a row and head as one.
-template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    constexpr int E = (D + 63) / 64;
-    __shared__ float sums[4][D];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int count = row_count(a.tokens.count, a.tokens.rows);
-    const int q_heads = a.cache.heads * a.group;
-    for (int unit = blockIdx.x; unit < count * q_heads; unit += gridDim.x) {
-        const int r = unit / q_heads, q_head = unit % q_heads, head = q_head / a.group, in_group = q_head % a.group;
-        const int64_t first = ((((int64_t)r * a.cache.heads + head) * a.blocks + in_group / 16) * a.splits) * 16 + in_group % 16;
-        float top = -INFINITY;
-        for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.stat[(first + (int64_t)s * 16) * 2]);
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
-        const float base = top == -INFINITY ? 0.0f : top;
-        float total = 0.0f, o[E] = {};
-#pragma unroll 4
-        for (int s = wave; s < a.splits; s += 4) {
-            const int64_t at = first + (int64_t)s * 16;
-            const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
-            total += a.stat[at * 2 + 1] * w;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (lane + 64 * e < D) o[e] += a.part[at * D + lane + 64 * e] * w;
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
-        __shared__ float totals[4];
-        if (lane == 0) totals[wave] = total;
-        __syncthreads();
-        total = totals[0] + totals[1] + totals[2] + totals[3];
-        if ((int)threadIdx.x < D) {
-            const int d = threadIdx.x;
-            const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
-            static_cast<T*>(a.y)[(int64_t)r * a.ldy + (int64_t)q_head * D + d] = (T)(total == 0.0f ? 0.0f : v / total);
-        }
-        __syncthreads();
-    }
-}
-
-AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t length) {
-    AttendPlan p;
-    p.units = rows * heads * cdiv(q_heads / heads, 16);
-    const int64_t wanted = cdiv(2048, p.units < 1 ? 1 : p.units), most = cdiv(length, 256);
-    p.splits = (int)(wanted < most ? wanted : most);
-    return p;
-}
-
 template <typename T, int NB> static dcnn_status launch_few(dcnn_ctx* ctx, const AttendArgs& a) {
     const int64_t units = (int64_t)a.tokens.rows * a.cache.heads * a.blocks * a.splits, most = (int64_t)ctx->num_cu * 16;
     hipLaunchKernelGGL((attend_few_kernel<T, NB>), dim3((unsigned)(units < most ? units : most)), dim3(256), 0, ctx->stream, a);
-    dcnn_status st = check_hip(ctx, hipGetLastError(), "attend_few_kernel launch");
-    if (st != DCNN_OK || a.splits == 1) return st;
-    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group;
-    hipLaunchKernelGGL((attend_join_kernel<T, NB * 32>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);
-    return check_hip(ctx, hipGetLastError(), "attend_join_kernel launch");
+    return check_hip(ctx, hipGetLastError(), "attend_few_kernel launch");
 }
 template <typename T> static dcnn_status launch_few_t(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
     switch (dim) {
@@ -328,7 +275,7 @@ template <typename T> static dcnn_status launch_few_t(dcnn_ctx* ctx, int dim, co
         default: return launch_few<T, 8>(ctx, a);
     }
 }
-dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a) {
+dcnn_status launch_attend_few(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a) {
     if (dtype == DCNN_F16) return launch_few_t<f16>(ctx, dim, a);
     if (dtype == DCNN_BF16) return launch_few_t<bf16>(ctx, dim, a);
     return launch_few_t<float>(ctx, dim, a);

@@ -1,0 +1,327 @@
+// Attention over the cache for many rows of a stream.
+//
+//   S^T = K Q^T,  P = exp2(S * scale log2(e) - max),  Y^T = V^T P^T / sum P, the maximum and the sums kept up to date from tile to tile
+//
+// A workgroup has 128 vectors of queries (rows and the query heads of one head of keys, rows first), 32 to a wave: the columns of its operands.
+// It goes through the tokens that any of them sees, 64 at a time.  A tile's codes come in registers two tiles ahead, become operands in LDS
+// (two buffers) by conversions that take the scale, one tile ahead, and every wave multiplies all of them:
+//   * S^T: rows are tokens, so a lane has one column's products with 32 tokens, in registers; a column's maximum takes one exchange
+//     between lanes, and the weights are the second product's operand as they are, in the order of tokens that the first leaves;
+//   * V^T: values lie in LDS as rows of tokens and are read transposed, four tokens of a channel at a time, in that same order.
+// Rows of several streams in a tile of rows are taken one stream after the other ("segments": columns outside of it see nothing).
+// Matrix cores and exponentials share the time of a wave: the two workgroups of a compute unit overlap them.
+#include "attend_device.h"
+
+namespace dcnn {
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+constexpr int kVectors = 128, kTokens = 64;
+
+// 16-byte columns of a row of LDS (4 NB of them), permuted against bank conflicts.
+template <int NB> __device__ __forceinline__ int tile_column(int row, int col) {
+    if constexpr (NB == 1) return col ^ (row >> 1 & 3);
+    if constexpr (NB == 3) return col ^ (row >> 2 & 3);
+    if constexpr (NB == 6) return col ^ (row >> 1 & 7);
+    return col ^ (row & 7);
+}
+
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int o = __shfl_xor(v, d, kWave);
+        v = o < v ? o : v;
+    }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+template <typename T, int NB> struct TileShape {
+    // queries, sums, products and weights of a lane: two waves to a SIMD where they leave room for addresses and codes
+    static constexpr int registers = NB * 8 * Operand<T>::TERMS + NB * 16 + 32 + 16 * Operand<T>::TERMS;
+    static constexpr int waves = registers <= 176 ? 2 : 1;
+    static constexpr int bytes = 2 * 2 * kTokens * NB * 64;            // two buffers of keys and values
+};
+
+template <typename T, int NB>
+__global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_kernel(AttendArgs a) {
+    typedef Operand<T> O;
+    typedef typename O::type Op;
+    constexpr int D = NB * 32, ROW = D * 2, TERMS = O::TERMS, CHUNKS = (NB + 1) / 2, PLANE = kTokens * ROW;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    __shared__ int streams[kVectors], lows[kVectors], highs[kVectors];
+    __shared__ uint64_t broken[2][NB];                                 // blocks of values that are NaN: bit token * NB + block
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int count = row_count(a.tokens.count, a.tokens.rows);
+    const int vectors = count * a.group, tiles = (vectors + kVectors - 1) / kVectors, heads = a.cache.heads;
+    if (tiles == 0) return;
+    // a few tiles of rows: their segments to workgroups of their own
+    int turns = 512 / ((int64_t)tiles * heads * a.splits < 512 ? tiles * heads * a.splits : 512);
+    turns = turns < kVectors ? turns : kVectors;
+    const int page_mask = (1 << a.cache.page_shift) - 1;
+    const int64_t page_tokens = (int64_t)heads << a.cache.page_shift;
+    for (int64_t item = blockIdx.x; item < (int64_t)tiles * heads * a.splits * turns; item += gridDim.x) {
+        int rest = (int)(item / heads);
+        const int head = (int)(item % heads), part = rest % a.splits;
+        rest /= a.splits;
+        const int turn = rest % turns, place = rest / turns, tile = a.causal ? tiles - 1 - place : place;      // (later rows see more: they go first)
+        const int v = tile * kVectors + wave * 32 + col;
+        const bool active = v < vectors;
+        const int r = active ? (int)fast_div((uint32_t)v, a.by_group) : 0, in_group = active ? v - r * a.group : 0;
+        Token token = {-1, 0, false};
+        Span span = {0, 0};
+        if (active) {
+            token = token_of(a.tokens, r);
+            span = span_of(a, token);
+        }
+        const int stream = token.here && (uint32_t)token.stream < (uint32_t)a.cache.streams ? token.stream : -1;
+        if (half == 0) streams[wave * 32 + col] = stream, lows[wave * 32 + col] = span.lo, highs[wave * 32 + col] = span.hi;
+        // queries, as operands
+        Op q[2 * NB][TERMS];
+        const T* qp = static_cast<const T*>(a.q) + (int64_t)r * a.ldq + ((int64_t)head * a.group + in_group) * D + half * 8;
+#pragma unroll
+        for (int j = 0; j < 2 * NB; ++j) load_operand<T>(qp + j * 16, a.negate, q[j]);
+        f32x16 o[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
+        float top = -INFINITY, sum = 0.0f;
+        bool mine = false;
+        __syncthreads();
+        const uint64_t starts0 = __ballot(lane == 0 || streams[lane] != streams[lane == 0 ? 0 : lane - 1]), starts1 = __ballot(streams[lane + 64] != streams[lane + 63]);
+        int index = 0;
+        for (int begin = 0, end; begin < kVectors; begin = end, ++index) {
+            const uint64_t later0 = begin < 63 ? starts0 >> (begin + 1) : 0, later1 = begin < 63 ? starts1 : (begin < 127 ? starts1 >> (begin - 63) : 0);
+            end = later0 ? begin + 1 + __builtin_ctzll(later0) : (later1 ? (begin < 63 ? 64 : begin + 1) + __builtin_ctzll(later1) : kVectors);
+            if (index % turns != turn) continue;
+            const int at = wave * 32 + col;
+            const bool in_segment = at >= begin && at < end;
+            mine = mine || in_segment;
+            const int lo = in_segment ? span.lo : 0, hi = in_segment ? span.hi : 0;
+            int first = 0x7fffffff, last = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int w = lane + 64 * i;
+                if (w >= begin && w < end && lows[w] < highs[w]) {
+                    first = lows[w] < first ? lows[w] : first;
+                    last = highs[w] > last ? highs[w] : last;
+                }
+            }
+            first = wave_min(first), last = -wave_min(-last);
+            if (last <= first) continue;
+            const int of = __builtin_amdgcn_readfirstlane(streams[begin]);
+            // what all of the wave's columns see, and what any of them does
+            const int see_from = -wave_min(-(lo < hi ? lo : 0x7fffffff)), see_to = wave_min(hi);
+            const int any_from = wave_min(lo < hi ? lo : 0x7fffffff), any_to = -wave_min(-hi);
+            const int start = first & ~(kTokens - 1), all = (last - start + kTokens - 1) / kTokens, share = (all + a.splits - 1) / a.splits;
+            const int from = part * share, to = from + share < all ? from + share : all;
+            if (from >= to) continue;
+
+            // ---- codes of a tile: from memory, to operands in LDS
+            u32x4 raw[CHUNKS];
+            uint32_t byte[CHUNKS];
+            const auto page_at = [&](int t) { return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift); };
+            const auto load = [&](int t, int page) {
+#pragma unroll
+                for (int n = 0; n < CHUNKS; ++n) {
+                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = within / NB, b = within % NB, which = c / (kTokens * NB);
+                    if (NB % 2 != 0 && c >= 2 * kTokens * NB) break;
+                    const int p = __shfl(page, token_in / 16, kWave), t_at = start + t * kTokens + token_in;
+                    const int64_t slot = ((int64_t)(p < 0 ? 0 : p) * 2 + which) * page_tokens + ((int64_t)head << a.cache.page_shift) + (t_at & page_mask);
+                    raw[n] = *reinterpret_cast<const u32x4*>(a.cache.codes + slot * (D / 2) + b * 16);
+                    byte[n] = a.cache.scales[slot * NB + b];
+                    if (p < 0 || t_at < first || t_at >= last) byte[n] = 0;                            // (what lies there may be anything)
+                }
+            };
+            const auto stage = [&](int buffer) {
+#pragma unroll
+                for (int n = 0; n < CHUNKS; ++n) {
+                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = within / NB, b = within % NB, which = c / (kTokens * NB);
+                    if (NB % 2 != 0 && c >= 2 * kTokens * NB) break;
+                    // a value that is NaN is not multiplied (a weight of zero would make it one of rows that do not see it): it is noted
+                    const bool nan = which == 1 && byte[n] == 255;
+                    const uint64_t noted = __ballot(nan);
+                    if (which == 1 && lane == 0) broken[buffer][within / 64] = noted;
+                    const float scale = scale_of_byte(nan ? 0 : byte[n]);
+                    uint8_t* const row = lds + (buffer * 2 + which) * PLANE + token_in * ROW;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<Op*>(row + tile_column<NB>(token_in, 4 * b + i) * 16) = decode8<T>(raw[n][i], scale);
+                }
+            };
+            int page = page_at(from);
+            uint32_t paged[3] = {0, 0, 0};                             // which sixteens of tokens have a page: of this tile, the next, the one behind
+            const auto sixteens = [&](int p) { return (uint32_t)__ballot(p >= 0) & 15u; };
+            paged[0] = sixteens(page);
+            load(from, page);
+            page = page_at(from + 1);
+            __syncthreads();                                           // (a segment before this one is done with the buffers)
+            stage(from & 1);
+            paged[1] = sixteens(page);
+            if (from + 1 < to) {
+                load(from + 1, page);
+                page = page_at(from + 2);
+                paged[2] = sixteens(page);
+            }
+            for (int t = from; t < to; ++t) {
+                __syncthreads();                                       // this tile is there, and all are done with the one before it
+                if (t + 1 < to) stage((t + 1) & 1);
+                const uint32_t has_page = paged[0];
+                paged[0] = paged[1], paged[1] = paged[2];
+                if (t + 2 < to) {
+                    load(t + 2, page);
+                    page = page_at(t + 3);
+                    paged[2] = sixteens(page);
+                }
+                const int t0 = start + t * kTokens;
+                if (t0 + kTokens <= any_from || t0 >= any_to) continue;
+                const uint8_t* const keys = lds + (t & 1) * 2 * PLANE;
+                const uint8_t* const vals = keys + PLANE;
+                f32x16 s[2];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 2 * NB; ++j) {
+                        const int row = kb * 32 + col;
+                        const Op k = *reinterpret_cast<const Op*>(keys + row * ROW + tile_column<NB>(row, 2 * j + half) * 16);
+#pragma unroll
+                        for (int m = 0; m < TERMS; ++m) s[kb] = O::mfma32(k, q[j][m], s[kb]);
+                    }
+                }
+                // the column's product with token t0 + 32 kb + 8 (e / 4) + 4 half + e % 4
+                if (t0 < see_from || t0 + kTokens > see_to || has_page != 15u) {
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int in_tile = 32 * kb + 8 * (e / 4) + 4 * half + e % 4;
+                            const bool seen = (uint32_t)(t0 + in_tile - lo) < (uint32_t)(hi - lo) && (has_page >> (2 * kb + e / 8) & 1);
+                            s[kb][e] = seen ? s[kb][e] : -INFINITY;
+                        }
+                }
+                float m = s[0][0];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
+                m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                m = fmaxf(m * a.factor, top);                          // (the factor is above zero)
+                if (__any(m > top)) {
+                    const float factor = m > top ? __builtin_amdgcn_exp2f(top - m) : 1.0f;
+                    top = m;
+                    sum *= factor;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) o[b] *= factor;
+                }
+                const float base = top == -INFINITY ? 0.0f : top;
+                Op p[2][2][TERMS];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * u + e], a.factor, -base));
+                            sum += w[e];
+                        }
+                        O::split(w, p[kb][u]);
+                    }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            i16x4 x[2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int row = kb * 32 + 16 * u + 8 * i + 4 * half + lane % 16 / 4;
+                                const int c = 4 * b + lane % 32 / 16 * 2 + lane % 4 / 2;
+                                x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vals + row * ROW + tile_column<NB>(row, c) * 16 + lane % 2 * 8));
+                            }
+                            const Op k = __builtin_bit_cast(Op, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                            for (int n = 0; n < TERMS; ++n) o[b] = O::mfma32(k, p[kb][u][n], o[b]);
+                        }
+                uint64_t noted = 0;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) noted |= broken[t & 1][b];
+                if (noted != 0) {
+                    for (int w = 0; w < NB; ++w)
+                        for (uint64_t bits = broken[t & 1][w]; bits != 0; bits &= bits - 1) {
+                            const int bit = w * 64 + __builtin_ctzll(bits), in_tile = bit / NB;
+                            if ((uint32_t)(t0 + in_tile - lo) < (uint32_t)(hi - lo)) {
+#pragma unroll
+                                for (int b = 0; b < NB; ++b)
+                                    if (bit % NB == b) {
+#pragma unroll
+                                        for (int e = 0; e < 16; ++e) o[b][e] = __builtin_nanf("");
+                                    }
+                            }
+                        }
+                }
+            }
+        }
+        // sums of both halves' tokens; the column's channels 32 b + 8 (e / 4) + 4 half + e % 4
+        sum += __shfl_xor(sum, 32, kWave);
+        if (mine && active) {
+            if (a.splits == 1) {
+                T* y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + ((int64_t)head * a.group + in_group) * D + 4 * half;
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        typename RowQuad<T>::type w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = (T)(o[b][4 * i + e] * inv);
+                        *reinterpret_cast<typename RowQuad<T>::type*>(y + b * 32 + 8 * i) = w;
+                    }
+            } else {
+                const int64_t at = ((int64_t)r * heads * a.group + head * a.group + in_group) * a.splits + part;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4*>(a.part + at * D + b * 32 + 8 * i + 4 * half) = f32x4{o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]};
+                if (half == 0) a.stat[at * 2] = top, a.stat[at * 2 + 1] = sum;
+            }
+        }
+        __syncthreads();                                               // (streams and spans have been read)
+    }
+}
+
+template <typename T, int NB> static dcnn_status launch_tile(dcnn_ctx* ctx, const AttendArgs& a) {
+    constexpr int bytes = TileShape<T, NB>::bytes;
+    auto* const kern = &attend_tile_kernel<T, NB>;
+    if (bytes > 64 * 1024) {
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (err != hipSuccess) return check_hip(ctx, err, "hipFuncSetAttribute(attend_tile_kernel)");
+    }
+    const int64_t items = cdiv((int64_t)a.tokens.rows * a.group, kVectors) * a.cache.heads * a.splits;
+    // a list's length is not known here: workgroups stride through what there is
+    int64_t grid = items < 512 ? 512 : items;
+    if (a.tokens.count != nullptr && grid > 2048) grid = 2048;
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), bytes, ctx->stream, a);
+    return check_hip(ctx, hipGetLastError(), "attend_tile_kernel launch");
+}
+template <typename T> static dcnn_status launch_tile_t(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
+    switch (dim) {
+        case 32: return launch_tile<T, 1>(ctx, a);
+        case 64: return launch_tile<T, 2>(ctx, a);
+        case 96: return launch_tile<T, 3>(ctx, a);
+        case 128: return launch_tile<T, 4>(ctx, a);
+        case 192: return launch_tile<T, 6>(ctx, a);
+        default: return launch_tile<T, 8>(ctx, a);
+    }
+}
+dcnn_status launch_attend_tile(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a) {
+    if (dtype == DCNN_F16) return launch_tile_t<f16>(ctx, dim, a);
+    if (dtype == DCNN_BF16) return launch_tile_t<bf16>(ctx, dim, a);
+    return launch_tile_t<float>(ctx, dim, a);
+}
+
+}  // namespace dcnn

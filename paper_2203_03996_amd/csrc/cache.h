@@ -54,17 +54,22 @@ struct AttendArgs {
     int64_t ldq, ldy;
     int group;                                 // query heads of a head of keys
     int blocks;                                // sixteens of them
-    float factor;                              // scale * log2(e)
+    float factor;                              // |scale| * log2(e), above zero
+    int negate;                                // scale is below zero: the queries' opposites
     int causal, window;
     const int32_t* lens;
+    FastDiv by_group;
     int splits;                                // workgroups that share a row's tokens
-    float *part, *stat;                        // with splits: sums [unit][split][16][dim], maxima and sums of weights [unit][split][16][2]
+    float *part, *stat;                        // with splits: sums [row][query head][split][dim], maxima and sums of weights [row][query head][split][2]
 };
+// Which kernel: a function of the sizes alone.
 struct AttendPlan {
+    bool tiles;                                // rows of one stream share its tiles of tokens
     int splits;
-    int64_t units;                             // rows (at most) * heads * blocks
 };
-AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t length);
-dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);
+AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t streams, int64_t length);
+dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendPlan& plan, const AttendArgs& a);
+dcnn_status launch_attend_few(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);
+dcnn_status launch_attend_tile(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);
 
 }  // namespace dcnn

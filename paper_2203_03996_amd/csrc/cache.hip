@@ -161,9 +161,9 @@ dcnn_status dcnn_cache_read(dcnn_ctx* ctx, const dcnn_cache_read_args* p) {
 size_t dcnn_cache_scratch_bytes(int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length) {
     if (rows < 0 || rows > kRowsMax || heads < 1 || q_heads < 1 || q_heads % heads != 0 || !cache_dim(dim) || length < 1 || length > kCacheMaxLength || streams < 1) return 0;
     if (rows * q_heads > kMaxHeadRows) return 0;
-    const AttendPlan plan = attend_plan(rows, q_heads, heads, length);
-    const int64_t parts = plan.splits > 1 ? plan.units * plan.splits : 0;
-    return align_up((size_t)parts * 16 * (size_t)(dim + 2) * sizeof(float) + kAlign);
+    const AttendPlan plan = attend_plan(rows, q_heads, heads, streams, length);
+    const int64_t parts = plan.splits > 1 ? rows * q_heads * plan.splits : 0;
+    return align_up((size_t)parts * (size_t)(dim + 2) * sizeof(float) + kAlign);
 }
 
 dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
@@ -194,16 +194,19 @@ dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
                          vector_bytes("lens", p->lens_dev, p->cache.streams * 4)};
     st = check_apart(ctx, what, outs, ins);
     if (st != DCNN_OK) return st;
-    const AttendPlan plan = attend_plan(rows, p->q_heads, p->cache.heads, p->cache.length);
+    const AttendPlan plan = attend_plan(rows, p->q_heads, p->cache.heads, p->cache.streams, p->cache.length);
     a.q = p->q_dev, a.y = p->y_dev, a.ldq = p->ldq, a.ldy = p->ldy;
     a.group = p->q_heads / p->cache.heads, a.blocks = (int)cdiv(a.group, 16);
-    a.factor = p->scale * 1.44269504088896341f;
+    // (a scale of zero: so small a number that any product with it is as good as zero, and what is masked, minus infinity, stays that)
+    a.factor = __builtin_fabsf(p->scale) * 1.44269504088896341f, a.negate = p->scale < 0.0f;
+    if (a.factor == 0.0f) a.factor = 0x1p-149f;
     a.causal = p->causal != 0, a.window = (int)(p->window < kCacheMaxLength ? p->window : kCacheMaxLength);
     a.lens = p->lens_dev;
+    a.by_group = make_fastdiv((uint32_t)a.group);
     a.splits = plan.splits;
     a.stat = static_cast<float*>(p->scratch_dev);
-    a.part = a.stat + align_up((size_t)plan.units * plan.splits * 32, 64);
-    return launch_attend(ctx, p->cache.dtype, p->cache.dim, a);
+    a.part = a.stat + align_up((size_t)(rows * p->q_heads) * plan.splits * 2, 64);
+    return launch_attend(ctx, p->cache.dtype, p->cache.dim, plan, a);
 }
 
 }  // extern "C"

@@ -125,14 +125,16 @@ __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float scale) {
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
     return w;
 }
+// The largest scale: what is held of a block stays finite in the cache's type (6 * 2^13 in fp16; a larger magnitude is held as that).
+template <typename T> constexpr int kMaxScale = std::is_same_v<T, f16> ? 13 : 125;
 // (codes, scale byte) of a lane's eight values; the four lanes of a block agree on the byte.
-__device__ __forceinline__ uint32_t encode(const double (&v)[8], uint32_t* byte) {
+template <int MOST> __device__ __forceinline__ uint32_t encode(const double (&v)[8], uint32_t* byte) {
     const double amax = block_amax(v);
     const uint64_t bits = __builtin_bit_cast(uint64_t, amax);
     const int exponent = (int)(bits >> 52) - 1023;
     const uint64_t mantissa = bits & 0xfffffffffffffull;
     int e = exponent - (mantissa <= 0x8000000000000ull ? 2 : 1);       // amax = m 2^exponent: m <= 1.5 fits 6 * 2^(exponent - 2)
-    e = e < -126 ? -126 : (e > 127 ? 127 : e);
+    e = e < -126 ? -126 : (e > MOST ? MOST : e);
     *byte = exponent == 1024 ? 255u : (uint32_t)(e + 127);
     if (exponent == 1024) return 0u;
     const double inv = __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
@@ -144,14 +146,14 @@ __device__ __forceinline__ uint32_t encode(const double (&v)[8], uint32_t* byte)
     }
     return codes_of(u, 1.0f);
 }
-__device__ __forceinline__ uint32_t encode(const float (&v)[8], uint32_t* byte) {
+template <int MOST> __device__ __forceinline__ uint32_t encode(const float (&v)[8], uint32_t* byte) {
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
     m = wave_reduce<MaxOp, 4>(m);
     const int exponent = (int)(m >> 23) - 127;
     int e = exponent - ((m & 0x7fffffu) <= 0x400000u ? 2 : 1);
-    e = e < -126 ? -126 : e;
+    e = e < -126 ? -126 : (e > MOST ? MOST : e);
     *byte = m >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
     if (m >= 0x7f800000u) return 0u;
     return codes_of(v, scale_of_byte((uint32_t)(e + 127)));
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a) {
                 if (both) load8<T>(x + partner, other);
                 if (OP == kAppendHeads && which == 1) {
                     uint32_t byte;
-                    const uint32_t w = encode(raw, &byte);
+                    const uint32_t w = encode<kMaxScale<T>>(raw, &byte);
                     if (here && in) {
                         const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
                         *reinterpret_cast<uint32_t*>(a.cache.codes + s * (D / 2) + lane * 4) = w;
@@ -267,7 +269,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a) {
                     if (live && in) store8<T>(static_cast<T*>(job.out) + r * job.ld_out + h * D + at, v);
                 } else {
                     uint32_t byte;
-                    const uint32_t w = encode(v, &byte);
+                    const uint32_t w = encode<kMaxScale<T>>(v, &byte);
                     if (here && in) {
                         const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
                         *reinterpret_cast<uint32_t*>(a.cache.codes + s * (D / 2) + lane * 4) = w;

@@ -26,16 +26,16 @@ def heads64(x, dim, kind="none", w=None, b=None, eps=0.0, table=None, style="hal
     return v, mag
 
 
-def quantised(v):
-    """(codes uint8 [..., n], scale bytes [..., n / 32]) of values in 64 bits: every candidate is looked at."""
+def quantised(v, most=125):
+    """(codes uint8 [..., n], scale bytes [..., n / 32]) of values in 64 bits: every candidate is looked at.  most: the largest exponent of a scale."""
     blocks = v.double().unflatten(-1, (-1, 32))
     amax = blocks.abs().amax(-1)
     broken = ~torch.isfinite(blocks).all(-1)
     e = torch.full(amax.shape, -126, dtype=torch.int64, device=v.device)
-    for k in range(-125, 128):
+    for k in range(-125, most + 1):
         e[amax > 6.0 * 2.0 ** (k - 1)] = k
     u = torch.where(broken[..., None], torch.zeros_like(blocks), blocks * torch.exp2(-e[..., None].double()))  # (codes of a broken block are zeros)
-    grid = GRID.to(v.device)
+    grid, u = GRID.to(v.device), u.clamp(-6.0, 6.0)
     off = (u.abs()[..., None] - grid).abs()
     best = off.amin(-1, keepdim=True)
     near = off == best

@@ -80,8 +80,8 @@ dcnn_status fail(dcnn_ctx* ctx, dcnn_status s, const char* fmt, ...) {
     return s;
 }
 dcnn_status launch_heads(dcnn_ctx*, int, int, HeadsOp, HeadsArgs) { ++launches; return DCNN_OK; }
-dcnn_status launch_attend(dcnn_ctx*, int, int, const AttendArgs&) { ++launches; return DCNN_OK; }
-AttendPlan attend_plan(int64_t, int, int, int64_t) { return AttendPlan(); }
+dcnn_status launch_attend(dcnn_ctx*, int, int, const AttendPlan&, const AttendArgs&) { ++launches; return DCNN_OK; }
+AttendPlan attend_plan(int64_t, int, int, int64_t, int64_t) { return AttendPlan(); }
 }
 extern "C" {
 dcnn_ctx ctx_of_tests;
