@@ -437,7 +437,7 @@ typedef struct {
 /* Writes the keys (normed and rotated first) and values of rows into the cache.  The scale of 32 values is the smallest
  * power of two with max|v| <= 6 * scale (2^-126 at least; at most 2^13 in fp16 and 2^125 else, so that what is held is
  * finite: larger magnitudes are held as 6 * scale), and each becomes the code next to v / scale, ties to the even one (a
- * zero keeps its sign); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
+ * zero is code 0); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
  * order of a sum.  Rows without a token, or with a position outside 0 .. length-1, write nothing.  The (stream, position)
  * of rows must be distinct.  rows * heads at most 2^30. */
 typedef struct {

@@ -42,9 +42,9 @@ struct HeadsArgs {
     CacheArgs cache;                           // append, read
     RotationArgs rotation;                     // of both jobs' heads (kTurnHeads), of the keys (kAppendHeads)
     HeadJob job[2];                            // queries and keys, or keys and values
-    int chunk, chunks[2];                      // heads that a workgroup takes one after the other, and how many such parts a job has
+    int jobs, shift;                           // 2^shift heads of a row are side by side in a workgroup at most (filled in at the launch)
 };
-dcnn_status launch_heads(dcnn_ctx* ctx, int dtype, int dim, HeadsOp op, HeadsArgs a);
+dcnn_status launch_heads(dcnn_ctx* ctx, int dtype, int dim, HeadsOp op, const HeadsArgs& a);
 
 struct AttendArgs {
     TokenArgs tokens;

@@ -5,8 +5,7 @@
 //
 // A head's D values lie in the registers of D / 8 lanes (eight to a lane), its statistics and a block's largest magnitude are lane
 // permutations, and a value's partner in a rotation by halves is read again (from the L1) rather than passed between lanes.  A workgroup
-// takes 256 / L rows and goes through some of their heads, so a row's position, page, angles and a norm's parameters are read once.
-// Rows beside each other are tokens beside each other, as a rule: the few bytes of a head and token fill whole lines of the cache.
+// takes some rows and up to eight heads of each side by side.
 // Keys are fp64 from the norm to the code (their cost hides behind the memory): a code is the same whatever the order of a sum.
 #include "cache_device.h"
 
@@ -48,133 +47,200 @@ template <int L> __device__ __forceinline__ double sum_lanes(double v) {
     if constexpr (L >= 32) v += __shfl_xor(v, 16, kWave);
     return v;
 }
-// Largest magnitude of a block of 32, over its four lanes; an infinity where there is one or a NaN.
-__device__ __forceinline__ double block_amax(const double (&v)[8]) {
-    double m = 0.0;
+// Eight values of a head as they lie, and those that they meet in the rotation.
+template <typename T> struct Raw8 {
+    static constexpr int N = (int)sizeof(T) / 2;
+    u32x4 v[N];
+    __device__ __forceinline__ void read(const T* p, bool take) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const double a = __builtin_fabs(v[e]);
-        m = a <= 1.7976931348623157e308 ? (a > m ? a : m) : __builtin_inf();
+        for (int i = 0; i < N; ++i) v[i] = take ? __builtin_bit_cast(u32x4, *reinterpret_cast<const typename RowVec<T>::type*>(p + i * RowVec<T>::E)) : u32x4{0u, 0u, 0u, 0u};
     }
-    const double n = dpp64<0xB1>(m);
-    m = n > m ? n : m;
-    const double o = dpp64<0x4E>(m);
-    return o > m ? o : m;
-}
-
-// A head's eight values of a lane, normed: what stays the same for all heads of a job.
-template <typename T> struct HeadNorm {
-    int kind;
-    float eps;
-    const T *w, *b;
+    // neighbours exchanged
+    __device__ __forceinline__ Raw8 crossed(bool take) const {
+        Raw8 r;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t w = sizeof(T) == 2 ? v[i][e] << 16 | v[i][e] >> 16 : v[i][e ^ 1];
+                r.v[i][e] = take ? w : 0u;
+            }
+        return r;
+    }
+    __device__ __forceinline__ float at(int e) const { return row_get<T>(v[e / RowVec<T>::E], e % RowVec<T>::E); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = at(e);
+    }
 };
-// v (and p, the partners' values, where `both`) <- norm.  Lanes behind the head (`!in`) hold zeros.
-template <typename T, typename A, int D, int L>
-__device__ __forceinline__ void norm_head(A (&v)[8], A (&p)[8], bool both, const HeadNorm<T>& n, int at, int partner, bool in) {
-    if (n.kind == DCNN_NORM_NONE) return;
-    A mean = 0;
-    if (n.kind == DCNN_NORM_LAYER) {
-        A s = 0;
+
+// Where a lane's values lie, and their partners: the same for all heads of a row.
+struct Place {
+    int at, partner;
+    bool in, here, turned, halves;             // in the head; the row has a token; rotated; by halves
+};
+// Norm and rotation as one: out = r (x - mean) a + r (partner - mean) b + c, with r and mean of the head.
+template <typename A> struct Turn {
+    A a[8], b[8];
+    float c[8];
+};
+template <typename T, typename A>
+__device__ __forceinline__ void turn_of(Turn<A>& f, const RotationArgs& rot, int pos, const HeadJob& job, const Place& at) {
+    float cs[8], sn[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += v[e];
-        mean = sum_lanes<L>(s) / (A)D;
+    for (int e = 0; e < 8; ++e) cs[e] = 1, sn[e] = 0;
+    if (at.turned) {
+        const int half = rot.rot / 2;
+        const bool second = at.at >= half;
+        const float* t = rot.table + (int64_t)pos * rot.rot;
+        float pair[16];
+        if (at.halves) {
+            t += (second ? at.at - half : at.at) * 2;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(pair + i) = *reinterpret_cast<const f32x4*>(t + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = pair[2 * e], sn[e] = second ? pair[2 * e + 1] : -pair[2 * e + 1];
+        } else {
+            t += at.at;
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) *reinterpret_cast<f32x4*>(pair + i) = *reinterpret_cast<const f32x4*>(t + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = pair[e & ~1], sn[e] = e % 2 ? pair[e | 1] : -pair[e | 1];
+        }
     }
-    A s = 0;
+    const auto weigh = [&](const void* params, float (&own)[8], float (&other)[8], float none) {
+        const T* p = static_cast<const T*>(params);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        v[e] = in ? v[e] - mean : (A)0;
-        s += v[e] * v[e];
+        for (int e = 0; e < 8; ++e) own[e] = none, other[e] = none;
+        if (p == nullptr || !at.in) return;
+        load8<T>(p + at.at, own);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) other[e] = own[e ^ 1];
+        if (at.halves) load8<T>(p + at.partner, other);
+    };
+    float own[8], other[8];
+    weigh(job.w, own, other, 1.0f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.a[e] = (A)own[e] * (A)cs[e], f.b[e] = (A)other[e] * (A)sn[e];
+    // (in fp64 a bias is read where it is used: few norms have one)
+    if constexpr (sizeof(A) == 4) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.c[e] = 0.0f;
+        if (job.b == nullptr) return;
+        weigh(job.b, own, other, 0.0f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.c[e] = own[e] * cs[e] + other[e] * sn[e];
     }
-    A r;
-    if constexpr (sizeof(A) == 8) r = 1.0 / sqrt(sum_lanes<L>(s) / (A)D + (A)n.eps);
-    else r = 1.0f / sqrtf(sum_lanes<L>(s) / (A)D + n.eps);
-    float w[8];
-    if (n.w != nullptr && in) load8<T>(n.w + at, w);
+}
+// Element e's part of the bias, in fp64.
+template <typename T> __device__ __forceinline__ double bias64(const RotationArgs& rot, int pos, const HeadJob& job, const Place& at, int e) {
+    const T* const b = static_cast<const T*>(job.b);
+    if (!at.in) return 0.0;
+    const int own = at.at + e;
+    if (!at.turned) return (double)(float)b[own];
+    const bool second = at.at >= rot.rot / 2;
+    const float* const pair = rot.table + (int64_t)pos * rot.rot + (at.halves ? (second ? own - rot.rot / 2 : own) * 2 : own & ~1);
+    const double o = (double)(float)b[at.halves ? at.partner + e : own ^ 1] * (double)pair[1];
+    return (double)(float)b[own] * (double)pair[0] + ((at.halves ? !second : e % 2 == 0) ? -o : o);
+}
+// r of a head; x and p less its mean.  A row without a token: zero.
+template <int D, int L> __device__ __forceinline__ float centre(float (&x)[8], float (&p)[8], const HeadJob& job, const Place& at) {
+    if (job.norm == DCNN_NORM_NONE) return 1.0f;
+    if (job.norm == DCNN_NORM_LAYER) {
+        float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= n.w != nullptr && in ? r * (A)w[e] : r;
-    if (n.b != nullptr && in) {
-        load8<T>(n.b + at, w);
+        for (int e = 0; e < 8; ++e) s += x[e];
+        const float mean = sum_lanes<L>(s) * (1.0f / (float)D);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += (A)w[e];
+        for (int e = 0; e < 8; ++e) x[e] = at.in ? x[e] - mean : 0.0f, p[e] -= mean;
     }
-    if (!both) return;
-    if (n.w != nullptr) load8<T>(n.w + partner, w);
+    float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = (p[e] - mean) * (n.w != nullptr ? r * (A)w[e] : r);
-    if (n.b != nullptr) {
-        load8<T>(n.b + partner, w);
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], x[e], s);
+    const float r = rsqrtf(sum_lanes<L>(s) * (1.0f / (float)D) + job.eps);
+    return at.here ? r : 0.0f;
+}
+// The same in fp64: r and the mean of values as they lie.  (They are converted where they are used: eight fp64 values more in registers, and the
+// compiler spills some: 26240 rows of 8 x 64 took 83 us.)
+template <typename T, int D, int L> __device__ __forceinline__ double centre64(const Raw8<T>& x, const HeadJob& job, const Place& at, double* mean) {
+    *mean = 0.0;
+    if (job.norm == DCNN_NORM_NONE) return 1.0;
+    double s = 0.0;
+    if (job.norm == DCNN_NORM_LAYER) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] += (A)w[e];
+        for (int e = 0; e < 8; ++e) s += (double)x.at(e);
+        *mean = sum_lanes<L>(s) * (1.0 / (double)D);
+        s = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double d = at.in ? (double)x.at(e) - *mean : 0.0;
+            s = __builtin_fma(d, d, s);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = __builtin_fma((double)x.at(e), (double)x.at(e), s);
     }
+    return rsqrt(sum_lanes<L>(s) * (1.0 / (double)D) + (double)job.eps);
 }
 
-// Eight values in [-6, 6] of a block's multiples, in fp64, as codes.  They are cut to fp32 with the last bit set where something was
-// cut off ("to odd"), so that the conversion's rounding is that of the fp64 value.  (Below 1/8 every one is a zero.)
-__device__ __forceinline__ float to_odd(double u) {
-    const uint64_t bits = __builtin_bit_cast(uint64_t, u);
-    const uint32_t hi = (uint32_t)(bits >> 32), lo = (uint32_t)bits;
-    const uint32_t mag = ((hi << 3 | lo >> 29) - (896u << 23)) & 0x7fffffffu;  // exponent with the bias of fp32
-    const uint32_t f = mag | ((lo & 0x1fffffffu) != 0 ? 1u : 0u) | (hi & 0x80000000u);
-    return __builtin_bit_cast(float, __builtin_fabs(u) < 0.125 ? hi & 0x80000000u : f);
+// An fp64 value as the fp32 one next to zero of it, with the last bit set where something was cut off ("to odd"): rounding that to a code, and
+// comparing it with a border, is rounding and comparing the fp64 value.  Magnitudes below 2^-126 become zero, from 2^128 on infinity.
+__device__ __forceinline__ float to_odd(double v) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t hi = (uint32_t)(bits >> 32), lo = (uint32_t)bits, rest = lo & 0x1fffffffu;
+    const uint32_t f = ((hi << 3 | lo >> 29) - (896u << 23)) & 0x7fffffffu;    // exponent with the bias of fp32
+    const uint32_t odd = f | (rest < 1u ? rest : 1u) | (hi & 0x80000000u);
+    const uint32_t size = hi & 0x7fffffffu;
+    return size < 0x38100000u ? 0.0f : __builtin_bit_cast(float, size < 0x47f00000u ? odd : 0x7f800000u);
 }
+// (a zero is code 0, whatever its sign was)
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float scale) {
     uint32_t w = 0;
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
-    return w;
+    const uint32_t m = w & 0x77777777u;
+    return m | (w & ((m << 1 | m << 2 | m << 3) & 0x88888888u));
 }
 // The largest scale: what is held of a block stays finite in the cache's type (6 * 2^13 in fp16; a larger magnitude is held as that).
 template <typename T> constexpr int kMaxScale = std::is_same_v<T, f16> ? 13 : 125;
-// (codes, scale byte) of a lane's eight values; the four lanes of a block agree on the byte.
-template <int MOST> __device__ __forceinline__ uint32_t encode(const double (&v)[8], uint32_t* byte) {
-    const double amax = block_amax(v);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, amax);
-    const int exponent = (int)(bits >> 52) - 1023;
-    const uint64_t mantissa = bits & 0xfffffffffffffull;
-    int e = exponent - (mantissa <= 0x8000000000000ull ? 2 : 1);       // amax = m 2^exponent: m <= 1.5 fits 6 * 2^(exponent - 2)
-    e = e < -126 ? -126 : (e > MOST ? MOST : e);
-    *byte = exponent == 1024 ? 255u : (uint32_t)(e + 127);
-    if (exponent == 1024) return 0u;
-    const double inv = __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
-    float u[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const double x = v[i] * inv;                                   // (a power of two: exact)
-        u[i] = __builtin_fabs(x) > 6.0 ? (x < 0.0 ? -6.0f : 6.0f) : to_odd(x);
-    }
-    return codes_of(u, 1.0f);
+// Exponent of the scale of a block: the largest magnitude is m 2^k, and m <= 1.5 fits 6 * 2^(k - 2).
+template <int MOST> __device__ __forceinline__ int scale_exponent(int k, bool small) {
+    const int e = k - (small ? 2 : 1);
+    return e < -126 ? -126 : (e > MOST ? MOST : e);
 }
+// (codes, scale byte) of a lane's eight values; the four lanes of a block agree on the byte.
 template <int MOST> __device__ __forceinline__ uint32_t encode(const float (&v)[8], uint32_t* byte) {
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = MaxOp::op(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
     m = wave_reduce<MaxOp, 4>(m);
-    const int exponent = (int)(m >> 23) - 127;
-    int e = exponent - ((m & 0x7fffffu) <= 0x400000u ? 2 : 1);
-    e = e < -126 ? -126 : (e > MOST ? MOST : e);
+    const int e = scale_exponent<MOST>((int)(m >> 23) - 127, (m & 0x7fffffu) <= 0x400000u);
     *byte = m >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
     if (m >= 0x7f800000u) return 0u;
     return codes_of(v, scale_of_byte((uint32_t)(e + 127)));
 }
 
-template <typename T, int D, HeadsOp OP>
-__global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a) {
+// BIAS: a norm of appended keys has one (a kernel of its own: the others need not its registers).
+template <typename T, int D, HeadsOp OP, bool BIAS = false>
+__global__ __launch_bounds__(256, OP == kAppendHeads && !BIAS ? 4 : 1) void heads_kernel(HeadsArgs a) {
     constexpr int L = D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32, R = 256 / L;
     const int lane = threadIdx.x % L, sub = threadIdx.x / L;
     const bool in = lane * 8 < D;
     const int at = in ? lane * 8 : 0;
     const int count = row_count(a.tokens.count, a.tokens.rows);
-    const int chunks = a.chunks[0] + a.chunks[1];
     const RotationArgs& rot = a.rotation;
-    const int64_t items = (int64_t)((count + R - 1) / R) * chunks;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int tile = (int)(item / chunks), part = (int)(item % chunks);
-        const int which = part >= a.chunks[0];
+    // 2^shift heads of a row side by side: two, so that what belongs to the row serves many, and as many as there are where workgroups are left
+    int shift = a.shift;
+    while (shift > 1 && (int64_t)((count + (R >> shift) - 1) / (R >> shift)) * a.jobs > (int)gridDim.x) --shift;
+    const int rows = R >> shift, stride = 1 << shift, h0 = sub & (stride - 1);
+    const int tiles = (count + rows - 1) / rows;
+    // one job before the other: what one costs is not what the other does, and workgroups that follow each other go to different L2 caches
+    for (int64_t item = blockIdx.x; item < (int64_t)tiles * a.jobs; item += gridDim.x) {
+        const int which = item >= tiles, tile = (int)(which ? item - tiles : item);
         const HeadJob& job = a.job[which];
-        const int first = (part - (which ? a.chunks[0] : 0)) * a.chunk, last = first + a.chunk < job.heads ? first + a.chunk : job.heads;
-        const int64_t r = (int64_t)tile * R + sub;
+        const int64_t r = (int64_t)tile * rows + (sub >> shift);
         const bool live = r < count;
         Token token = {0, 0, false};
         if (live) token = token_of(a.tokens, (int)r);
@@ -189,8 +255,14 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a) {
             here = page >= 0;
             slot = head_of_page(a.cache, here ? page : 0, which, 0) + (token.pos & ((1 << a.cache.page_shift) - 1));
         }
+        const auto put = [&](int h, uint32_t words, uint32_t byte, bool take) {
+            const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
+            if (!take) return;
+            *reinterpret_cast<uint32_t*>(a.cache.codes + s * (D / 2) + lane * 4) = words;
+            if (lane % 4 == 0) a.cache.scales[s * (D / 32) + lane / 4] = (uint8_t)byte;
+        };
         if constexpr (OP == kReadHeads) {
-            for (int h = first; h < last; ++h) {
+            for (int h = h0; h < job.heads; h += stride) {
                 const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
                 float v[8] = {};
                 if (here && in) {
@@ -207,85 +279,71 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a) {
                 }
                 if (live && in) store8<T>(static_cast<T*>(job.out) + r * job.ld_out + h * D + at, v);
             }
-        } else {
-            // angles: out = v * cs + partner * sn
-            typedef std::conditional_t<OP == kAppendHeads, double, float> A;
-            float cs[8], sn[8];
-            int partner = at;
-            const bool turned = turns && here && in && at < rot.rot;
-            const bool halves = rot.style == DCNN_ROT_HALVES;
-            if (turned) {
-                const int half = rot.rot / 2;
-                const bool second = at >= half;
-                const float* t = rot.table + (int64_t)token.pos * rot.rot;
-                float pair[16];
-                if (halves) {
-                    partner = second ? at - half : at + half;
-                    const float* p = t + (second ? at - half : at) * 2;
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(pair + i) = *reinterpret_cast<const f32x4*>(p + i);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) cs[e] = pair[2 * e], sn[e] = second ? pair[2 * e + 1] : -pair[2 * e + 1];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4) *reinterpret_cast<f32x4*>(pair + i) = *reinterpret_cast<const f32x4*>(t + at + i);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) cs[e] = pair[e & ~1], sn[e] = e % 2 ? pair[e | 1] : -pair[e | 1];
-                }
+            continue;
+        }
+        Place place;
+        place.at = at, place.in = in, place.here = here;
+        place.halves = rot.style == DCNN_ROT_HALVES;
+        place.turned = turns && here && in && at < rot.rot;
+        place.partner = !place.turned || !place.halves ? at : (at >= rot.rot / 2 ? at - rot.rot / 2 : at + rot.rot / 2);
+        const T* const source = static_cast<const T*>(job.in) + r * job.ld_in;
+        if (OP == kAppendHeads && which == 1) {                // values: exact as they are
+            for (int h = h0; h < job.heads; h += stride) {
+                Raw8<T> raw;
+                raw.read(source + h * D + at, here && in);
+                float x[8];
+                raw.get(x);
+                uint32_t byte;
+                const uint32_t words = encode<kMaxScale<T>>(x, &byte);
+                put(h, words, byte, here && in);
             }
-            const HeadNorm<T> norm = {job.norm, job.eps, static_cast<const T*>(job.w), static_cast<const T*>(job.b)};
-            for (int h = first; h < last; ++h) {
-                const T* x = static_cast<const T*>(job.in) + r * job.ld_in + h * D;
-                float raw[8] = {}, other[8] = {};
-                const bool both = turned && halves;
-                if (here && in) load8<T>(x + at, raw);
-                if (both) load8<T>(x + partner, other);
-                if (OP == kAppendHeads && which == 1) {
-                    uint32_t byte;
-                    const uint32_t w = encode<kMaxScale<T>>(raw, &byte);
-                    if (here && in) {
-                        const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
-                        *reinterpret_cast<uint32_t*>(a.cache.codes + s * (D / 2) + lane * 4) = w;
-                        if (lane % 4 == 0) a.cache.scales[s * (D / 32) + lane / 4] = (uint8_t)byte;
-                    }
-                    continue;
+            continue;
+        }
+        typedef std::conditional_t<OP == kAppendHeads, double, float> A;
+        Turn<A> turn;
+        turn_of<T>(turn, rot, token.pos, job, place);
+        for (int h = h0; h < job.heads; h += stride) {
+            Raw8<T> raw, met;
+            raw.read(source + h * D + at, here && in);
+            met = raw.crossed(place.turned);
+            if (place.halves) met.read(source + h * D + place.partner, place.turned);
+            float o[8];
+            if constexpr (OP == kAppendHeads) {
+                double mean;
+                const double scale = centre64<T, D, L>(raw, job, place, &mean);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    double v = (double)raw.at(e) * turn.a[e] + (double)met.at(e) * turn.b[e];
+                    if (job.norm == DCNN_NORM_LAYER) v -= mean * (turn.a[e] + turn.b[e]);
+                    v *= scale;
+                    if constexpr (BIAS) v += bias64<T>(rot, token.pos, job, place, e);
+                    o[e] = to_odd(v);
                 }
-                A v[8], p[8];
+                uint32_t byte;
+                const uint32_t words = encode<kMaxScale<T>>(o, &byte);
+                put(h, words, byte, here && in);
+            } else {
+                float x[8], p[8];
+                raw.get(x), met.get(p);
+                const float scale = centre<D, L>(x, p, job, place);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = raw[e], p[e] = other[e];
-                norm_head<T, A, D, L>(v, p, both, norm, at, partner, in);
-                if (turned) {
-                    A o[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = v[e] * (A)cs[e] + (halves ? p[e] : v[e ^ 1]) * (A)sn[e];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = o[e];
-                }
-                if constexpr (OP == kTurnHeads) {
-                    if (!here) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-                    }
-                    if (live && in) store8<T>(static_cast<T*>(job.out) + r * job.ld_out + h * D + at, v);
-                } else {
-                    uint32_t byte;
-                    const uint32_t w = encode<kMaxScale<T>>(v, &byte);
-                    if (here && in) {
-                        const int64_t s = slot + ((int64_t)h << a.cache.page_shift);
-                        *reinterpret_cast<uint32_t*>(a.cache.codes + s * (D / 2) + lane * 4) = w;
-                        if (lane % 4 == 0) a.cache.scales[s * (D / 32) + lane / 4] = (uint8_t)byte;
-                    }
-                }
+                for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(scale, __builtin_fmaf(p[e], turn.b[e], x[e] * turn.a[e]), turn.c[e]);
+                if (live && in) store8<T>(static_cast<T*>(job.out) + r * job.ld_out + h * D + at, o);
             }
         }
     }
 }
 
-template <typename T, int D> static dcnn_status launch_heads_dim(dcnn_ctx* ctx, HeadsOp op, const HeadsArgs& a) {
+template <typename T, int D> static dcnn_status launch_heads_dim(dcnn_ctx* ctx, HeadsOp op, HeadsArgs a) {
     constexpr int L = D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32;
-    const int64_t items = cdiv(a.tokens.rows, 256 / L) * (a.chunks[0] + a.chunks[1]), most = (int64_t)ctx->num_cu * 8;
+    const int most_heads = a.job[0].heads > a.job[1].heads ? a.job[0].heads : a.job[1].heads;
+    a.shift = 0;
+    while ((2 << a.shift) <= 256 / L && 1 << a.shift < most_heads) ++a.shift;
+    a.jobs = a.job[1].heads > 0 ? 2 : 1;
+    const int64_t items = cdiv(a.tokens.rows, 256 / L >> a.shift) * a.jobs, most = (int64_t)ctx->num_cu * 8;
     const dim3 grid((unsigned)(items < most ? items : most));
     if (op == kTurnHeads) hipLaunchKernelGGL((heads_kernel<T, D, kTurnHeads>), grid, dim3(256), 0, ctx->stream, a);
+    else if (op == kAppendHeads && a.job[0].b != nullptr) hipLaunchKernelGGL((heads_kernel<T, D, kAppendHeads, true>), grid, dim3(256), 0, ctx->stream, a);
     else if (op == kAppendHeads) hipLaunchKernelGGL((heads_kernel<T, D, kAppendHeads>), grid, dim3(256), 0, ctx->stream, a);
     else hipLaunchKernelGGL((heads_kernel<T, D, kReadHeads>), grid, dim3(256), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "heads_kernel launch");
@@ -301,12 +359,7 @@ template <typename T> static dcnn_status launch_heads_t(dcnn_ctx* ctx, int dim, 
     }
 }
 
-dcnn_status launch_heads(dcnn_ctx* ctx, int dtype, int dim, HeadsOp op, HeadsArgs a) {
-    const int lanes = dim <= 32 ? 4 : dim <= 64 ? 8 : dim <= 128 ? 16 : 32, heads = a.job[0].heads + a.job[1].heads;
-    // heads one after the other only where there are workgroups enough for all compute units without
-    const int64_t chunk = cdiv(a.tokens.rows, 256 / lanes) * heads / ((int64_t)ctx->num_cu * 8);
-    a.chunk = (int)(chunk < 1 ? 1 : (chunk < heads ? chunk : heads));
-    for (int j = 0; j < 2; ++j) a.chunks[j] = (int)cdiv(a.job[j].heads, a.chunk);
+dcnn_status launch_heads(dcnn_ctx* ctx, int dtype, int dim, HeadsOp op, const HeadsArgs& a) {
     if (dtype == DCNN_F16) return launch_heads_t<f16>(ctx, dim, op, a);
     if (dtype == DCNN_BF16) return launch_heads_t<bf16>(ctx, dim, op, a);
     return launch_heads_t<float>(ctx, dim, op, a);

@@ -41,7 +41,7 @@ def quantised(v, most=125):
     near = off == best
     even = torch.arange(8, device=v.device) % 2 == 0
     code = torch.where((near & even).any(-1), (near & even).to(torch.uint8).argmax(-1), near.to(torch.uint8).argmax(-1))
-    code = code + 8 * torch.signbit(u)                     # (a zero keeps its sign)
+    code = torch.where(u < 0, code + 8, code) * (code > 0)     # (a zero is code 0)
     byte = torch.where(broken, torch.full_like(e, 255), e + 127)
     return code.flatten(-2).to(torch.uint8), byte.to(torch.uint8)
 

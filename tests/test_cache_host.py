@@ -79,7 +79,7 @@ dcnn_status fail(dcnn_ctx* ctx, dcnn_status s, const char* fmt, ...) {
     va_list ap; va_start(ap, fmt); vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap); va_end(ap);
     return s;
 }
-dcnn_status launch_heads(dcnn_ctx*, int, int, HeadsOp, HeadsArgs) { ++launches; return DCNN_OK; }
+dcnn_status launch_heads(dcnn_ctx*, int, int, HeadsOp, const HeadsArgs&) { ++launches; return DCNN_OK; }
 dcnn_status launch_attend(dcnn_ctx*, int, int, const AttendPlan&, const AttendArgs&) { ++launches; return DCNN_OK; }
 AttendPlan attend_plan(int64_t, int, int, int64_t, int64_t) { return AttendPlan(); }
 }
