@@ -34,39 +34,52 @@ template <int NB> __device__ __forceinline__ int value_column(int row, int col) 
     return col;
 }
 
-// The page of the sixteen tokens `lane % 4` of a tile.
-__device__ __forceinline__ int tile_page(const CacheArgs& c, int stream, int first, int lane) { return page_of(c, stream, (first + 16 * (lane & 3)) >> c.page_shift); }
+// The page of a tile (WHOLE: pages hold whole tiles), or of its sixteen tokens `lane % 4`.
+template <bool WHOLE> __device__ __forceinline__ int tile_page(const CacheArgs& c, int stream, int first, int lane) {
+    const int page = page_of(c, stream, (first + (WHOLE ? 0 : 16 * (lane & 3))) >> c.page_shift);
+    return WHOLE ? __builtin_amdgcn_readfirstlane(page) : page;
+}
 
-template <int NB> __device__ __forceinline__ void load_tile(KvTile<NB>& t, const CacheArgs& c, int page, int head, int first, int lane) {
+template <int NB, bool WHOLE> __device__ __forceinline__ void load_tile(KvTile<NB>& t, const CacheArgs& c, int page, int head, int first, int lane) {
     constexpr int ROW = NB * 16;
     const int g = lane / 16, i = lane % 16, mask = (1 << c.page_shift) - 1;
     const int64_t page_tokens = (int64_t)c.heads << c.page_shift;      // tokens of a page's keys, or values
+    // where sixteen tokens of the page `p` begin; with whole tiles that is the same for all lanes, and what differs between them are 32-bit offsets
     const auto token_at = [&](int p, int group, int which) {
         return ((int64_t)(p < 0 ? 0 : p) * 2 + which) * page_tokens + ((int64_t)head << c.page_shift) + ((first + 16 * group) & mask);
     };
-    const int k_page = __shfl(page, i / 4, kWave);
-    const int64_t k_at = token_at(k_page, i / 4, 0) + i % 4;
-    const uint32_t* kp = reinterpret_cast<const uint32_t*>(c.codes + k_at * ROW) + g * NB;
-    const uint8_t* sp = c.scales + k_at * NB;
+    const int64_t keys = WHOLE ? token_at(page, 0, 0) : token_at(__shfl(page, i / 4, kWave), i / 4, 0);
+    const uint32_t row = (WHOLE ? 16 * (i / 4) : 0) + i % 4;
+    const uint8_t *const kp = c.codes + keys * ROW, *const sp = c.scales + keys * NB;
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) t.k[kt][j] = kp[kt * 4 * (ROW / 4) + j];
-        t.ks[kt][0] = sp[kt * 4 * NB + g * NB / 4];
-        if constexpr (NB % 4 != 0 && NB > 2) t.ks[kt][1] = sp[kt * 4 * NB + (g * NB + NB - 1) / 4];
-        if constexpr (NB == 8) t.ks[kt][1] = sp[kt * 4 * NB + g * 2 + 1];
+        for (int j = 0; j < NB; ++j) t.k[kt][j] = *reinterpret_cast<const uint32_t*>(kp + (row * ROW + g * NB * 4 + kt * 4 * ROW + j * 4));
+        t.ks[kt][0] = sp[row * NB + kt * 4 * NB + g * NB / 4];
+        if constexpr (NB % 4 != 0 && NB > 2) t.ks[kt][1] = sp[row * NB + kt * 4 * NB + (g * NB + NB - 1) / 4];
+        if constexpr (NB == 8) t.ks[kt][1] = sp[row * NB + kt * 4 * NB + g * 2 + 1];
     }
+    if constexpr (WHOLE) {
+        const int64_t values = token_at(page, 0, 1);
+        const uint8_t *const vp = c.codes + values * ROW, *const wp = c.scales + values * NB;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        const int chunk = lane + 64 * n, group = chunk / (16 * NB), within = chunk % (16 * NB);
-        const int64_t at = token_at(__shfl(page, group, kWave), group, 1);
-        t.v[n] = *reinterpret_cast<const u32x4*>(c.codes + at * ROW + within * 16);
+        for (int n = 0; n < NB; ++n) t.v[n] = *reinterpret_cast<const u32x4*>(vp + (uint32_t)(lane * 16 + n * 1024));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) t.vs[n] = *reinterpret_cast<const u32x4*>(wp + (uint32_t)(g * 16 * NB + n * 16));
+        t.page = page >= 0;
+    } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const int chunk = lane + 64 * n, group = chunk / (16 * NB), within = chunk % (16 * NB);
+            const int64_t at = token_at(__shfl(page, group, kWave), group, 1);
+            t.v[n] = *reinterpret_cast<const u32x4*>(c.codes + at * ROW + within * 16);
+        }
+        const int v_page = __shfl(page, g, kWave);
+        t.page = v_page >= 0;
+        const u32x4* wp = reinterpret_cast<const u32x4*>(c.scales + token_at(v_page, g, 1) * NB);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) t.vs[n] = wp[n];
     }
-    const int v_page = __shfl(page, g, kWave);
-    t.page = v_page >= 0;
-    const u32x4* vp = reinterpret_cast<const u32x4*>(c.scales + token_at(v_page, g, 1) * NB);
-#pragma unroll
-    for (int n = 0; n < NB; ++n) t.vs[n] = vp[n];
 }
 
 // Scale of token e and block b among a lane's value scales, as a conversion takes it.
@@ -76,22 +89,25 @@ template <int NB> __device__ __forceinline__ float value_scale(const u32x4 (&vs)
     return __builtin_bit_cast(float, at == 3 ? w >> 1 : w << (23 - 8 * at));
 }
 
-template <typename T, int NB>
-__global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
+template <typename T, int NB, bool WHOLE>
+__global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void attend_few_kernel(AttendArgs a) {
     typedef Operand<T> O;
     typedef typename O::type Op;
     constexpr int D = NB * 32, ROW = NB * 16, TERMS = O::TERMS;
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * 64 * ROW];         // values of the waves' tiles, then sums
     __shared__ float stat[4][16][2];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 16, i = lane % 16;
     uint8_t* const mine = lds + wave * 64 * ROW;
     const int count = row_count(a.tokens.count, a.tokens.rows);
     const int units = count * a.cache.heads * a.blocks;
     for (int64_t item = blockIdx.x; item < (int64_t)units * a.splits; item += gridDim.x) {
         const int unit = (int)(item / a.splits), part = (int)(item % a.splits);
         const int block = unit % a.blocks, rest = unit / a.blocks, head = rest % a.cache.heads, r = rest / a.cache.heads;
-        const Token token = token_of(a.tokens, r);
-        const Span span = span_of(a, token);
+        // (the same for all lanes, and the compiler is told: what is made of it takes no vector registers)
+        Token token = token_of(a.tokens, r);
+        Span span = span_of(a, token);
+        token.stream = __builtin_amdgcn_readfirstlane(token.stream);
+        span.lo = __builtin_amdgcn_readfirstlane(span.lo), span.hi = __builtin_amdgcn_readfirstlane(span.hi);
         const int start = span.lo & ~63, tiles = (span.hi - start + 63) / 64, share = (tiles + a.splits - 1) / a.splits;
         const int from = part * share, to = from + share < tiles ? from + share : tiles;
         // this lane's query head, and its values that meet the lane's part of a key
@@ -113,15 +129,16 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
         float top = -INFINITY, sum = 0.0f;
 
         int tile = from + wave;
-        KvTile<NB> next;
+        KvTile<NB> tiles_ahead[2];
         int page = -1;
+        const auto page_at = [&](int t) { return tile_page<WHOLE>(a.cache, token.stream, start + t * 64, lane); };
         if (tile < to) {
-            page = tile_page(a.cache, token.stream, start + tile * 64, lane);
-            load_tile<NB>(next, a.cache, page, head, start + tile * 64, lane);
-            if (tile + 4 < to) page = tile_page(a.cache, token.stream, start + (tile + 4) * 64, lane);
+            page = page_at(tile);
+            load_tile<NB, WHOLE>(tiles_ahead[0], a.cache, page, head, start + tile * 64, lane);
+            if (tile + 4 < to) page = page_at(tile + 4);
         }
-        for (; tile < to; tile += 4) {
-            const KvTile<NB> now = next;
+        // a tile in work while the next one's codes are on the way, into the other of two places
+        const auto work = [&](KvTile<NB>& now, KvTile<NB>& next) {
             const int first = start + tile * 64;
             // (a wave's accesses to LDS follow each other: what it reads of the tile before has been read)
 #pragma unroll
@@ -131,8 +148,8 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             if (tile + 4 < to) {
-                load_tile<NB>(next, a.cache, page, head, first + 256, lane);
-                if (tile + 8 < to) page = tile_page(a.cache, token.stream, first + 512, lane);
+                load_tile<NB, WHOLE>(next, a.cache, page, head, first + 256, lane);
+                if (tile + 8 < to) page = page_at(tile + 8);
             }
             float p[16];
 #pragma unroll
@@ -147,25 +164,31 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
                     for (int t = 0; t < TERMS; ++t) s = O::mfma16(k, qo[j][t], s);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[kt * 4 + e] = s[e] * a.factor;
+                for (int e = 0; e < 4; ++e) p[kt * 4 + e] = s[e];
             }
             // the lane's column, tokens first + 16 g + 0 .. 15
-            uint32_t seen = 0xffffu;
-            const bool ragged = first < span.lo || first + 64 > span.hi || !__all(now.page);
-            if (ragged) {
+            if (__builtin_amdgcn_readfirstlane(first < span.lo || first + 64 > span.hi || !__all(now.page))) {
                 const int t = first + 16 * g;
-                seen = 0;
+                uint32_t seen = 0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) seen |= now.page && t + e >= span.lo && t + e < span.hi ? 1u << e : 0u;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) p[e] = seen >> e & 1 ? p[e] : -INFINITY;
+                // (what lies in masked places may be anything, and a zero times NaN is one: their values' scales become the smallest)
+#pragma unroll
+                for (int w = 0; w < 4 * NB; ++w) {
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int byte = 0; byte < 4; ++byte) keep |= seen >> ((4 * w + byte) / NB) & 1 ? 0xffu << 8 * byte : 0u;
+                    now.vs[w / 4][w % 4] &= keep;
+                }
             }
             float m = p[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) m = fmaxf(m, p[e]);
             m = fmaxf(m, __shfl_xor(m, 16, kWave));
             m = fmaxf(m, __shfl_xor(m, 32, kWave));
-            m = fmaxf(m, top);
+            m = fmaxf(m * a.factor, top);                              // (the factor is above zero)
             if (__any(m > top)) {
                 const float factor = m > top ? __builtin_amdgcn_exp2f(top - m) : 1.0f;        // (top may be -inf: 0)
                 top = m;
@@ -176,7 +199,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
             const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                p[e] = __builtin_amdgcn_exp2f(p[e] - base);
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], a.factor, -base));
                 sum += p[e];
             }
             Op w[2][TERMS];
@@ -187,10 +210,6 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
                 float vs[2][8];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) vs[e / 8][e % 8] = value_scale<NB>(now.vs, e, b);
-                if (ragged) {                                          // (what lies in masked places may be anything, and a zero times NaN is one)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) vs[e / 8][e % 8] = seen >> e & 1 ? vs[e / 8][e % 8] : 0.0f;
-                }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const int d = 2 * b + half;
@@ -204,6 +223,13 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        };
+        while (tile < to) {
+            work(tiles_ahead[0], tiles_ahead[1]);
+            tile += 4;
+            if (tile >= to) break;
+            work(tiles_ahead[1], tiles_ahead[0]);
+            tile += 4;
         }
 
         // the waves' sums as one: those of waves 2 and 3 to waves 0 and 1, then wave 1's to wave 0
@@ -262,7 +288,9 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
 
 template <typename T, int NB> static dcnn_status launch_few(dcnn_ctx* ctx, const AttendArgs& a) {
     const int64_t units = (int64_t)a.tokens.rows * a.cache.heads * a.blocks * a.splits, most = (int64_t)ctx->num_cu * 16;
-    hipLaunchKernelGGL((attend_few_kernel<T, NB>), dim3((unsigned)(units < most ? units : most)), dim3(256), 0, ctx->stream, a);
+    const dim3 grid((unsigned)(units < most ? units : most));
+    if (a.cache.page_shift >= 6) hipLaunchKernelGGL((attend_few_kernel<T, NB, true>), grid, dim3(256), 0, ctx->stream, a);
+    else hipLaunchKernelGGL((attend_few_kernel<T, NB, false>), grid, dim3(256), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "attend_few_kernel launch");
 }
 template <typename T> static dcnn_status launch_few_t(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
