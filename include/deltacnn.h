@@ -482,7 +482,7 @@ typedef struct {
     void*           scratch_dev;
     size_t          scratch_bytes;
 } dcnn_cache_attend_args;
-size_t      dcnn_cache_scratch_bytes(int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length);
+size_t      dcnn_cache_scratch_bytes(int32_t dtype, int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length);
 dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* args);
 
 #ifdef __cplusplus

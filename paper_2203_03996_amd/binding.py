@@ -194,7 +194,7 @@ def load_library() -> C.CDLL:
     lib.dcnn_rows_heads.argtypes = [vp, P(RowsHeadsArgs)]
     lib.dcnn_cache_append.argtypes = [vp, P(CacheAppendArgs)]
     lib.dcnn_cache_read.argtypes = [vp, P(CacheReadArgs)]
-    lib.dcnn_cache_scratch_bytes.argtypes = [C.c_int64, i32, i32, i32, C.c_int64, C.c_int64]
+    lib.dcnn_cache_scratch_bytes.argtypes = [i32, C.c_int64, i32, i32, i32, C.c_int64, C.c_int64]
     lib.dcnn_cache_scratch_bytes.restype = sz
     lib.dcnn_cache_attend.argtypes = [vp, P(CacheAttendArgs)]
     _lib = lib
@@ -875,7 +875,7 @@ class TokenCache:
 
     def _scratch_for(self, rows, q_heads):
         """(address, bytes) of scratch for a call; a larger one takes the place of a smaller one."""
-        need = self.ctx.lib.dcnn_cache_scratch_bytes(rows, q_heads, self.heads, self.dim, self.streams, self.length)
+        need = self.ctx.lib.dcnn_cache_scratch_bytes(self._code, rows, q_heads, self.heads, self.dim, self.streams, self.length)
         scratch, capturing = self._scratch, self.ctx.capturing()
         if scratch is None or scratch.numel() < need:
             scratch = self.ctx.empty(max(need, 256), torch.uint8)

@@ -12,16 +12,29 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_
     const int q_heads = a.cache.heads * a.group;
     for (int unit = blockIdx.x; unit < count * q_heads; unit += gridDim.x) {
         const int r = unit / q_heads, q_head = unit % q_heads;
-        const int64_t first = (int64_t)unit * a.splits;
+        // the row's parts: those of its tile, or those of the workgroups that its tokens were shared among
+        int parts = a.splits, from = 0, tiles_before = 0, share = 0;
+        if (a.plan != nullptr) {
+            share = a.plan[0], tiles_before = a.plan[1 + r];
+            const int tiles = a.plan[2 + r] - tiles_before;
+            from = tiles_before / share;
+            parts = tiles > 0 ? (tiles_before + tiles - 1) / share - from + 1 : 1;
+            if (parts == 1) continue;                          // (written already)
+        }
+        const int column = q_head % a.group, hb = q_head / a.group * a.blocks + column / 16;
+        const auto part = [&](int s) {
+            if (a.plan == nullptr) return (int64_t)unit * a.splits + s;
+            return part_at(hb, from + s, a.splits, s == 0 && tiles_before % share != 0) + column % 16;
+        };
         float top = -INFINITY;
-        for (int s = lane; s < a.splits; s += kWave) top = fmaxf(top, a.stat[(first + s) * 2]);
+        for (int s = lane; s < parts; s += kWave) top = fmaxf(top, a.stat[part(s) * 2]);
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
         const float base = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, o[E] = {};
 #pragma unroll 4
-        for (int s = wave; s < a.splits; s += 4) {
-            const int64_t at = first + s;
+        for (int s = wave; s < parts; s += 4) {
+            const int64_t at = part(s);
             const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
             total += a.stat[at * 2 + 1] * w;
 #pragma unroll
@@ -44,13 +57,21 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_
     }
 }
 
-AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t streams, int64_t length) {
+AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int dim, int64_t streams, int64_t length) {
     const int64_t group = q_heads / heads;
     AttendPlan p;
     p.tiles = rows > 2 * streams;
-    const int64_t units = p.tiles ? cdiv(rows * group, 128) * heads : rows * heads * cdiv(group, 16);
-    const int64_t wanted = cdiv(p.tiles ? 512 : 2048, units < 1 ? 1 : units), most = cdiv(length, p.tiles ? 512 : 256);
-    p.splits = (int)(wanted < most ? wanted : most);
+    if (p.tiles) {
+        const int64_t units = cdiv(rows * group, 128) * heads, wanted = cdiv(512, units < 1 ? 1 : units), most = cdiv(length, 512);
+        p.splits = (int)(wanted < most ? wanted : most);
+        p.parts = p.splits > 1 ? rows * q_heads * p.splits : 0;
+    } else {
+        // as many workgroups as are resident at a time; where every row is a few tiles, or rows are many, one takes whole rows
+        const int64_t columns = heads * cdiv(group, 16), resident = dim * (dtype_size == 4 ? 3 : 1) <= 192 ? 512 : 256;
+        const int64_t shares = resident / columns;
+        p.splits = shares > 1 && rows <= kShareRows && length > 256 && rows * cdiv(length, 64) < 1 << 30 ? (int)shares : 0;
+        p.parts = columns * p.splits * 32;
+    }
     return p;
 }
 
@@ -70,7 +91,7 @@ template <typename T> static dcnn_status launch_join(dcnn_ctx* ctx, int dim, con
 
 dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendPlan& plan, const AttendArgs& a) {
     const dcnn_status st = plan.tiles ? launch_attend_tile(ctx, dtype, dim, a) : launch_attend_few(ctx, dtype, dim, a);
-    if (st != DCNN_OK || a.splits == 1) return st;
+    if (st != DCNN_OK || plan.parts == 0) return st;
     if (dtype == DCNN_F16) return launch_join<f16>(ctx, dim, a);
     if (dtype == DCNN_BF16) return launch_join<bf16>(ctx, dim, a);
     return launch_join<float>(ctx, dim, a);

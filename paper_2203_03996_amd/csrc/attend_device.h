@@ -77,6 +77,14 @@ template <typename T> __device__ __forceinline__ void load_operand(const T* p, i
     }
 }
 
+// Tiles that each of the `shares` workgroups of a head takes: a tile for each wave at least.
+__device__ __forceinline__ int share_of(int tiles, int shares) {
+    const int n = (tiles + shares - 1) / shares;
+    return n < 4 ? 4 : n;
+}
+// Where the first of a part's 16 columns lies: a workgroup has one of the row that it begins in (0) and one of the row that it ends in (1) at most.
+__device__ __forceinline__ int64_t part_at(int hb, int share, int shares, int which) { return (((int64_t)hb * shares + share) * 2 + which) * 16; }
+
 // Tokens that a row sees: lo .. hi-1.
 struct Span { int lo, hi; };
 __device__ __forceinline__ Span span_of(const AttendArgs& a, const Token& t) {

@@ -3,8 +3,8 @@
 //   S = K q,  p = exp2(S * scale log2(e) - max),  y = V^T p / sum p, the maximum and the sums kept up to date from tile to tile
 //
 // The cache is read once and nothing else is large: HBM bounds it, so every step serves to keep loads in flight.  A workgroup has one row, one
-// head of keys and up to 16 query heads of it (the columns of an operand), and every `splits`-th part of the row's tokens; its four waves go
-// through tiles of 64 tokens in turn, each with its own sums, which are joined at the end.  A tile:
+// head of keys and up to 16 query heads of it (the columns of an operand) at a time; its four waves go through tiles of 64 tokens in turn, each
+// with its own sums, which are joined at the end.  A tile:
 //   * lane (g, i), g = lane / 16, i = lane % 16.  Operand rows are tokens in the order that puts the products of tokens 16 g .. 16 g + 15
 //     into lane group g: row i of the kt-th sixteen is token 16 (i / 4) + 4 kt + i % 4.  Group g multiplies the words [g NB, (g + 1) NB) of a
 //     token's codes: one wide load, mostly one scale.
@@ -89,6 +89,8 @@ template <int NB> __device__ __forceinline__ float value_scale(const u32x4 (&vs)
     return __builtin_bit_cast(float, at == 3 ? w >> 1 : w << (23 - 8 * at));
 }
 
+__device__ __forceinline__ int tiles_of(const Span& s) { return (s.hi - (s.lo & ~63) + 63) / 64; }
+
 template <typename T, int NB, bool WHOLE>
 __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void attend_few_kernel(AttendArgs a) {
     typedef Operand<T> O;
@@ -98,18 +100,91 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
     __shared__ float stat[4][16][2];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 16, i = lane % 16;
     uint8_t* const mine = lds + wave * 64 * ROW;
+    // the rows' tiles of tokens, one row's behind the other's: each of the workgroups of a head takes as many of them
+    __shared__ int before[kShareRows + 1], row_stream[kShareRows], row_lo[kShareRows], row_hi[kShareRows], wave_sum[4];
     const int count = row_count(a.tokens.count, a.tokens.rows);
-    const int units = count * a.cache.heads * a.blocks;
-    for (int64_t item = blockIdx.x; item < (int64_t)units * a.splits; item += gridDim.x) {
-        const int unit = (int)(item / a.splits), part = (int)(item % a.splits);
-        const int block = unit % a.blocks, rest = unit / a.blocks, head = rest % a.cache.heads, r = rest / a.cache.heads;
+    const int shares = a.splits, column_blocks = a.cache.heads * a.blocks;
+    int first_row, last_row, begin = 0, end = 0, total_tiles = 0, hb, share_index = 0, share_tiles = 0;
+    if (shares > 0) {
+        constexpr int PER = kShareRows / 256;
+        hb = blockIdx.x % column_blocks, share_index = blockIdx.x / column_blocks;
+        int mine_tiles[PER], sum_tiles = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r = threadIdx.x * PER + k;
+            Span span = {0, 0};
+            Token token = {0, 0, false};
+            if (r < count) {
+                token = token_of(a.tokens, r);
+                span = span_of(a, token);
+            }
+            row_stream[r] = token.stream, row_lo[r] = span.lo, row_hi[r] = span.hi;
+            mine_tiles[k] = tiles_of(span);
+            sum_tiles += mine_tiles[k];
+        }
+        int scan = sum_tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int other = __shfl_up(scan, d, kWave);
+            if (lane >= d) scan += other;
+        }
+        if (lane == kWave - 1) wave_sum[wave] = scan;
+        __syncthreads();
+        int at = scan - sum_tiles;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) at += wave_sum[w];
+            total_tiles += wave_sum[w];
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) before[threadIdx.x * PER + k] = at, at += mine_tiles[k];
+        if (threadIdx.x == 255) before[kShareRows] = at;
+        __syncthreads();
+        share_tiles = share_of(total_tiles, shares);
+        if (blockIdx.x == 0) {                                 // (what the joining kernel goes by)
+            for (int r = threadIdx.x; r <= count; r += 256) a.plan[1 + r] = before[r];
+            if (threadIdx.x == 0) a.plan[0] = share_tiles;
+        }
+        begin = share_index * share_tiles, end = begin + share_tiles < total_tiles ? begin + share_tiles : total_tiles;
+        if (begin >= total_tiles && share_index > 0) return;
+        // the first row that begins here or later, or the one before it, if that reaches into this part
+        int low = 0, high = count;
+        while (low < high) {
+            const int middle = (low + high) / 2;
+            if (before[middle] < begin) low = middle + 1;
+            else high = middle;
+        }
+        first_row = low > 0 && (low == count || before[low] > begin) ? low - 1 : low;
+        last_row = count;
+    } else {
+        first_row = 0, last_row = 0, hb = 0;
+    }
+    // one row after the other of this part, or, where rows are many, of all that this workgroup strides through
+    const int64_t units = (int64_t)count * column_blocks;
+    int row = first_row;
+    for (int64_t item = blockIdx.x;; item += gridDim.x, ++row) {
+        int r, from, to, start;
+        Span span;
+        int stream;
+        if (shares > 0) {
+            if (row >= last_row || !(before[row] < end || (before[row] == total_tiles && end == total_tiles))) break;
+            r = row;
+            span.lo = row_lo[r], span.hi = row_hi[r], stream = row_stream[r];
+            from = begin > before[r] ? begin - before[r] : 0, to = (end < before[r + 1] ? end : before[r + 1]) - before[r];
+        } else {
+            if (item >= units) break;
+            r = (int)(item / column_blocks), hb = (int)(item % column_blocks);
+            const Token token = token_of(a.tokens, r);
+            span = span_of(a, token), stream = token.stream;
+            from = 0, to = tiles_of(span);
+        }
         // (the same for all lanes, and the compiler is told: what is made of it takes no vector registers)
-        Token token = token_of(a.tokens, r);
-        Span span = span_of(a, token);
-        token.stream = __builtin_amdgcn_readfirstlane(token.stream);
+        r = __builtin_amdgcn_readfirstlane(r), stream = __builtin_amdgcn_readfirstlane(stream);
+        from = __builtin_amdgcn_readfirstlane(from), to = __builtin_amdgcn_readfirstlane(to);
         span.lo = __builtin_amdgcn_readfirstlane(span.lo), span.hi = __builtin_amdgcn_readfirstlane(span.hi);
-        const int start = span.lo & ~63, tiles = (span.hi - start + 63) / 64, share = (tiles + a.splits - 1) / a.splits;
-        const int from = part * share, to = from + share < tiles ? from + share : tiles;
+        start = span.lo & ~63;
+        const bool whole = from == 0 && to == tiles_of(span);
+        const int block = hb % a.blocks, head = hb / a.blocks;
         // this lane's query head, and its values that meet the lane's part of a key
         const int column = block * 16 + i;
         const bool asks = column < a.group;
@@ -131,7 +206,7 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
         int tile = from + wave;
         KvTile<NB> tiles_ahead[2];
         int page = -1;
-        const auto page_at = [&](int t) { return tile_page<WHOLE>(a.cache, token.stream, start + t * 64, lane); };
+        const auto page_at = [&](int t) { return tile_page<WHOLE>(a.cache, stream, start + t * 64, lane); };
         if (tile < to) {
             page = page_at(tile);
             load_tile<NB, WHOLE>(tiles_ahead[0], a.cache, page, head, start + tile * 64, lane);
@@ -265,7 +340,7 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
         if (wave == 0 && asks) {
 #pragma unroll
             for (int d = 0; d < 2 * NB; ++d) o[d] += sums[d * kWave + lane];
-            if (a.splits == 1) {
+            if (whole) {
                 T* y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + ((int64_t)head * a.group + column) * D + 4 * g;
                 const float inv = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
@@ -276,7 +351,7 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
                     *reinterpret_cast<typename RowQuad<T>::type*>(y + d * 16) = v;
                 }
             } else {
-                const int64_t at = ((int64_t)r * a.cache.heads * a.group + head * a.group + column) * a.splits + part;
+                const int64_t at = part_at(hb, share_index, shares, before[r] > begin) + i;
 #pragma unroll
                 for (int d = 0; d < 2 * NB; ++d) *reinterpret_cast<f32x4*>(a.part + at * D + d * 16 + 4 * g) = o[d];
                 if (g == 0) a.stat[at * 2] = all, a.stat[at * 2 + 1] = total;
@@ -287,8 +362,8 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
 }
 
 template <typename T, int NB> static dcnn_status launch_few(dcnn_ctx* ctx, const AttendArgs& a) {
-    const int64_t units = (int64_t)a.tokens.rows * a.cache.heads * a.blocks * a.splits, most = (int64_t)ctx->num_cu * 16;
-    const dim3 grid((unsigned)(units < most ? units : most));
+    const int64_t columns = (int64_t)a.cache.heads * a.blocks, units = a.splits > 0 ? columns * a.splits : a.tokens.rows * columns, most = (int64_t)ctx->num_cu * 16;
+    const dim3 grid((unsigned)(a.splits > 0 || units < most ? units : most));
     if (a.cache.page_shift >= 6) hipLaunchKernelGGL((attend_few_kernel<T, NB, true>), grid, dim3(256), 0, ctx->stream, a);
     else hipLaunchKernelGGL((attend_few_kernel<T, NB, false>), grid, dim3(256), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "attend_few_kernel launch");

@@ -59,15 +59,18 @@ struct AttendArgs {
     int causal, window;
     const int32_t* lens;
     FastDiv by_group;
-    int splits;                                // workgroups that share a row's tokens
-    float *part, *stat;                        // with splits: sums [row][query head][split][dim], maxima and sums of weights [row][query head][split][2]
+    int splits;                                // tiles: workgroups that share the tokens of a tile of rows; else: that share all rows' of a head (0: none do)
+    int* plan;                                 // (shared rows) tiles of a share, then the tiles before each row and behind the last
+    float *part, *stat;                        // sums of parts [part][dim], their maxima and sums of weights [part][2]
 };
+constexpr int kShareRows = 512;                // rows at most whose tokens are shared evenly
 // Which kernel: a function of the sizes alone.
 struct AttendPlan {
     bool tiles;                                // rows of one stream share its tiles of tokens
     int splits;
+    int64_t parts;                             // of the sums of workgroups that share a row
 };
-AttendPlan attend_plan(int64_t rows, int q_heads, int heads, int64_t streams, int64_t length);
+AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int dim, int64_t streams, int64_t length);
 dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendPlan& plan, const AttendArgs& a);
 dcnn_status launch_attend_few(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);
 dcnn_status launch_attend_tile(dcnn_ctx* ctx, int dtype, int dim, const AttendArgs& a);

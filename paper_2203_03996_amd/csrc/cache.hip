@@ -6,6 +6,9 @@ using namespace dcnn;
 
 namespace {
 
+constexpr size_t kPlanBytes = 4096;            // of the scratch: the tiles of a share, and those before each of up to kShareRows rows
+static_assert((kShareRows + 2) * sizeof(int) <= kPlanBytes, "room for the rows");
+
 dcnn_status check_tokens(dcnn_ctx* ctx, const char* what, const dcnn_row_tokens& t, bool streams, bool positions, TokenArgs* a) {
     dcnn_status st = check_list(ctx, what, t.list);
     if (st == DCNN_OK) st = check_map(ctx, what, t.list);
@@ -158,12 +161,11 @@ dcnn_status dcnn_cache_read(dcnn_ctx* ctx, const dcnn_cache_read_args* p) {
     return launch_heads(ctx, p->cache.dtype, p->cache.dim, kReadHeads, a);
 }
 
-size_t dcnn_cache_scratch_bytes(int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length) {
-    if (rows < 0 || rows > kRowsMax || heads < 1 || q_heads < 1 || q_heads % heads != 0 || !cache_dim(dim) || length < 1 || length > kCacheMaxLength || streams < 1) return 0;
-    if (rows * q_heads > kMaxHeadRows) return 0;
-    const AttendPlan plan = attend_plan(rows, q_heads, heads, streams, length);
-    const int64_t parts = plan.splits > 1 ? rows * q_heads * plan.splits : 0;
-    return align_up((size_t)parts * (size_t)(dim + 2) * sizeof(float) + kAlign);
+size_t dcnn_cache_scratch_bytes(int32_t dtype, int64_t rows, int32_t q_heads, int32_t heads, int32_t dim, int64_t streams, int64_t length) {
+    if (!rows_float(dtype) || rows < 0 || rows > kRowsMax || heads < 1 || q_heads < 1 || q_heads % heads != 0 || !cache_dim(dim)) return 0;
+    if (streams < 1 || streams > kRowsMax || length < 1 || length > kCacheMaxLength || rows * q_heads > kMaxHeadRows) return 0;
+    const AttendPlan plan = attend_plan((int)rows_dtype_size(dtype), rows, q_heads, heads, dim, streams, length);
+    return kPlanBytes + align_up((size_t)plan.parts * 2 * sizeof(float)) + align_up((size_t)plan.parts * (size_t)dim * sizeof(float));
 }
 
 dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
@@ -185,7 +187,7 @@ dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
     st = check_heads_matrix(ctx, what, "q", p->q_dev, p->ldq, c, es);
     if (st == DCNN_OK) st = check_heads_matrix(ctx, what, "y", p->y_dev, p->ldy, c, es);
     if (st != DCNN_OK) return st;
-    const size_t need = dcnn_cache_scratch_bytes(rows, p->q_heads, p->cache.heads, p->cache.dim, p->cache.streams, p->cache.length);
+    const size_t need = dcnn_cache_scratch_bytes(p->cache.dtype, rows, p->q_heads, p->cache.heads, p->cache.dim, p->cache.streams, p->cache.length);
     if (p->scratch_bytes < need) return fail(ctx, DCNN_ENOMEM, "%s: scratch of %zu bytes, %zu needed", what, p->scratch_bytes, need);
     if (p->scratch_dev == nullptr || !aligned(p->scratch_dev, kAlign)) return fail(ctx, DCNN_EINVAL, "%s: scratch null or not 256-byte aligned", what);
     const Bytes outs[] = {matrix_bytes("y", p->y_dev, rows, p->ldy, c, es), vector_bytes("scratch", p->scratch_dev, (int64_t)need)};
@@ -194,7 +196,7 @@ dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
                          vector_bytes("lens", p->lens_dev, p->cache.streams * 4)};
     st = check_apart(ctx, what, outs, ins);
     if (st != DCNN_OK) return st;
-    const AttendPlan plan = attend_plan(rows, p->q_heads, p->cache.heads, p->cache.streams, p->cache.length);
+    const AttendPlan plan = attend_plan((int)es, rows, p->q_heads, p->cache.heads, p->cache.dim, p->cache.streams, p->cache.length);
     a.q = p->q_dev, a.y = p->y_dev, a.ldq = p->ldq, a.ldy = p->ldy;
     a.group = p->q_heads / p->cache.heads, a.blocks = (int)cdiv(a.group, 16);
     // (a scale of zero: so small a number that any product with it is as good as zero, and what is masked, minus infinity, stays that)
@@ -204,8 +206,10 @@ dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
     a.lens = p->lens_dev;
     a.by_group = make_fastdiv((uint32_t)a.group);
     a.splits = plan.splits;
-    a.stat = static_cast<float*>(p->scratch_dev);
-    a.part = a.stat + align_up((size_t)(rows * p->q_heads) * plan.splits * 2, 64);
+    char* const scratch = static_cast<char*>(p->scratch_dev);
+    a.plan = plan.tiles ? nullptr : reinterpret_cast<int*>(scratch);
+    a.stat = reinterpret_cast<float*>(scratch + kPlanBytes);
+    a.part = reinterpret_cast<float*>(scratch + kPlanBytes + align_up((size_t)plan.parts * 2 * sizeof(float)));
     return launch_attend(ctx, p->cache.dtype, p->cache.dim, plan, a);
 }
 

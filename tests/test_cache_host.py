@@ -60,13 +60,16 @@ def test_calls_without_a_context_are_refused():
 
 def test_scratch():
     size = pkg.load_library().dcnn_cache_scratch_bytes
+    for dtype in range(3):
+        sizes = [size(dtype, rows, 8, 8, 64, 4, 4096) for rows in range(0, 9)]
+        assert min(sizes) > 0
     for rows, q_heads, heads, dim, streams, length in ((1, 32, 8, 128, 1, 1 << 20), (64, 32, 8, 128, 64, 8192), (5000, 8, 8, 64, 1, 4096), (1, 1, 1, 256, 1, 1 << 30),
                                                        (1 << 15, 1 << 15, 1, 32, 1, 1)):
-        assert 0 < size(rows, q_heads, heads, dim, streams, length) < 1 << 28
-    assert size(0, 1, 1, 32, 1, 1) > 0
+        assert 0 < size(1, rows, q_heads, heads, dim, streams, length) < 1 << 28
+    assert size(0, 0, 1, 1, 32, 1, 1) > 0 and size(3, 1, 8, 8, 64, 1, 64) == 0
     for bad in ((-1, 8, 8, 64, 1, 64), (1, 9, 8, 64, 1, 64), (1, 8, 0, 64, 1, 64), (1, 8, 8, 65, 1, 64), (1, 8, 8, 64, 1, 0), (1, 8, 8, 64, 1, (1 << 30) + 1),
                 (1 << 27, 16, 8, 64, 1, 64), (1, 8, 8, 64, 0, 64)):
-        assert size(*bad) == 0
+        assert size(0, *bad) == 0
 
 
 # ---- the entry points' checks, compiled for the host with launches that count -----------------------------------------
@@ -81,7 +84,7 @@ dcnn_status fail(dcnn_ctx* ctx, dcnn_status s, const char* fmt, ...) {
 }
 dcnn_status launch_heads(dcnn_ctx*, int, int, HeadsOp, const HeadsArgs&) { ++launches; return DCNN_OK; }
 dcnn_status launch_attend(dcnn_ctx*, int, int, const AttendPlan&, const AttendArgs&) { ++launches; return DCNN_OK; }
-AttendPlan attend_plan(int64_t, int, int, int64_t, int64_t) { return AttendPlan(); }
+AttendPlan attend_plan(int, int64_t, int, int, int, int64_t, int64_t) { return AttendPlan(); }
 }
 extern "C" {
 dcnn_ctx ctx_of_tests;

@@ -508,6 +508,33 @@ def test_attend_long_cache_in_parts(ctx, dt):
         check_attend(cache, dt, q, zero, pos, [19987], causal=True, streams=zero, positions=pos, what=f"{rows} rows")
 
 
+@pytest.mark.parametrize("rows", [2, 3, 64, 200, 511, 512, 513, 700])
+@pytest.mark.parametrize("lengths", ["none", "one long", "first", "last", "gaps", "all alike", "one tile", "mixed"])
+def test_attend_tokens_shared_among_workgroups(ctx, rows, lengths):
+    """One row of each stream, whose lengths put the borders of the workgroups' parts at, before and behind the rows'; streams share a few pages."""
+    length = 1100
+    cache = pkg.TokenCache(ctx, rows, length, 1, 32, dtype=torch.float16, page=64, num_pages=40, pages=torch.zeros((rows, 18), dtype=torch.int32, device="cuda"))
+    gen = seeded(rows)
+    cache.pages.random_(0, 40, generator=gen)
+    cache.codes.random_(0, 256, generator=gen)
+    cache.scales.random_(124, 128, generator=gen)
+    r = torch.arange(rows)
+    lens = {"none": 0 * r, "one long": torch.where(r == rows // 2, 1100, 0), "first": torch.where(r == 0, 1024, 0), "last": torch.where(r == rows - 1, 1088, 0),
+            "gaps": torch.where(r % 3 == 1, 64 * (r % 17), 0), "all alike": 0 * r + 256, "one tile": 0 * r + 64, "mixed": (r * 7919) % 1101}[lengths].to(torch.int32)
+    q = rand(gen, rows, 2 * 32, dt="f16")
+    got = cache.attend(q, lens=lens.cuda(), positions=torch.zeros(rows, dtype=torch.int32, device="cuda"))
+    ctx.sync()
+    # rows of one length at a time, in 64 bits
+    k, v = (plain.values(cache.codes[:, w, 0], cache.scales[:, w, 0])[cache.pages.long()].flatten(1, 2) for w in (0, 1))
+    x = torch.einsum("rhd,rtd->rht", q.double().view(rows, 2, 32), k) * 32 ** -0.5
+    seen = torch.arange(k.shape[1], device="cuda") < lens.cuda()[:, None]
+    w = torch.softmax(x.masked_fill(~seen[:, None], -1e300), 2) * seen[:, None]
+    want = torch.einsum("rht,rtd->rhd", w, v)
+    met = torch.einsum("rht,rtd->rhd", w, v.abs())
+    error = 2 * (40 * U32 * torch.einsum("rhd,rtd->rht", q.double().view(rows, 2, 32).abs(), k.abs()) * 32 ** -0.5 + 8 * U32 * x.abs()).amax(2, keepdim=True)
+    close(got, want, "f16", (2 * error + 2.0 ** -11 + 3400 * U32) * met + 2.0 ** -25 * v.abs().sum(1)[:, None] * w.amax(2, keepdim=True), lengths)
+
+
 @pytest.mark.parametrize("dt", list(TYPES))
 def test_the_same_call_gives_the_same_bits(ctx, dt):
     cache = filled(ctx, 3, 500, 2, 128, dt)
