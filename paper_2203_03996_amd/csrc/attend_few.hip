@@ -36,8 +36,8 @@ template <int NB> __device__ __forceinline__ int value_column(int row, int col) 
 
 // The page of a tile (WHOLE: pages hold whole tiles), or of its sixteen tokens `lane % 4`.
 template <bool WHOLE> __device__ __forceinline__ int tile_page(const CacheArgs& c, int stream, int first, int lane) {
-    const int page = page_of(c, stream, (first + (WHOLE ? 0 : 16 * (lane & 3))) >> c.page_shift);
-    return WHOLE ? __builtin_amdgcn_readfirstlane(page) : page;
+    if constexpr (WHOLE) return page_of_all(c, stream, first >> c.page_shift);
+    else return page_of(c, stream, (first + 16 * (lane & 3)) >> c.page_shift);
 }
 
 template <int NB, bool WHOLE> __device__ __forceinline__ void load_tile(KvTile<NB>& t, const CacheArgs& c, int page, int head, int first, int lane) {

@@ -19,12 +19,18 @@ typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int kVectors = 128, kTokens = 64;
 
-// 16-byte columns of a row of LDS (4 NB of them), permuted against bank conflicts.
+// 16-byte columns of a row of LDS (4 NB of them), permuted so that sixteen lanes meet sixteen different ones of the 256 bytes that the banks span: the same
+// column of sixteen rows in a row (keys), four columns of four rows (values, read transposed).
 template <int NB> __device__ __forceinline__ int tile_column(int row, int col) {
-    if constexpr (NB == 1) return col ^ (row >> 1 & 3);
-    if constexpr (NB == 3) return col ^ (row >> 2 & 3);
-    if constexpr (NB == 6) return col ^ (row >> 1 & 7);
-    return col ^ (row & 7);
+    if constexpr (NB % 4 == 0) return col ^ ((row & 3) << 2 | (row >> 2 & 3));
+    if constexpr (NB % 2 == 0) return col ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+    return col ^ (row >> 2 & 3);
+}
+// The token of the x-th group of lanes that writes a tile: those that write together differ in the bits that permute columns.
+template <int NB> __device__ __forceinline__ int staged_token(int x) {
+    if constexpr (NB == 1) return x;
+    if constexpr (NB % 4 == 0 || NB == 3) return (x & ~15) | (x & 3) << 2 | (x >> 2 & 3);
+    return (x & ~14) | (x & 6) << 1 | (x >> 2 & 2);
 }
 
 __device__ __forceinline__ int wave_min(int v) {
@@ -43,15 +49,16 @@ template <typename T, int NB> struct TileShape {
     static constexpr int bytes = 2 * 2 * kTokens * NB * 64;            // two buffers of keys and values
 };
 
-template <typename T, int NB>
+// WHOLE: pages hold whole tiles of tokens.
+template <typename T, int NB, bool WHOLE>
 __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_kernel(AttendArgs a) {
     typedef Operand<T> O;
     typedef typename O::type Op;
     constexpr int D = NB * 32, ROW = D * 2, TERMS = O::TERMS, CHUNKS = (NB + 1) / 2, PLANE = kTokens * ROW;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int streams[kVectors], lows[kVectors], highs[kVectors];
-    __shared__ uint64_t broken[2][NB];                                 // blocks of values that are NaN: bit token * NB + block
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    __shared__ uint64_t broken[2][NB];                                 // blocks of values that are NaN, in the order in which they are written
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = lane / 32, col = lane % 32;
     const int count = row_count(a.tokens.count, a.tokens.rows);
     const int vectors = count * a.group, tiles = (vectors + kVectors - 1) / kVectors, heads = a.cache.heads;
     if (tiles == 0) return;
@@ -121,75 +128,119 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             // ---- codes of a tile: from memory, to operands in LDS
             u32x4 raw[CHUNKS];
             uint32_t byte[CHUNKS];
-            const auto page_at = [&](int t) { return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift); };
+            bool drop[CHUNKS];
+            const auto page_at = [&](int t) {
+                if constexpr (WHOLE) return page_of_all(a.cache, of, (start + t * kTokens) >> a.cache.page_shift);
+                else return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift);
+            };
             const auto load = [&](int t, int page) {
 #pragma unroll
                 for (int n = 0; n < CHUNKS; ++n) {
-                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = within / NB, b = within % NB, which = c / (kTokens * NB);
-                    if (NB % 2 != 0 && c >= 2 * kTokens * NB) break;
-                    const int p = __shfl(page, token_in / 16, kWave), t_at = start + t * kTokens + token_in;
-                    const int64_t slot = ((int64_t)(p < 0 ? 0 : p) * 2 + which) * page_tokens + ((int64_t)head << a.cache.page_shift) + (t_at & page_mask);
-                    raw[n] = *reinterpret_cast<const u32x4*>(a.cache.codes + slot * (D / 2) + b * 16);
-                    byte[n] = a.cache.scales[slot * NB + b];
-                    if (p < 0 || t_at < first || t_at >= last) byte[n] = 0;                            // (what lies there may be anything)
+                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB;
+                    const int which = __builtin_amdgcn_readfirstlane(c / (kTokens * NB)), t_at = start + t * kTokens + token_in;
+                    if (NB % 2 != 0 && which > 1) break;
+                    bool counts = t_at >= first && t_at < last;
+                    if constexpr (WHOLE) {
+                        // the tile's first token, one for all lanes, and 32-bit offsets from it
+                        const int64_t slot = ((int64_t)(page < 0 ? 0 : page) * 2 + which) * page_tokens + ((int64_t)head << a.cache.page_shift) + ((start + t * kTokens) & page_mask);
+                        const uint8_t *const codes = a.cache.codes + slot * (D / 2), *const scales = a.cache.scales + slot * NB;
+                        raw[n] = *reinterpret_cast<const u32x4*>(codes + (uint32_t)(token_in * (D / 2) + b * 16));
+                        byte[n] = scales[(uint32_t)(token_in * NB + b)];
+                        counts = counts && page >= 0;
+                    } else {
+                        const int p = __shfl(page, token_in / 16, kWave);
+                        const int64_t slot = ((int64_t)(p < 0 ? 0 : p) * 2 + which) * page_tokens + ((int64_t)head << a.cache.page_shift) + (t_at & page_mask);
+                        raw[n] = *reinterpret_cast<const u32x4*>(a.cache.codes + slot * (D / 2) + b * 16);
+                        byte[n] = a.cache.scales[slot * NB + b];
+                        counts = counts && p >= 0;
+                    }
+                    drop[n] = !counts;                                 // (what lies there may be anything)
                 }
             };
             const auto stage = [&](int buffer) {
 #pragma unroll
                 for (int n = 0; n < CHUNKS; ++n) {
-                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = within / NB, b = within % NB, which = c / (kTokens * NB);
-                    if (NB % 2 != 0 && c >= 2 * kTokens * NB) break;
+                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB;
+                    const int which = __builtin_amdgcn_readfirstlane(c / (kTokens * NB));
+                    if (NB % 2 != 0 && which > 1) break;
                     // a value that is NaN is not multiplied (a weight of zero would make it one of rows that do not see it): it is noted
-                    const bool nan = which == 1 && byte[n] == 255;
+                    const bool nan = which == 1 && byte[n] == 255 && !drop[n];
                     const uint64_t noted = __ballot(nan);
                     if (which == 1 && lane == 0) broken[buffer][within / 64] = noted;
-                    const float scale = scale_of_byte(nan ? 0 : byte[n]);
+                    const float scale = scale_of_byte(nan || drop[n] ? 0 : byte[n]);
                     uint8_t* const row = lds + (buffer * 2 + which) * PLANE + token_in * ROW;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) *reinterpret_cast<Op*>(row + tile_column<NB>(token_in, 4 * b + i) * 16) = decode8<T>(raw[n][i], scale);
                 }
             };
+            // which sixteens of a tile's tokens have a page
+            const auto sixteens = [&](int p) { return WHOLE ? (p >= 0 ? 15u : 0u) : (uint32_t)__ballot(p >= 0) & 15u; };
             int page = page_at(from);
-            uint32_t paged[3] = {0, 0, 0};                             // which sixteens of tokens have a page: of this tile, the next, the one behind
-            const auto sixteens = [&](int p) { return (uint32_t)__ballot(p >= 0) & 15u; };
-            paged[0] = sixteens(page);
+            uint32_t paged = sixteens(page), paged_next = 0;
             load(from, page);
             page = page_at(from + 1);
             __syncthreads();                                           // (a segment before this one is done with the buffers)
             stage(from & 1);
-            paged[1] = sixteens(page);
             if (from + 1 < to) {
+                paged_next = sixteens(page);
                 load(from + 1, page);
                 page = page_at(from + 2);
-                paged[2] = sixteens(page);
             }
             for (int t = from; t < to; ++t) {
                 __syncthreads();                                       // this tile is there, and all are done with the one before it
                 if (t + 1 < to) stage((t + 1) & 1);
-                const uint32_t has_page = paged[0];
-                paged[0] = paged[1], paged[1] = paged[2];
-                if (t + 2 < to) {
+                const uint32_t has_page = paged;
+                paged = paged_next;
+                if (t + 2 < to) {                                      // (nothing of these loads is looked at before the next tile's turn)
+                    paged_next = sixteens(page);
                     load(t + 2, page);
                     page = page_at(t + 3);
-                    paged[2] = sixteens(page);
                 }
                 const int t0 = start + t * kTokens;
                 if (t0 + kTokens <= any_from || t0 >= any_to) continue;
-                const uint8_t* const keys = lds + (t & 1) * 2 * PLANE;
-                const uint8_t* const vals = keys + PLANE;
+                // (lane's parts of addresses: made anew for each tile, or the compiler keeps one in a register for each read)
+                int key_x = half ^ tile_column<NB>(col, 0), value_x = (lane % 32 / 16 * 2 + lane % 4 / 2) ^ tile_column<NB>(4 * half + lane % 16 / 4, 0);
+                asm volatile("" : "+v"(key_x), "+v"(value_x));
+                const uint8_t* const keys = lds + (t & 1) * 2 * PLANE + col * ROW;
+                const uint8_t* const vals = lds + (t & 1) * 2 * PLANE + PLANE + (4 * half + lane % 16 / 4) * ROW + lane % 2 * 8;
+                // operands are read four products ahead: one at a time, each product waits for its own (prompts of 14348 rows took 850 us)
                 f32x16 s[2];
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
+                for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
+                Op k[2][4];
+                const auto read_keys = [&](int group) {
 #pragma unroll
-                    for (int j = 0; j < 2 * NB; ++j) {
-                        const int row = kb * 32 + col;
-                        const Op k = *reinterpret_cast<const Op*>(keys + row * ROW + tile_column<NB>(row, 2 * j + half) * 16);
+                    for (int n = 0; n < 4; ++n) k[group % 2][n] = *reinterpret_cast<const Op*>(keys + n % 2 * 32 * ROW + (key_x ^ 2 * (group * 2 + n / 2)) * 16);
+                };
+                read_keys(0);
 #pragma unroll
-                        for (int m = 0; m < TERMS; ++m) s[kb] = O::mfma32(k, q[j][m], s[kb]);
-                    }
+                for (int group = 0; group < NB; ++group) {
+                    if (group + 1 < NB) read_keys(group + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int m = 0; m < TERMS; ++m) s[n % 2] = O::mfma32(k[group % 2][n], q[group * 2 + n / 2][m], s[n % 2]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                // values: two blocks of channels side by side; step n is tokens 16 * (n / 2 % 4) on and block 2 * (n / 8) + n % 2
+                constexpr auto block_of = [](int n) { return n < NB / 2 * 8 ? n / 8 * 2 + n % 2 : NB - 1; };
+                constexpr auto tokens_of = [](int n) { return n < NB / 2 * 8 ? n / 2 % 4 : n % 4; };
+                Op x[2][4];
+                const auto read_values = [&](int group) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        i16x4 part[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            part[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vals + (16 * tokens_of(group * 4 + n) + 8 * i) * ROW +
+                                                                                            (value_x ^ (4 * block_of(group * 4 + n) + 2 * i)) * 16));
+                        x[group % 2][n] = __builtin_bit_cast(Op, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+                };
+                read_values(0);
                 // the column's product with token t0 + 32 kb + 8 (e / 4) + 4 half + e % 4
                 if (t0 < see_from || t0 + kTokens > see_to || has_page != 15u) {
 #pragma unroll
@@ -207,8 +258,10 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
 #pragma unroll
                     for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
                 m = fmaxf(m, __shfl_xor(m, 32, kWave));
-                m = fmaxf(m * a.factor, top);                          // (the factor is above zero)
-                if (__any(m > top)) {
+                m *= a.factor;                                         // (the factor is above zero)
+                // (weights up to 2^8 do as well as those up to one: sums are scaled anew where a column's maximum has grown by more than that)
+                if (__any(m > top + 8.0f)) {
+                    m = fmaxf(m, top);
                     const float factor = m > top ? __builtin_amdgcn_exp2f(top - m) : 1.0f;
                     top = m;
                     sum *= factor;
@@ -230,29 +283,24 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                         O::split(w, p[kb][u]);
                     }
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int group = 0; group < NB; ++group) {
+                    if (group + 1 < NB) read_values(group + 1);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+                    for (int n = 0; n < 4; ++n) {
+                        const int b = block_of(group * 4 + n), tokens = tokens_of(group * 4 + n);
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            i16x4 x[2];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int row = kb * 32 + 16 * u + 8 * i + 4 * half + lane % 16 / 4;
-                                const int c = 4 * b + lane % 32 / 16 * 2 + lane % 4 / 2;
-                                x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vals + row * ROW + tile_column<NB>(row, c) * 16 + lane % 2 * 8));
-                            }
-                            const Op k = __builtin_bit_cast(Op, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                            for (int n = 0; n < TERMS; ++n) o[b] = O::mfma32(k, p[kb][u][n], o[b]);
-                        }
+                        for (int m = 0; m < TERMS; ++m) o[b] = O::mfma32(x[group % 2][n], p[tokens / 2][tokens % 2][m], o[b]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 uint64_t noted = 0;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) noted |= broken[t & 1][b];
                 if (noted != 0) {
                     for (int w = 0; w < NB; ++w)
                         for (uint64_t bits = broken[t & 1][w]; bits != 0; bits &= bits - 1) {
-                            const int bit = w * 64 + __builtin_ctzll(bits), in_tile = bit / NB;
+                            const int bit = w * 64 + __builtin_ctzll(bits), in_tile = staged_token<NB>(bit / NB);
                             if ((uint32_t)(t0 + in_tile - lo) < (uint32_t)(hi - lo)) {
 #pragma unroll
                                 for (int b = 0; b < NB; ++b)
@@ -296,7 +344,7 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
 
 template <typename T, int NB> static dcnn_status launch_tile(dcnn_ctx* ctx, const AttendArgs& a) {
     constexpr int bytes = TileShape<T, NB>::bytes;
-    auto* const kern = &attend_tile_kernel<T, NB>;
+    auto* const kern = a.cache.page_shift >= 6 ? &attend_tile_kernel<T, NB, true> : &attend_tile_kernel<T, NB, false>;
     if (bytes > 64 * 1024) {
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (err != hipSuccess) return check_hip(ctx, err, "hipFuncSetAttribute(attend_tile_kernel)");
