@@ -382,26 +382,34 @@ class Context:
         without keys."""
         a, dt, dev = RowsHeadsArgs(), q.dtype, self.index
         a.dtype, a.dim = _row_dtype(dt), dim
-        a.q, a.ldq, rows, a.q_heads = _as_heads(q, "q", dim, dt, dev)
-        if idx is None and positions is not None:
-            _whole(positions, rows, "positions", "q")
-        rows = _set_tokens(a, rows, rows, None, positions, rotation.positions if rotation is not None else 1, idx, count, dev)
+        a.q, a.ldq, rows, c = _matrix(q, "q", dim, 0, dt, dev)
+        a.q_heads = c // dim
+        period = 1
+        if rotation is not None:
+            period = rotation.positions
+            a.table, a.positions, a.rot, a.style = rotation.pointers(dev)
+        rows = _set_tokens(a, rows, None, positions, period, idx, count, dev)
         if k is not None:
-            a.k, a.ldk, n, a.k_heads = _as_heads(k, "k", dim, dt, dev)
-            rows = _room(rows, n, "k", count)
-        q_out = self.empty((rows, a.q_heads * dim), dt) if q_out is None else q_out
-        a.q_out, a.ldq_out, n = _as_rows(q_out, "q_out", a.q_heads * dim, dt, dev)
-        rows = _room(rows, n, "q_out", count)
-        if k is not None:
-            k_out = self.empty((rows, a.k_heads * dim), dt) if k_out is None else k_out
-            a.k_out, a.ldk_out, n = _as_rows(k_out, "k_out", a.k_heads * dim, dt, dev)
+            a.k, a.ldk, n, ck = _matrix(k, "k", dim, 0, dt, dev)
+            a.k_heads = ck // dim
+            if n < rows:
+                rows = _room(rows, n, "k", count)
+        if q_out is not None:
+            a.q_out, a.ldq_out, n, _ = _matrix(q_out, "q_out", dim, c, dt, dev)
+            rows = _room(rows, n, "q_out", count)
+        if k_out is not None and k is not None:
+            a.k_out, a.ldk_out, n, _ = _matrix(k_out, "k_out", dim, ck, dt, dev)
             rows = _room(rows, n, "k_out", count)
+        if q_out is None:
+            q_out = self.empty((rows, c), dt)
+            a.q_out, a.ldq_out = q_out.data_ptr(), c
+        if k_out is None and k is not None:
+            k_out = self.empty((rows, ck), dt)
+            a.k_out, a.ldk_out = k_out.data_ptr(), ck
         if q_norm is not None:
             a.q_norm_kind, a.q_norm_eps, a.q_norm_w, a.q_norm_b = q_norm.pointers(dim, dt, dev)
         if k_norm is not None:
             a.k_norm_kind, a.k_norm_eps, a.k_norm_w, a.k_norm_b = k_norm.pointers(dim, dt, dev)
-        if rotation is not None:
-            a.table, a.positions, a.rot, a.style = rotation.pointers(dev)
         a.rows = rows
         st = self.lib.dcnn_rows_heads(self.handle, a)
         if st:
@@ -688,34 +696,39 @@ class RowWeights:
         return self._call(self.ctx.lib.dcnn_rows_linear, 1, a, rows, dt, count, out)
 
 
-def _as_heads(t, name, dim, dt, dev):
-    """(address, leading dimension, rows, heads) of a matrix of heads of `dim` values."""
-    if t.dim() != 2 or t.shape[1] == 0 or t.shape[1] % dim:
-        raise ValueError(f"{name} must be a matrix [rows, heads * {dim}], got {tuple(t.shape)}")
-    return *_as_rows(t, name, t.shape[1], dt, dev), t.shape[1] // dim
+def _matrix(t, name, dim, c, dt, dev):
+    """(address, leading dimension, rows, columns) of a matrix of heads of `dim` values, of c columns if c is not 0."""
+    if t.dim() != 2 or t.dtype is not dt or t.get_device() != dev:
+        raise ValueError(f"{name} must be a matrix of {dt} on GPU {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    n, cols = t.shape
+    ld, one = t.stride()
+    if cols != c if c else cols == 0 or cols % dim:
+        raise ValueError(f"{name} must have {c or f'heads * {dim}'} columns, got {tuple(t.shape)}")
+    if one != 1 or (ld < cols and n > 1):
+        raise ValueError(f"{name}: rows of {cols} elements side by side, apart from each other (strides {t.stride()})")
+    return t.data_ptr(), ld if n > 1 else cols, n, cols
 
 
-def _whole(t, rows, name, of):
-    if t.numel() < rows:
-        raise ValueError(f"{name} has {t.numel()} entries, {of} {rows} rows")
-
-
-def _set_tokens(a, n, map_rows, streams, positions, period, idx, count, dev):
+def _set_tokens(a, n, streams, positions, period, idx, count, dev):
     """Fills in which tokens the rows of an n-row matrix are; returns the rows of the call so far."""
-    a.period, rows = period, n
-    if streams is not None:
-        a.stream, map_rows = _int32(streams, "streams", dev), streams.numel()
+    a.period, rows, known = period, n, None
     if positions is not None:
-        a.pos = _int32(positions, "positions", dev)
-        map_rows = positions.numel() if streams is None else min(map_rows, positions.numel())
+        a.pos, known = _int32(positions, "positions", dev), positions.numel()
+    if streams is not None:
+        a.stream, m = _int32(streams, "streams", dev), streams.numel()
+        known = m if known is None or m < known else known
     if idx is not None:
         a.idx, rows = _int32(idx, "idx", dev), idx.numel()
-        if streams is None and positions is None:
-            map_rows = _ROWS_MAX
+        a.map_rows = _ROWS_MAX if known is None else known
+    elif known is None:
+        a.map_rows = n
+    else:
+        if known < n:
+            raise ValueError(f"{known} streams or positions for a matrix of {n} rows")
+        a.map_rows = known
     if count is not None:
         a.count = _int32(count, "count", dev)
-    a.map_rows = map_rows
-    return _room(rows, n, "a matrix of rows", count)
+    return rows if n >= rows else _room(rows, n, "a matrix of rows", count)
 
 
 class Rotation:
@@ -793,39 +806,38 @@ class TokenCache:
         if pages is None and self.num_pages < streams * per_stream:
             raise ValueError(f"{self.num_pages} pages for {streams} streams of {per_stream}")
         self.codes, self.scales, self.pages = codes, scales, pages
-        self._scratch, self._captured, self._one_call = None, set(), threading.Lock()
+        # (scratch that a larger one has taken the place of is kept: a graph may hold its address)
+        self._scratch, self._scratch_at, self._kept, self._needs, self._one_call = None, (0, 0), [], {}, threading.Lock()
 
     def _args(self, a, n, streams, positions, idx, count):
         """Fills in the cache and the tokens of a call with an n-row matrix; returns its rows."""
-        dev = self.ctx.index
         a.dtype, a.heads, a.dim, a.page = self._code, self.heads, self.dim, self.page
         a.streams, a.length, a.num_pages = self.streams, self.length, self.num_pages
         a.codes, a.scales = self.codes.data_ptr(), self.scales.data_ptr()
         if self.pages is not None:
             a.pages = self.pages.data_ptr()
-        if streams is not None and positions is None:
-            raise ValueError("streams come with positions")
-        if idx is None:
-            for name, t in (("streams", streams), ("positions", positions)):
-                if t is not None:
-                    _whole(t, n, name, "a matrix of")
-        return _set_tokens(a, n, n, streams, positions, self.length if positions is None else 1, idx, count, dev)
+        if positions is None:
+            if streams is not None:
+                raise ValueError("streams come with positions")
+            return _set_tokens(a, n, None, None, self.length, idx, count, self.ctx.index)
+        return _set_tokens(a, n, streams, positions, 1, idx, count, self.ctx.index)
 
     def append(self, k, v, *, norm: RowNorm | None = None, rotation: Rotation | None = None, streams=None, positions=None, idx=None, count=None):
         """dcnn_cache_append: keys k [rows, heads * dim] (normed and rotated on the way) and values v into their tokens' places,
         which must be distinct."""
-        a, dev, c = CacheAppendArgs(), self.ctx.index, self.heads * self.dim
-        a.k, a.ldk, n = _as_rows(k, "k", c, self.dtype, dev)
+        a, ctx, c = CacheAppendArgs(), self.ctx, self.heads * self.dim
+        dev = ctx.index
+        a.k, a.ldk, n, _ = _matrix(k, "k", self.dim, c, self.dtype, dev)
         rows = self._args(a, n, streams, positions, idx, count)
-        a.v, a.ldv, n = _as_rows(v, "v", c, self.dtype, dev)
-        a.rows = _room(rows, n, "v", count)
+        a.v, a.ldv, n, _ = _matrix(v, "v", self.dim, c, self.dtype, dev)
+        a.rows = rows if n >= rows else _room(rows, n, "v", count)
         if norm is not None:
             a.k_norm_kind, a.k_norm_eps, a.k_norm_w, a.k_norm_b = norm.pointers(self.dim, self.dtype, dev)
         if rotation is not None:
             a.table, a.positions, a.rot, a.style = rotation.pointers(dev)
-        st = self.ctx.lib.dcnn_cache_append(self.ctx.handle, a)
+        st = ctx.lib.dcnn_cache_append(ctx.handle, a)
         if st:
-            self.ctx.check(st)
+            ctx.check(st)
 
     def read(self, *, streams=None, positions=None, idx=None, count=None, rows: int | None = None):
         """dcnn_cache_read: (keys, values) [rows, heads * dim] that the cache holds for tokens, zeros for those it has no place for.
@@ -837,13 +849,13 @@ class TokenCache:
             n = positions.numel()
         else:
             n = self.streams * self.length if rows is None else rows
-        a, c = CacheReadArgs(), self.heads * self.dim
+        a, ctx, c = CacheReadArgs(), self.ctx, self.heads * self.dim
         a.rows = self._args(a, n, streams, positions, idx, count)
-        k, v = (self.ctx.empty((n, c), self.dtype) for _ in range(2))
+        k, v = ctx.empty((2, n, c), self.dtype).unbind()
         a.k_out, a.v_out, a.ldk, a.ldv = k.data_ptr(), v.data_ptr(), c, c
-        st = self.ctx.lib.dcnn_cache_read(self.ctx.handle, a)
+        st = ctx.lib.dcnn_cache_read(ctx.handle, a)
         if st:
-            self.ctx.check(st)
+            ctx.check(st)
         return k, v
 
     def attend(self, q, *, lens=None, causal=False, window: int = 0, scale: float | None = None, streams=None, positions=None, idx=None, count=None, out=None):
@@ -852,38 +864,45 @@ class TokenCache:
         q_heads is a multiple of the cache's heads; consecutive query heads share one.  lens: int32 [streams], the tokens that
         count (None: `length`).  causal: none behind the row's position; window: only those nearer to it than so many (0: all).
         scale: of the products, 1 / sqrt(dim) where it is None.  out: a matrix to write."""
-        a, dev = CacheAttendArgs(), self.ctx.index
-        a.q, a.ldq, n, a.q_heads = _as_heads(q, "q", self.dim, self.dtype, dev)
+        a, ctx = CacheAttendArgs(), self.ctx
+        dev = ctx.index
+        a.q, a.ldq, n, c = _matrix(q, "q", self.dim, 0, self.dtype, dev)
         rows = self._args(a, n, streams, positions, idx, count)
         if out is None:
-            out = self.ctx.empty((rows, a.q_heads * self.dim), self.dtype)
-            a.y, a.ldy = out.data_ptr(), a.q_heads * self.dim
+            out = ctx.empty((rows, c), self.dtype)
+            a.y, a.ldy = out.data_ptr(), c
         else:
-            a.y, a.ldy, n = _as_rows(out, "out", a.q_heads * self.dim, self.dtype, dev)
+            a.y, a.ldy, n, _ = _matrix(out, "out", self.dim, c, self.dtype, dev)
             rows = _room(rows, n, "out", count)
         if lens is not None:
             a.lens = _int32(lens, "lens", dev)
-            _whole(lens, self.streams, "lens", "the cache's streams are")
-        a.rows, a.causal, a.window = rows, 1 if causal else 0, window
+            if lens.numel() < self.streams:
+                raise ValueError(f"lens of {lens.numel()} streams, the cache has {self.streams}")
+        q_heads = c // self.dim
+        a.rows, a.q_heads, a.window = rows, q_heads, window
+        if causal:
+            a.causal = 1
         a.scale = self.dim ** -0.5 if scale is None else scale
+        need = self._needs.get((rows, q_heads))
+        if need is None:
+            need = ctx.lib.dcnn_cache_scratch_bytes(self._code, rows, q_heads, self.heads, self.dim, self.streams, self.length)
+            if len(self._needs) < 4096:
+                self._needs[rows, q_heads] = need
         with self._one_call:                                      # (a call's kernels follow each other: both use the scratch)
-            a.scratch, a.scratch_bytes = self._scratch_for(rows, a.q_heads)
-            st = self.ctx.lib.dcnn_cache_attend(self.ctx.handle, a)
+            a.scratch, a.scratch_bytes = self._scratch_at if need <= self._scratch_at[1] else self._larger_scratch(need)
+            st = ctx.lib.dcnn_cache_attend(ctx.handle, a)
             if st:
-                self.ctx.check(st)
+                ctx.check(st)
         return out
 
-    def _scratch_for(self, rows, q_heads):
-        """(address, bytes) of scratch for a call; a larger one takes the place of a smaller one."""
-        need = self.ctx.lib.dcnn_cache_scratch_bytes(self._code, rows, q_heads, self.heads, self.dim, self.streams, self.length)
-        scratch, capturing = self._scratch, self.ctx.capturing()
-        if scratch is None or scratch.numel() < need:
-            scratch = self.ctx.empty(max(need, 256), torch.uint8)
-            if not capturing:                                     # (else it is the graph's)
-                self._scratch = scratch
-        elif capturing:
-            self._captured.add(scratch)
-        return scratch.data_ptr(), scratch.numel()
+    def _larger_scratch(self, need):
+        """(address, bytes) of new scratch, which takes the place of the one before it, unless a graph is being captured: then it is the graph's."""
+        scratch = self.ctx.empty(max(need, 256), torch.uint8)
+        at = scratch.data_ptr(), scratch.numel()
+        self._kept.append(scratch)
+        if not self.ctx.capturing():
+            self._scratch, self._scratch_at = scratch, at
+        return at
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

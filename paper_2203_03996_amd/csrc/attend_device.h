@@ -77,6 +77,12 @@ template <typename T> __device__ __forceinline__ void load_operand(const T* p, i
     }
 }
 
+// The larger of a lane's value and that of the lane 32 on, or before.
+__device__ __forceinline__ float max_of_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
 // Tiles that each of the `shares` workgroups of a head takes: a tile for each wave at least.
 __device__ __forceinline__ int share_of(int tiles, int shares) {
     const int n = (tiles + shares - 1) / shares;

@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
-                m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                m = max_of_halves(m);
                 m *= a.factor;                                         // (the factor is above zero)
                 // (weights up to 2^8 do as well as those up to one: sums are scaled anew where a column's maximum has grown by more than that)
                 if (__any(m > top + 8.0f)) {

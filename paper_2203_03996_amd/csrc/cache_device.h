@@ -26,10 +26,12 @@ __device__ __forceinline__ int page_of(const CacheArgs& c, int stream, int block
 // The same where stream and block are one for all lanes: through the scalar cache, so that it waits for no other load.
 __device__ __forceinline__ int page_of_all(const CacheArgs& c, int stream, int block) {
     typedef __attribute__((address_space(4))) const int32_t ConstInt;
-    if ((uint32_t)block >= (uint32_t)c.per_stream) return -1;
-    const int64_t at = (int64_t)stream * c.per_stream + block;
-    const int page = c.pages != nullptr ? ((ConstInt*)(uintptr_t)c.pages)[at] : (int)at;
-    return (uint32_t)page < (uint32_t)c.num_pages ? page : -1;
+    const bool in = (uint32_t)block < (uint32_t)c.per_stream;
+    const int64_t at = (int64_t)stream * c.per_stream + (in ? block : 0);
+    // (no branches: what is loaded is waited for where it is used.  Without a table a word of the codes is read, and not looked at)
+    const int entry = *((ConstInt*)(c.pages != nullptr ? (uintptr_t)(c.pages + at) : (uintptr_t)c.codes));
+    const int page = c.pages != nullptr ? entry : (int)at;
+    return in && (uint32_t)page < (uint32_t)c.num_pages ? page : -1;
 }
 // Tokens before the first one of a page's head; `which`: 0 keys, 1 values.
 __device__ __forceinline__ int64_t head_of_page(const CacheArgs& c, int page, int which, int head) {
