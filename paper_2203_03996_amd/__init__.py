@@ -8,4 +8,4 @@ from .binding import (  # noqa: F401
     ACCUM, ACT, CONCAT, GAVGPOOL, UPSAMPLE_BILINEAR, ACT_CODES, ACT_NONE, ACT_RELU, ACT_RELU6, CONV, DELTAGEN, DWCONV, F16, F32, MAXPOOL, UPSAMPLE,
     BF16, I8, Context, DcnnError, Delta, Layer, Net, Rotation, RowNorm, RowWeights, TokenCache, EXPORTS, LIB_PATH, load_library, make_desc,
 )
-from .blocks import RowBlock, TokenStack  # noqa: E402,F401
+from .blocks import AttentionBlock, RowBlock, TokenStack  # noqa: E402,F401

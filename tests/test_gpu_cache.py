@@ -630,6 +630,83 @@ def test_captured_steps_replayed_with_other_lengths(ctx):
             assert torch.equal(got, want), f"replay {i}"
 
 
+def attention_block(ctx, gen, dt, c, streams, side, q_heads, heads, dim, **kw):
+    cache = pkg.TokenCache(ctx, streams, side * side, heads, dim, dtype=TYPES[dt][0], page=16)
+    norm = lambda n: pkg.RowNorm("rms", rand(gen, n, dt=dt, scale=0.1, mean=1.0))  # noqa: E731
+    return pkg.AttentionBlock(ctx, rand(gen, c, (q_heads + 2 * heads) * dim, dt=dt, scale=c ** -0.5), rand(gen, q_heads * dim, c, dt=dt, scale=(q_heads * dim) ** -0.5), cache, q_heads,
+                              qkv_bias=rand(gen, (q_heads + 2 * heads) * dim, dt=dt, scale=0.1), q_norm=norm(dim), k_norm=norm(dim), rotation=pkg.Rotation.of_pixels(side, side, dim),
+                              pre=norm(c), post=norm(c), scale=0.5, **kw)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_attention_blocks_on_flagged_pixels(ctx, dt):
+    """A step renews the keys and values of the flagged pixels, as a first frame of the new map has them, and these pixels' rows; the attention in it is the plain one."""
+    streams, side, c, q_heads, heads, dim = 3, 9, 96, 4, 2, 32
+    n = side * side
+    gen = seeded(28)
+    block = attention_block(ctx, gen, dt, c, streams, side, q_heads, heads, dim)
+    x = rand(gen, streams, side, side, c, dt=dt)
+    y = torch.zeros_like(x)
+    block.step(x, y)
+    ctx.sync()
+    before = y.clone()
+    m = 40
+    idx = torch.full((streams * n,), 1 << 30, dtype=torch.int32, device="cuda")
+    idx[:m] = torch.randperm(streams * n, device="cuda", generator=gen)[:m].sort().values.to(torch.int32)
+    at = idx[:m].long()
+    x.view(-1, c)[at] = rand(gen, m, c, dt=dt)
+    block.step(x, y, idx, ints(m))
+    ctx.sync()
+    rest = torch.ones(streams * n, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert torch.equal(y.view(-1, c)[rest], before.view(-1, c)[rest]) and not torch.equal(y.view(-1, c)[at], before.view(-1, c)[at])
+    codes, scales = block.cache.codes.clone(), block.cache.scales.clone()
+    block.step(x, torch.empty_like(x))
+    ctx.sync()
+    assert torch.equal(block.cache.codes, codes) and torch.equal(block.cache.scales, scales)
+    # the block's calls one by one
+    rows = block.qkv.linear(x, pre=block.pre, idx=idx, count=ints(m))
+    q = ctx.rows_heads(rows[:, :block.q_end], dim=dim, q_norm=block.q_norm, rotation=block.rotation, idx=idx, count=ints(m))
+    mixed = block.cache.attend(q, idx=idx, count=ints(m))
+    out = block.out.linear(mixed, count=ints(m))
+    want = before.clone()
+    ctx.rows_norm(x, out, post=block.post, scale=block.scale, idx=idx, count=ints(m), y=want)
+    ctx.sync()
+    assert torch.equal(y, want)
+    pages = torch.arange(streams * 6, device="cuda").view(streams, 6)
+    plain_out, slack = plain.attend64(q[:m], codes, scales, pages, 16, at // n, at % n, [n] * streams, dim ** -0.5, False, 0, 1, TYPES[dt][1], 2.0 ** -25 if dt == "f16" else 0.0)
+    close(mixed[:m], plain_out, dt, slack, "attention of the block")
+
+
+def test_a_stack_of_attention_and_rows(ctx):
+    """Blocks of both kinds behind each other: a step on every pixel is a first frame; a step on none leaves everything."""
+    gen = seeded(29)
+    c, streams, side = 64, 2, 8
+    half = lambda *shape, scale=1.0, mean=0.0: rand(gen, *shape, dt="f16", scale=scale, mean=mean)  # noqa: E731
+    blocks = [attention_block(ctx, gen, "f16", c, streams, side, 2, 2, 32, gate=half(c, scale=0.1, mean=0.5)),
+              pkg.RowBlock(ctx, half(c, 128, scale=c ** -0.5), half(128, c, scale=0.1), pre=pkg.RowNorm("layer", half(c, mean=1.0), half(c)), scale=0.5)]
+    stack = pkg.TokenStack(blocks)
+    x = half(streams, side, side, c)
+    first = stack.init(x).clone()
+    every = torch.arange(streams * side * side, dtype=torch.int32, device="cuda")
+    again = stack.step(x, every, ints(len(every))).clone()
+    none = stack.step(half(streams, side, side, c), every, ints(0)).clone()
+    ctx.sync()
+    assert torch.isfinite(first).all() and torch.equal(first, again) and torch.equal(first, none)
+    with pytest.raises(ValueError):
+        blocks[0].step(half(streams, side, side + 1, c), half(streams, side, side + 1, c))
+
+
+def test_attention_blocks_that_do_not_fit_are_refused(ctx):
+    half = lambda *shape: torch.zeros(*shape, dtype=torch.float16, device="cuda")  # noqa: E731
+    cache = pkg.TokenCache(ctx, 1, 16, 2, 32)
+    pkg.AttentionBlock(ctx, half(64, 8 * 32), half(4 * 32, 64), cache, 4)
+    for qkv, out, q_heads, rotation in ((half(64, 7 * 32), half(4 * 32, 64), 4, None), (half(64, 8 * 32), half(3 * 32, 64), 4, None), (half(64, 7 * 32), half(3 * 32, 64), 3, None),
+                                        (half(64, 8 * 32), half(4 * 32, 64), 4, pkg.Rotation.of_positions(17, 32))):
+        with pytest.raises(ValueError):
+            pkg.AttentionBlock(ctx, qkv, out, cache, q_heads, rotation=rotation)
+
+
 def test_calls_run_on_the_contexts_stream(ctx):
     """With torch on another stream: new outputs belong to the context's stream, whose work waits for nothing else."""
     cache = filled(ctx, 2, 100, 1, 64, "bf16")
