@@ -45,7 +45,7 @@ __device__ __forceinline__ int wave_min(int v) {
 template <typename T, int NB> struct TileShape {
     // queries, sums, products and weights of a lane: two waves to a SIMD where they leave room for addresses and codes
     static constexpr int registers = NB * 8 * Operand<T>::TERMS + NB * 16 + 32 + 16 * Operand<T>::TERMS;
-    static constexpr int waves = registers <= 176 ? 2 : 1;
+    static constexpr int waves = registers <= 112 ? 3 : registers <= 176 ? 2 : 1;
     static constexpr int bytes = 2 * 2 * kTokens * NB * 64;            // two buffers of keys and values
 };
 
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
     int turns = 512 / ((int64_t)tiles * heads * a.splits < 512 ? tiles * heads * a.splits : 512);
     turns = turns < kVectors ? turns : kVectors;
     const int page_mask = (1 << a.cache.page_shift) - 1;
-    const int64_t page_tokens = (int64_t)heads << a.cache.page_shift;
+    const uint32_t page_tokens = (uint32_t)heads << a.cache.page_shift;
     for (int64_t item = blockIdx.x; item < (int64_t)tiles * heads * a.splits * turns; item += gridDim.x) {
         int rest = (int)(item / heads);
         const int head = (int)(item % heads), part = rest % a.splits;
@@ -129,20 +129,27 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             u32x4 raw[CHUNKS];
             uint32_t byte[CHUNKS];
             bool drop[CHUNKS];
-            const auto page_at = [&](int t) {
-                if constexpr (WHOLE) return page_of_all(a.cache, of, (start + t * kTokens) >> a.cache.page_shift);
+            // (keys 0, values 1, nothing 2: one for all of a wave's lanes)
+            const auto which_of = [&](int n) { return NB % 4 == 0 ? 4 * n / NB : (wave + 4 * n) / NB; };
+            // the entry of a tile's page in the table, and what it says: looked at one tile after it was asked for
+            const auto entry_at = [&](int t) {
+                if constexpr (WHOLE) return entry_of_all(a.cache, of, (start + t * kTokens) >> a.cache.page_shift);
                 else return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift);
             };
+            const auto page_at = [&](int t, int entry) {
+                if constexpr (WHOLE) return page_of_entry(a.cache, of, (start + t * kTokens) >> a.cache.page_shift, entry);
+                else return entry;
+            };
             const auto load = [&](int t, int page) {
+                const uint64_t tile_slot = (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (2 * page_tokens) + ((start + t * kTokens) & page_mask);
 #pragma unroll
                 for (int n = 0; n < CHUNKS; ++n) {
-                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB;
-                    const int which = __builtin_amdgcn_readfirstlane(c / (kTokens * NB)), t_at = start + t * kTokens + token_in;
+                    const int within = (tid + 256 * n) % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB, which = which_of(n), t_at = start + t * kTokens + token_in;
                     if (NB % 2 != 0 && which > 1) break;
-                    bool counts = t_at >= first && t_at < last;
+                    bool counts = (uint32_t)(t_at - first) < (uint32_t)(last - first);
                     if constexpr (WHOLE) {
                         // the tile's first token, one for all lanes, and 32-bit offsets from it
-                        const int64_t slot = ((int64_t)(page < 0 ? 0 : page) * 2 + which) * page_tokens + ((int64_t)head << a.cache.page_shift) + ((start + t * kTokens) & page_mask);
+                        const uint64_t slot = tile_slot + ((uint32_t)(which * heads + head) << a.cache.page_shift);
                         const uint8_t *const codes = a.cache.codes + slot * (D / 2), *const scales = a.cache.scales + slot * NB;
                         raw[n] = *reinterpret_cast<const u32x4*>(codes + (uint32_t)(token_in * (D / 2) + b * 16));
                         byte[n] = scales[(uint32_t)(token_in * NB + b)];
@@ -160,14 +167,16 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             const auto stage = [&](int buffer) {
 #pragma unroll
                 for (int n = 0; n < CHUNKS; ++n) {
-                    const int c = tid + 256 * n, within = c % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB;
-                    const int which = __builtin_amdgcn_readfirstlane(c / (kTokens * NB));
+                    const int within = (tid + 256 * n) % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB, which = which_of(n);
                     if (NB % 2 != 0 && which > 1) break;
-                    // a value that is NaN is not multiplied (a weight of zero would make it one of rows that do not see it): it is noted
-                    const bool nan = which == 1 && byte[n] == 255 && !drop[n];
-                    const uint64_t noted = __ballot(nan);
-                    if (which == 1 && lane == 0) broken[buffer][within / 64] = noted;
-                    const float scale = scale_of_byte(nan || drop[n] ? 0 : byte[n]);
+                    float scale = scale_of_byte(byte[n]);
+                    // keys of tokens that do not count may be anything: their products are not looked at.  Values are multiplied by weights of zero there,
+                    // and so is a value that is NaN for rows that do not see it: they become zeros, and the second kind is noted
+                    if (which == 1) {
+                        const uint64_t noted = __ballot(byte[n] == 255 && !drop[n]);
+                        if (lane == 0) broken[buffer][within / 64] = noted;
+                        scale = drop[n] || byte[n] == 255 ? 0.0f : scale;
+                    }
                     uint8_t* const row = lds + (buffer * 2 + which) * PLANE + token_in * ROW;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) *reinterpret_cast<Op*>(row + tile_column<NB>(token_in, 4 * b + i) * 16) = decode8<T>(raw[n][i], scale);
@@ -175,16 +184,17 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             };
             // which sixteens of a tile's tokens have a page
             const auto sixteens = [&](int p) { return WHOLE ? (p >= 0 ? 15u : 0u) : (uint32_t)__ballot(p >= 0) & 15u; };
-            int page = page_at(from);
+            int page = page_at(from, entry_at(from));
             uint32_t paged = sixteens(page), paged_next = 0;
             load(from, page);
-            page = page_at(from + 1);
+            int entry = entry_at(from + 1);
             __syncthreads();                                           // (a segment before this one is done with the buffers)
             stage(from & 1);
             if (from + 1 < to) {
+                page = page_at(from + 1, entry);
                 paged_next = sixteens(page);
                 load(from + 1, page);
-                page = page_at(from + 2);
+                entry = entry_at(from + 2);
             }
             for (int t = from; t < to; ++t) {
                 __syncthreads();                                       // this tile is there, and all are done with the one before it
@@ -192,9 +202,10 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                 const uint32_t has_page = paged;
                 paged = paged_next;
                 if (t + 2 < to) {                                      // (nothing of these loads is looked at before the next tile's turn)
+                    page = page_at(t + 2, entry);
                     paged_next = sixteens(page);
                     load(t + 2, page);
-                    page = page_at(t + 3);
+                    entry = entry_at(t + 3);
                 }
                 const int t0 = start + t * kTokens;
                 if (t0 + kTokens <= any_from || t0 >= any_to) continue;
