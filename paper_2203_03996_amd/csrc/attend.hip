@@ -3,14 +3,15 @@
 
 namespace dcnn {
 
-// The parts of a row and head as one.
-template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    constexpr int E = (D + 63) / 64;
-    __shared__ float sums[4][D];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+// The parts of a row and head as one: out = sum_s 2^(top_s - top) part_s / sum_s 2^(top_s - top) sum_s.  What it takes is the way to memory and back, so
+// a wave takes few parts (W = 1) by itself: with four and a barrier, 512 rows of 32 heads in two parts took 22 us.  Many are shared by four.
+template <typename T, int D, int W> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    constexpr int E = (D + 63) / 64, UNITS = 4 / W;
+    __shared__ float sums[W == 1 ? 1 : 4][D], totals[4];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), first = W == 1 ? 0 : wave;
     const int count = row_count(a.tokens.count, a.tokens.rows);
     const int q_heads = a.cache.heads * a.group;
-    for (int unit = blockIdx.x; unit < count * q_heads; unit += gridDim.x) {
+    for (int unit = (int)blockIdx.x * UNITS + (W == 1 ? wave : 0); unit < count * q_heads; unit += gridDim.x * UNITS) {
         const int r = unit / q_heads, q_head = unit % q_heads;
         // the row's parts: those of its tile, or those of the workgroups that its tokens were shared among
         int parts = a.splits, from = 0, tiles_before = 0, share = 0;
@@ -33,7 +34,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_
         const float base = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, o[E] = {};
 #pragma unroll 4
-        for (int s = wave; s < parts; s += 4) {
+        for (int s = first; s < parts; s += W) {
             const int64_t at = part(s);
             const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
             total += a.stat[at * 2 + 1] * w;
@@ -41,52 +42,70 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_
             for (int e = 0; e < E; ++e)
                 if (lane + 64 * e < D) o[e] += a.part[at * D + lane + 64 * e] * w;
         }
+        T* const y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + (int64_t)q_head * D;
+        if constexpr (W == 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
-        __shared__ float totals[4];
-        if (lane == 0) totals[wave] = total;
-        __syncthreads();
-        total = totals[0] + totals[1] + totals[2] + totals[3];
-        if ((int)threadIdx.x < D) {
-            const int d = threadIdx.x;
-            const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
-            static_cast<T*>(a.y)[(int64_t)r * a.ldy + (int64_t)q_head * D + d] = (T)(total == 0.0f ? 0.0f : v / total);
+            for (int e = 0; e < E; ++e)
+                if (lane + 64 * e < D) y[lane + 64 * e] = (T)(total == 0.0f ? 0.0f : o[e] / total);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
+            if (lane == 0) totals[wave] = total;
+            __syncthreads();
+            total = totals[0] + totals[1] + totals[2] + totals[3];
+            if ((int)threadIdx.x < D) {
+                const int d = threadIdx.x;
+                const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
+                y[d] = (T)(total == 0.0f ? 0.0f : v / total);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
 AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int dim, int64_t streams, int64_t length) {
     const int64_t group = q_heads / heads;
     AttendPlan p;
-    p.tiles = rows > 2 * streams;
+    // A tile of 128 query vectors reads its tokens once, a row alone reads them for itself: some rows of a stream find them in the caches.
+    // (16 streams of 4096 tokens, 32 heads on 8 of 128: four rows each take 46 us alone and 58 in tiles, six 69 and 82, eight 85 and 57.)
+    p.tiles = rows > 6 * streams;
     if (p.tiles) {
-        const int64_t units = cdiv(rows * group, 128) * heads, wanted = cdiv(512, units < 1 ? 1 : units), most = cdiv(length, 512);
+        // two workgroups to a compute unit, with 256 tokens each at least (512 rows of a stream of 8192 tokens, the same heads: 284 us unsplit, 96 us;
+        // 64 rows of 2048: 81, 32 with 512 tokens at least, 23)
+        const int64_t units = cdiv(rows * group, 128) * heads, wanted = cdiv(512, units < 1 ? 1 : units), most = cdiv(length, 256);
         p.splits = (int)(wanted < most ? wanted : most);
         p.parts = p.splits > 1 ? rows * q_heads * p.splits : 0;
     } else {
-        // as many workgroups as are resident at a time; where every row is a few tiles, or rows are many, one takes whole rows
+        // As many workgroups as are resident at a time, each an equal part of the tokens of all rows: their lengths may be any.  Where every row is a
+        // few tiles, or rows are many, workgroups take whole rows and need neither the plan nor the join (a row of the same heads: 512 tokens take
+        // 8.3 us whole and 10.5 shared, 1024 11.3 and 10.7, 2048 17.0 and 11.1; 512 rows of 1024, 113 and 126).
         const int64_t columns = heads * cdiv(group, 16), resident = dim * (dtype_size == 4 ? 3 : 1) <= 192 ? 512 : 256;
         const int64_t shares = resident / columns;
-        p.splits = shares > 1 && rows <= kShareRows && length > 256 && rows * cdiv(length, 64) < 1 << 30 ? (int)shares : 0;
+        p.splits = shares > 1 && rows <= kShareRows && length > 1024 && rows * cdiv(length, 64) < 1 << 30 ? (int)shares : 0;
         p.parts = columns * p.splits * 32;
     }
     return p;
 }
 
-template <typename T> static dcnn_status launch_join(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
-    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group, most = (int64_t)ctx->num_cu * 16;
-    const dim3 grid((unsigned)(outs < most ? outs : most));
-    switch (dim) {
-        case 32: hipLaunchKernelGGL((attend_join_kernel<T, 32>), grid, dim3(256), 0, ctx->stream, a); break;
-        case 64: hipLaunchKernelGGL((attend_join_kernel<T, 64>), grid, dim3(256), 0, ctx->stream, a); break;
-        case 96: hipLaunchKernelGGL((attend_join_kernel<T, 96>), grid, dim3(256), 0, ctx->stream, a); break;
-        case 128: hipLaunchKernelGGL((attend_join_kernel<T, 128>), grid, dim3(256), 0, ctx->stream, a); break;
-        case 192: hipLaunchKernelGGL((attend_join_kernel<T, 192>), grid, dim3(256), 0, ctx->stream, a); break;
-        default: hipLaunchKernelGGL((attend_join_kernel<T, 256>), grid, dim3(256), 0, ctx->stream, a); break;
-    }
+template <typename T, int D> static dcnn_status launch_join_dim(dcnn_ctx* ctx, const AttendArgs& a) {
+    // parts of a row: as many as its tile has, or its part of those of the rows together
+    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group, most = (int64_t)ctx->num_cu * 16, parts = a.plan != nullptr ? a.splits / a.tokens.rows + 2 : a.splits;
+    if (parts <= 8) {
+        const int64_t groups = cdiv(outs, 4);
+        hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)(groups < most ? groups : most)), dim3(256), 0, ctx->stream, a);
+    } else hipLaunchKernelGGL((attend_join_kernel<T, D, 4>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "attend_join_kernel launch");
+}
+template <typename T> static dcnn_status launch_join(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
+    switch (dim) {
+        case 32: return launch_join_dim<T, 32>(ctx, a);
+        case 64: return launch_join_dim<T, 64>(ctx, a);
+        case 96: return launch_join_dim<T, 96>(ctx, a);
+        case 128: return launch_join_dim<T, 128>(ctx, a);
+        case 192: return launch_join_dim<T, 192>(ctx, a);
+        default: return launch_join_dim<T, 256>(ctx, a);
+    }
 }
 
 dcnn_status launch_attend(dcnn_ctx* ctx, int dtype, int dim, const AttendPlan& plan, const AttendArgs& a) {

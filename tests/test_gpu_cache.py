@@ -508,6 +508,24 @@ def test_attend_long_cache_in_parts(ctx, dt):
         check_attend(cache, dt, q, zero, pos, [19987], causal=True, streams=zero, positions=pos, what=f"{rows} rows")
 
 
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dim", DIMS)
+def test_attend_long_rows_of_every_width(ctx, dt, dim, page):
+    """Lengths that one workgroup does not take alone, with a page missing and a value that is NaN, and some rows of each stream."""
+    lens = [1100, 0, 1025, 1, 700]
+    cache = filled(ctx, 5, 1100, 2, dim, dt, page=page, written=lens)
+    cache.pages[0, 3] = -1
+    at, slot = places(cache, torch.full((1,), 2, device="cuda"), torch.full((1,), 1001, device="cuda"))
+    cache.scales[at[0], 1, 1, slot[0], 0] = 255         # head 1, token 1001 of stream 2
+    for each in (1, 4):
+        q = rand(seeded(dim + each), 5 * each, 2 * 3 * dim, dt=dt, scale=1.5)
+        stream = torch.arange(5, dtype=torch.int32, device="cuda").repeat_interleave(each)
+        pos = ints(*[max(0, n - 1 - 300 * i) for n in lens for i in range(each)])
+        got = check_attend(cache, dt, q, stream, pos, lens, True, streams=stream, positions=pos, what=f"{each} rows of each").view(-1, 2, 3, dim)
+        assert torch.equal(torch.isnan(got[:, 1, :, :32]).all(2).all(1), (stream == 2) & (pos >= 1001)) and not torch.isnan(got[:, 0]).any()
+
+
 @pytest.mark.parametrize("rows", [2, 3, 64, 200, 511, 512, 513, 700])
 @pytest.mark.parametrize("lengths", ["none", "one long", "first", "last", "gaps", "all alike", "one tile", "mixed"])
 def test_attend_tokens_shared_among_workgroups(ctx, rows, lengths):
