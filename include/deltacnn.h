@@ -45,7 +45,8 @@ typedef enum {
     DCNN_EUNSUPPORTED = 7
 } dcnn_status;
 
-/* DCNN_BF16 and DCNN_I8 exist for the row operators (dcnn_rows_*) only; layers and networks refuse them. */
+/* DCNN_BF16 exists for the row operators and the cache (dcnn_rows_*, dcnn_cache_*) only, DCNN_I8 for the former; layers and
+ * networks refuse them. */
 typedef enum { DCNN_F32 = 0, DCNN_F16 = 1, DCNN_BF16 = 2, DCNN_I8 = 3 } dcnn_dtype;
 
 typedef enum {
@@ -437,9 +438,10 @@ typedef struct {
 /* Writes the keys (normed and rotated first) and values of rows into the cache.  The scale of 32 values is the smallest
  * power of two with max|v| <= 6 * scale (2^-126 at least; at most 2^13 in fp16 and 2^125 else, so that what is held is
  * finite: larger magnitudes are held as 6 * scale), and each becomes the code next to v / scale, ties to the even one (a
- * zero is code 0); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed in fp64 up to that rounding: a code does not depend on the
- * order of a sum.  Rows without a token, or with a position outside 0 .. length-1, write nothing.  The (stream, position)
- * of rows must be distinct.  rows * heads at most 2^30. */
+ * zero is code 0); 32 values among which there is a NaN or an infinity become NaN (codes 0, scale 255).  Keys are computed
+ * in fp64 up to that rounding: a code does not depend on the order of a sum.  Rows without a token, or with a position
+ * outside 0 .. length-1, write nothing.  The places that rows have in the cache must be distinct: no token twice, and none
+ * of two streams in a page that they share.  rows * heads at most 2^30. */
 typedef struct {
     dcnn_cache      cache;
     dcnn_row_tokens tokens;

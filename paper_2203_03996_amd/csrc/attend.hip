@@ -33,7 +33,7 @@ template <typename T, int D, int W> __global__ __launch_bounds__(256) void atten
         for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
         const float base = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, o[E] = {};
-#pragma unroll 4
+#pragma unroll 8
         for (int s = first; s < parts; s += W) {
             const int64_t at = part(s);
             const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
@@ -89,9 +89,8 @@ AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int
 }
 
 template <typename T, int D> static dcnn_status launch_join_dim(dcnn_ctx* ctx, const AttendArgs& a) {
-    // parts of a row: as many as its tile has, or its part of those of the rows together
-    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group, most = (int64_t)ctx->num_cu * 16, parts = a.plan != nullptr ? a.splits / a.tokens.rows + 2 : a.splits;
-    if (parts <= 8) {
+    const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group, most = (int64_t)ctx->num_cu * 16;
+    if (a.plan == nullptr && a.splits <= 8) {                  // (of rows alone, one may have most of the parts)
         const int64_t groups = cdiv(outs, 4);
         hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)(groups < most ? groups : most)), dim3(256), 0, ctx->stream, a);
     } else hipLaunchKernelGGL((attend_join_kernel<T, D, 4>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);

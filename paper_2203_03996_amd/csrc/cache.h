@@ -56,7 +56,8 @@ struct AttendArgs {
     int blocks;                                // sixteens of them
     float factor;                              // |scale| * log2(e), above zero
     int negate;                                // scale is below zero: the queries' opposites
-    int causal, window;
+    int causal;
+    int64_t window;                            // 0: none
     const int32_t* lens;
     FastDiv by_group;
     int splits;                                // tiles: workgroups that share the tokens of a tile of rows; else: that share all rows' of a head (0: none do)

@@ -202,7 +202,8 @@ dcnn_status dcnn_cache_attend(dcnn_ctx* ctx, const dcnn_cache_attend_args* p) {
     // (a scale of zero: so small a number that any product with it is as good as zero, and what is masked, minus infinity, stays that)
     a.factor = __builtin_fabsf(p->scale) * 1.44269504088896341f, a.negate = p->scale < 0.0f;
     if (a.factor == 0.0f) a.factor = 0x1p-149f;
-    a.causal = p->causal != 0, a.window = (int)(p->window < kCacheMaxLength ? p->window : kCacheMaxLength);
+    if (a.factor > 3.4028234e38f) a.factor = 3.4028234e38f;    // (finite, for products of zero)
+    a.causal = p->causal != 0, a.window = p->window < (int64_t)1 << 33 ? p->window : (int64_t)1 << 33;    // (positions are 32 bits)
     a.lens = p->lens_dev;
     a.by_group = make_fastdiv((uint32_t)a.group);
     a.splits = plan.splits;

@@ -438,6 +438,28 @@ def test_attend_scales(ctx, dt, scale):
         check_attend(cache, dt, q, zero, zero, None, scale=scale, streams=zero, positions=zero, what=f"scale {scale}")
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_windows_and_positions_of_any_size(ctx, rows):
+    """Positions far behind the cache see what a window as large reaches; the last one that is not reached is seen by none."""
+    cache = filled(ctx, 1, 100, 1, 64, "f16")
+    q = rand(seeded(31), rows, 2 * 64, dt="f16")
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    far = zero + (2 ** 31 - 1)
+    for window in (2 ** 31, 2 ** 31 - 50, 2 ** 31 - 99, 2 ** 31 - 100, 2 ** 40, 2 ** 62):
+        got = check_attend(cache, "f16", q, zero, far, None, window=window, streams=zero, positions=far, what=f"window {window}")
+        assert bool((got == 0).all()) == (window == 2 ** 31 - 100)
+    check_attend(cache, "f16", q, zero, -far, None, window=2 ** 40, streams=zero, positions=-far, what="before zero")
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_largest_scale_of_zeros(ctx, rows):
+    """The largest finite scale: products of zero stay zero, all tokens weigh the same."""
+    cache = filled(ctx, 1, 100, 1, 64, "f32")
+    q = torch.zeros(rows, 2 * 64, device="cuda")
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    check_attend(cache, "f32", q, zero, zero, None, scale=torch.finfo(torch.float32).max, streams=zero, positions=zero)
+
+
 @pytest.mark.parametrize("dt", list(TYPES))
 @pytest.mark.parametrize("rows", [1, 70])
 def test_attend_products_far_apart(ctx, dt, rows):
