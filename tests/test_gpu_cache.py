@@ -6,6 +6,8 @@ Tolerances follow from the arithmetic.  U32 and U are the unit round-offs of fp3
 * the cache: codes and scales are equal to those of 64 bits.
 * attention: see attend64, and U of the result.
 * results below the storage type's normal range are good to half of its smallest step."""
+import threading
+
 import pytest
 import torch
 
@@ -668,6 +670,64 @@ def test_captured_steps_replayed_with_other_lengths(ctx):
             want = step()
             side.synchronize()
             assert torch.equal(got, want), f"replay {i}"
+
+
+@pytest.mark.parametrize("dim", [64, 192])
+def test_captured_prompts_replayed_with_other_pages(ctx, dim):
+    """Rows of a prompt, in tiles whose tokens are split, as a graph: replayed with new rows and pages handed out anew, with eager work between."""
+    heads, n, rows = 2, 700, 40
+    gen = seeded(27)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        own = pkg.Context(0)
+        cache = filled(own, 1, n, heads, dim, "bf16", page=64)
+        q = rand(gen, rows, 4 * dim, dt="bf16")
+        pos, zero = torch.arange(n - rows, n, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+
+        def step():
+            return cache.attend(q, streams=zero, positions=pos, causal=True)
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured = step()
+        for i in range(4):
+            q.copy_(rand(gen, rows, 4 * dim, dt="bf16"))
+            cache.pages.copy_(cache.pages.roll(1, 1))
+            graph.replay()
+            side.synchronize()
+            got = captured.clone()
+            want = step()
+            side.synchronize()
+            # (bits: a page that was the last holds anything behind the last token, NaN among it)
+            assert torch.equal(got.view(torch.int16), want.view(torch.int16)), f"replay {i}: {(got != want).sum()} differ, {got.isnan().sum()} and {want.isnan().sum()} are NaN"
+
+
+def test_threads_that_share_a_cache(ctx):
+    """Calls of several threads on one cache: scratch that grows meanwhile is nobody's loss."""
+    cache = filled(ctx, 4, 1500, 2, 64, "f16", page=64)
+    gen = seeded(29)
+    calls = []
+    for rows in (4, 1, 4, 40, 90, 4, 200, 40):
+        q = rand(gen, rows, 4 * 64, dt="f16")
+        pos = torch.randint(0, 1500, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+        calls.append((q, pos, torch.arange(rows, dtype=torch.int32, device="cuda") % 4))
+    want = [cache.attend(q, streams=s, positions=p, causal=True) for q, p, s in calls]
+    ctx.sync()
+    other = pkg.TokenCache(ctx, 4, 1500, 2, 64, dtype=torch.float16, page=64, pages=cache.pages, codes=cache.codes, scales=cache.scales)
+    got = [None] * len(calls)
+
+    def work(i):
+        q, p, s = calls[i]
+        for _ in range(20):
+            got[i] = other.attend(q, streams=s, positions=p, causal=True)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    ctx.sync()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
 
 
 def attention_block(ctx, gen, dt, c, streams, side, q_heads, heads, dim, **kw):
