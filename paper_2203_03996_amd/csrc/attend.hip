@@ -3,15 +3,53 @@
 
 namespace dcnn {
 
-// The parts of a row and head as one: out = sum_s 2^(top_s - top) part_s / sum_s 2^(top_s - top) sum_s.  What it takes is the way to memory and back, so
-// a wave takes few parts (W = 1) by itself: with four and a barrier, 512 rows of 32 heads in two parts took 22 us.  Many are shared by four.
-template <typename T, int D, int W> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    constexpr int E = (D + 63) / 64, UNITS = 4 / W;
-    __shared__ float sums[W == 1 ? 1 : 4][D], totals[4];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), first = W == 1 ? 0 : wave;
+// The parts of a row and head as one: out = sum_s 2^(top_s - top) part_s / sum_s 2^(top_s - top) sum_s.  What it takes is the way to memory and back:
+// few parts are asked for all at once, by a wave for itself (512 rows of 32 heads of 128 in two parts took 22 us with four waves and a barrier); of rows
+// alone, one may have most of the parts, and four waves share them.
+constexpr int kFewParts = 8;
+
+template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a) {
+    constexpr int E = (D + 63) / 64;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int q_heads = a.cache.heads * a.group, units = row_count(a.tokens.count, a.tokens.rows) * q_heads, parts = a.splits;
+    for (int unit = (int)blockIdx.x * 4 + wave; unit < units; unit += gridDim.x * 4) {
+        const int64_t at = (int64_t)unit * parts;
+        float v[kFewParts][E], top = -INFINITY, sum = 0.0f;
+        if (lane < parts) top = a.stat[(at + lane) * 2], sum = a.stat[(at + lane) * 2 + 1];
+#pragma unroll
+        for (int s = 0; s < kFewParts; ++s)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[s][e] = s < parts && lane + 64 * e < D ? a.part[(at + s) * D + lane + 64 * e] : 0.0f;
+        float most = top;
+#pragma unroll
+        for (int d = 1; d < kFewParts; d *= 2) most = fmaxf(most, __shfl_xor(most, d, kWave));
+        // (a part that sees nothing has sums of zero)
+        const float w = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
+        float total = sum * w;
+#pragma unroll
+        for (int d = 1; d < kFewParts; d *= 2) total += __shfl_xor(total, d, kWave);
+        total = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, total)));
+        float o[E] = {};
+#pragma unroll
+        for (int s = 0; s < kFewParts; ++s) {
+            const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s));
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = s < parts ? __builtin_fmaf(v[s][e], ws, o[e]) : o[e];
+        }
+        const int r = unit / q_heads, q_head = unit - r * q_heads;
+        T* const y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + (int64_t)q_head * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < D) y[lane + 64 * e] = (T)(total == 0.0f ? 0.0f : o[e] / total);
+    }
+}
+template <typename T, int D> __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    constexpr int E = (D + 63) / 64;
+    __shared__ float sums[4][D], totals[4];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int count = row_count(a.tokens.count, a.tokens.rows);
     const int q_heads = a.cache.heads * a.group;
-    for (int unit = (int)blockIdx.x * UNITS + (W == 1 ? wave : 0); unit < count * q_heads; unit += gridDim.x * UNITS) {
+    for (int unit = blockIdx.x; unit < count * q_heads; unit += gridDim.x) {
         const int r = unit / q_heads, q_head = unit % q_heads;
         // the row's parts: those of its tile, or those of the workgroups that its tokens were shared among
         int parts = a.splits, from = 0, tiles_before = 0, share = 0;
@@ -34,7 +72,7 @@ template <typename T, int D, int W> __global__ __launch_bounds__(256) void atten
         const float base = top == -INFINITY ? 0.0f : top;
         float total = 0.0f, o[E] = {};
 #pragma unroll 8
-        for (int s = first; s < parts; s += W) {
+        for (int s = wave; s < parts; s += 4) {
             const int64_t at = part(s);
             const float m = a.stat[at * 2], w = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - base);
             total += a.stat[at * 2 + 1] * w;
@@ -42,25 +80,18 @@ template <typename T, int D, int W> __global__ __launch_bounds__(256) void atten
             for (int e = 0; e < E; ++e)
                 if (lane + 64 * e < D) o[e] += a.part[at * D + lane + 64 * e] * w;
         }
-        T* const y = static_cast<T*>(a.y) + (int64_t)r * a.ldy + (int64_t)q_head * D;
-        if constexpr (W == 1) {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (lane + 64 * e < D) y[lane + 64 * e] = (T)(total == 0.0f ? 0.0f : o[e] / total);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
-            if (lane == 0) totals[wave] = total;
-            __syncthreads();
-            total = totals[0] + totals[1] + totals[2] + totals[3];
-            if ((int)threadIdx.x < D) {
-                const int d = threadIdx.x;
-                const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
-                y[d] = (T)(total == 0.0f ? 0.0f : v / total);
-            }
-            __syncthreads();
+        for (int e = 0; e < E; ++e)
+            if (lane + 64 * e < D) sums[wave][lane + 64 * e] = o[e];
+        if (lane == 0) totals[wave] = total;
+        __syncthreads();
+        total = totals[0] + totals[1] + totals[2] + totals[3];
+        if ((int)threadIdx.x < D) {
+            const int d = threadIdx.x;
+            const float v = sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d];
+            static_cast<T*>(a.y)[(int64_t)r * a.ldy + (int64_t)q_head * D + d] = (T)(total == 0.0f ? 0.0f : v / total);
         }
+        __syncthreads();
     }
 }
 
@@ -90,10 +121,10 @@ AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int
 
 template <typename T, int D> static dcnn_status launch_join_dim(dcnn_ctx* ctx, const AttendArgs& a) {
     const int64_t outs = (int64_t)a.tokens.rows * a.cache.heads * a.group, most = (int64_t)ctx->num_cu * 16;
-    if (a.plan == nullptr && a.splits <= 8) {                  // (of rows alone, one may have most of the parts)
+    if (a.plan == nullptr && a.splits <= kFewParts) {
         const int64_t groups = cdiv(outs, 4);
-        hipLaunchKernelGGL((attend_join_kernel<T, D, 1>), dim3((unsigned)(groups < most ? groups : most)), dim3(256), 0, ctx->stream, a);
-    } else hipLaunchKernelGGL((attend_join_kernel<T, D, 4>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL((attend_join_few_kernel<T, D>), dim3((unsigned)(groups < most ? groups : most)), dim3(256), 0, ctx->stream, a);
+    } else hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(outs < most ? outs : most)), dim3(256), 0, ctx->stream, a);
     return check_hip(ctx, hipGetLastError(), "attend_join_kernel launch");
 }
 template <typename T> static dcnn_status launch_join(dcnn_ctx* ctx, int dim, const AttendArgs& a) {
