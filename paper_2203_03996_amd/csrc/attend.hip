@@ -106,6 +106,12 @@ AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int
         // 64 rows of 2048: 81, 32 with 512 tokens at least, 23)
         const int64_t units = cdiv(rows * group, 128) * heads, wanted = cdiv(512, units < 1 ? 1 : units), most = cdiv(length, 256);
         p.splits = (int)(wanted < most ? wanted : most);
+        // A few more tiles than are resident at a time leave most of the card to the last ones: halves or thirds fill it better, up to where the join
+        // costs as much (2080 rows of 32 heads on 8 of 128, 8192 tokens: 398, 365 and 349 us whole, in halves, in thirds; 3000 rows 394, 389, 405; 4000
+        // rows 436, 476, 500; of heads of 64 the sums of parts are small: 20000 rows of 8, 4096 tokens, 254, 233, 231; 26240 rows 261, 255, 253)
+        const int waves = tile_waves(dim / 32, dtype_size == 4 ? 3 : 1);
+        const int64_t slots = 256 * waves;
+        if (units > slots && length >= 2048) p.splits = units * 10 <= slots * 13 ? 3 : units * 2 <= slots * (waves > 2 ? 5 : 3) ? 2 : p.splits;
         p.parts = p.splits > 1 ? rows * q_heads * p.splits : 0;
     } else {
         // As many workgroups as are resident at a time, each an equal part of the tokens of all rows: their lengths may be any.  Where every row is a

@@ -83,6 +83,13 @@ __device__ __forceinline__ float max_of_halves(float v) {
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
+// Waves to a SIMD of the kernel for tiles of rows: as many as leave a lane's queries, sums, products and weights (heads of 32 NB values, numbers of
+// `terms` operands) room for addresses and codes.  Heads of 64 with three in place of two: 655 us and 548 (26240 rows of 8 heads, 4096 tokens each).
+constexpr int tile_waves(int nb, int terms) {
+    const int registers = nb * 8 * terms + nb * 16 + 32 + 16 * terms;
+    return registers <= 112 ? 3 : registers <= 176 ? 2 : 1;
+}
+
 // Tiles that each of the `shares` workgroups of a head takes: a tile for each wave at least.
 __device__ __forceinline__ int share_of(int tiles, int shares) {
     const int n = (tiles + shares - 1) / shares;

@@ -43,9 +43,7 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 
 template <typename T, int NB> struct TileShape {
-    // queries, sums, products and weights of a lane: two waves to a SIMD where they leave room for addresses and codes
-    static constexpr int registers = NB * 8 * Operand<T>::TERMS + NB * 16 + 32 + 16 * Operand<T>::TERMS;
-    static constexpr int waves = registers <= 112 ? 3 : registers <= 176 ? 2 : 1;
+    static constexpr int waves = tile_waves(NB, Operand<T>::TERMS);
     static constexpr int bytes = 2 * 2 * kTokens * NB * 64;            // two buffers of keys and values
 };
 

@@ -550,6 +550,32 @@ def test_attend_long_rows_of_every_width(ctx, dt, dim, page):
         assert torch.equal(torch.isnan(got[:, 1, :, :32]).all(2).all(1), (stream == 2) & (pos >= 1001)) and not torch.isnan(got[:, 0]).any()
 
 
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [900, 1600, 2000])
+def test_attend_more_tiles_than_are_resident(ctx, dt, rows):
+    """Many tiles of rows, whose tokens are taken whole, in halves or in thirds (as attend64, with all rows of a head at once)."""
+    heads, dim, n = 64, 32, 2100
+    cache = filled(ctx, 1, n, heads, dim, dt, page=64, seed=33)
+    gen = seeded(rows)
+    q = rand(gen, rows, heads * dim, dt=dt, scale=1.5)
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    pos = torch.randint(0, n, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    got = cache.attend(q, causal=True, streams=zero, positions=pos)
+    ctx.sync()
+    q64, seen = q.double().view(rows, heads, dim), torch.arange(n, device="cuda") <= pos[:, None]
+    want, slack = torch.zeros_like(q64), torch.zeros_like(q64)
+    tiny = 2.0 ** -25 if dt == "f16" else 0.0
+    for h in range(heads):
+        k, v = (plain.stream_values(cache.codes, cache.scales, cache.pages, 0, h, w, n, 64)[0] for w in (0, 1))
+        x = dim ** -0.5 * (q64[:, h] @ k.T)
+        e = (dim ** -0.5 * (TERMS[dt] * dim + 8) * U32 * (q64[:, h].abs() @ k.abs().T) + 8 * U32 * x.abs()) * seen
+        w = torch.softmax(x.masked_fill(~seen, -torch.inf), 1)
+        want[:, h] = w @ v
+        off = 4.0 * e.amax(1, keepdim=True) + TYPES[dt][1] + (3 * n + 64) * U32
+        slack[:, h] = off * (w @ v.abs()) + tiny * w.amax(1, keepdim=True) * (seen.double() @ v.abs())
+    close(got, want, dt, slack, f"{rows} rows")
+
+
 @pytest.mark.parametrize("rows", [2, 3, 64, 200, 511, 512, 513, 700])
 @pytest.mark.parametrize("lengths", ["none", "one long", "first", "last", "gaps", "all alike", "one tile", "mixed"])
 def test_attend_tokens_shared_among_workgroups(ctx, rows, lengths):
