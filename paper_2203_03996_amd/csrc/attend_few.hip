@@ -1,4 +1,4 @@
-// Attention over the cache for rows that share no stream: one token of each.
+// Attention over the cache for rows by themselves: one of each stream, or some (attend_plan).
 //
 //   S = K q,  p = exp2(S * scale log2(e) - max),  y = V^T p / sum p, the maximum and the sums kept up to date from tile to tile
 //
@@ -11,7 +11,9 @@
 //   * values lie in LDS as they came (rows of D / 2 bytes, columns of 16 bytes permuted against bank conflicts) and are read transposed: 16
 //     tokens of a channel to a lane, the ones whose weights the lane has.  Their 16 scales come straight from the cache.
 //   * codes become operands by conversions that take the scale: one instruction for two values.
-// The next tile's codes and scales are in flight meanwhile.
+// The next tile's codes and scales are in flight meanwhile.  Where rows are long, the tokens of all of them are dealt out evenly to as many workgroups
+// as are resident (two to a compute unit), whatever the rows' lengths, and attend_join_kernel makes their parts one.
+// Measured (32 heads on 8 of 128, bf16 and fp16): 64 rows of up to 8192 tokens, 309 MB, 67 us, 4.6 TB/s; one row of 262143, 285 MB, 57 us, 5.0 TB/s.
 #include "attend_device.h"
 
 namespace dcnn {
