@@ -59,7 +59,10 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
     constexpr int D = NB * 32, ROW = D * 2, TERMS = O::TERMS, CHUNKS = (NB + 1) / 2, PLANE = kTokens * ROW;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int streams[kVectors], lows[kVectors], highs[kVectors];
-    __shared__ uint64_t broken[2][NB];                                 // blocks of values that are NaN, in the order in which they are written
+    // blocks of values that are NaN, in the order in which they are written, and whether there were any.  (Looked at word by word, and written, only
+    // where there are.)
+    __shared__ uint64_t broken[2][NB];
+    __shared__ int any_broken;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = lane / 32, col = lane % 32;
     const int count = row_count(a.tokens.count, a.tokens.rows);
     const int vectors = count * a.group, tiles = (vectors + kVectors - 1) / kVectors, heads = a.cache.heads;
@@ -97,6 +100,9 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
         float top = -INFINITY, sum = 0.0f;
         bool mine = false;
+        if (tid < 2 * NB) broken[tid / NB][tid % NB] = 0;
+        if (tid == 2 * NB) any_broken = 0;
+        uint32_t dirty = 0;                                            // words of this wave that are not zero
         __syncthreads();
         const uint64_t starts0 = __ballot(lane == 0 || streams[lane] != streams[lane == 0 ? 0 : lane - 1]), starts1 = __ballot(streams[lane + 64] != streams[lane + 63]);
         int index = 0;
@@ -129,18 +135,17 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
 
             // ---- codes of a tile: from memory, to operands in LDS
             u32x4 raw[CHUNKS];
-            uint32_t byte[CHUNKS];
+            uint8_t byte[CHUNKS];                                      // (as words, they would be waited for where they were asked for: to cut them to bytes)
             bool drop[CHUNKS];
             // (keys 0, values 1, nothing 2: one for all of a wave's lanes)
             const auto which_of = [&](int n) { return NB % 4 == 0 ? 4 * n / NB : (wave + 4 * n) / NB; };
-            // the entry of a tile's page in the table, and what it says: looked at one tile after it was asked for
-            const auto entry_at = [&](int t) {
-                if constexpr (WHOLE) return entry_of_all(a.cache, of, (start + t * kTokens) >> a.cache.page_shift);
-                else return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift);
-            };
-            const auto page_at = [&](int t, int entry) {
-                if constexpr (WHOLE) return page_of_entry(a.cache, of, (start + t * kTokens) >> a.cache.page_shift, entry);
-                else return entry;
+            // The page of a tile: of sixty-four tiles at once, a lane each.  (One by one through the scalar cache, every wait for LDS is one for that load too.)
+            int pages = -1;
+            const auto page_at = [&](int t) {
+                if constexpr (WHOLE) {
+                    if ((t - from) % 64 == 0) pages = page_of(a.cache, of, (start + (t + lane) * kTokens) >> a.cache.page_shift);
+                    return __builtin_amdgcn_readlane(pages, (t - from) % 64);
+                } else return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift);
             };
             const auto load = [&](int t, int page) {
                 const uint64_t tile_slot = (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (2 * page_tokens) + ((start + t * kTokens) & page_mask);
@@ -176,7 +181,12 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                     // and so is a value that is NaN for rows that do not see it: they become zeros, and the second kind is noted
                     if (which == 1) {
                         const uint64_t noted = __ballot(byte[n] == 255 && !drop[n]);
-                        if (lane == 0) broken[buffer][within / 64] = noted;
+                        const uint32_t bit = 1u << (buffer * CHUNKS + n);
+                        if (noted != 0 || (dirty & bit) != 0) {
+                            if (lane == 0) broken[buffer][within / 64] = noted;
+                            if (noted != 0) any_broken = 1;
+                            dirty = noted != 0 ? dirty | bit : dirty & ~bit;
+                        }
                         scale = drop[n] || byte[n] == 255 ? 0.0f : scale;
                     }
                     uint8_t* const row = lds + (buffer * 2 + which) * PLANE + token_in * ROW;
@@ -186,17 +196,16 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             };
             // which sixteens of a tile's tokens have a page
             const auto sixteens = [&](int p) { return WHOLE ? (p >= 0 ? 15u : 0u) : (uint32_t)__ballot(p >= 0) & 15u; };
-            int page = page_at(from, entry_at(from));
+            int page = page_at(from);
             uint32_t paged = sixteens(page), paged_next = 0;
             load(from, page);
-            int entry = entry_at(from + 1);
+            page = page_at(from + 1);
             __syncthreads();                                           // (a segment before this one is done with the buffers)
             stage(from & 1);
             if (from + 1 < to) {
-                page = page_at(from + 1, entry);
                 paged_next = sixteens(page);
                 load(from + 1, page);
-                entry = entry_at(from + 2);
+                page = page_at(from + 2);
             }
             for (int t = from; t < to; ++t) {
                 __syncthreads();                                       // this tile is there, and all are done with the one before it
@@ -204,10 +213,9 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                 const uint32_t has_page = paged;
                 paged = paged_next;
                 if (t + 2 < to) {                                      // (nothing of these loads is looked at before the next tile's turn)
-                    page = page_at(t + 2, entry);
                     paged_next = sixteens(page);
                     load(t + 2, page);
-                    entry = entry_at(t + 3);
+                    page = page_at(t + 3);
                 }
                 const int t0 = start + t * kTokens;
                 if (t0 + kTokens <= any_from || t0 >= any_to) continue;
@@ -307,10 +315,7 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                uint64_t noted = 0;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) noted |= broken[t & 1][b];
-                if (noted != 0) {
+                if (__builtin_amdgcn_readfirstlane(any_broken) != 0) {
                     for (int w = 0; w < NB; ++w)
                         for (uint64_t bits = broken[t & 1][w]; bits != 0; bits &= bits - 1) {
                             const int bit = w * 64 + __builtin_ctzll(bits), in_tile = staged_token<NB>(bit / NB);
