@@ -139,13 +139,15 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
             bool drop[CHUNKS];
             // (keys 0, values 1, nothing 2: one for all of a wave's lanes)
             const auto which_of = [&](int n) { return NB % 4 == 0 ? 4 * n / NB : (wave + 4 * n) / NB; };
-            // The page of a tile: of sixty-four tiles at once, a lane each.  (One by one through the scalar cache, every wait for LDS is one for that load too.)
+            // The page of a tile, or of its sixteen tokens `lane % 4`: 64 pages are asked for at once, a lane each.  (One by one, through either cache, every
+            // tile waits for them, and for what was asked for before.)
+            constexpr int PER = WHOLE ? 1 : 4, SPAN = kTokens / PER;
             int pages = -1;
             const auto page_at = [&](int t) {
-                if constexpr (WHOLE) {
-                    if ((t - from) % 64 == 0) pages = page_of(a.cache, of, (start + (t + lane) * kTokens) >> a.cache.page_shift);
-                    return __builtin_amdgcn_readlane(pages, (t - from) % 64);
-                } else return page_of(a.cache, of, (start + t * kTokens + 16 * (lane & 3)) >> a.cache.page_shift);
+                const int at = (t - from) * PER % 64;
+                if (at == 0) pages = page_of(a.cache, of, (start + t * kTokens + lane * SPAN) >> a.cache.page_shift);
+                if constexpr (WHOLE) return __builtin_amdgcn_readlane(pages, at);
+                else return __shfl(pages, at + lane % 4, kWave);
             };
             const auto load = [&](int t, int page) {
                 const uint64_t tile_slot = (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (2 * page_tokens) + ((start + t * kTokens) & page_mask);
