@@ -99,16 +99,16 @@ AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int
     const int64_t group = q_heads / heads;
     AttendPlan p;
     // A tile of 128 query vectors reads its tokens once, a row alone reads them for itself: some rows of a stream find them in the caches.
-    // (16 streams of 4096 tokens, 32 heads on 8 of 128: four rows each take 46 us alone and 58 in tiles, six 69 and 82, eight 85 and 57.)
+    // (16 streams of 4096 tokens, 32 heads on 8 of 128: four rows each take 48 us alone and 57 in tiles, six 72 and 79, eight 87 and 56.)
     p.tiles = rows > 6 * streams;
     if (p.tiles) {
-        // two workgroups to a compute unit, with 256 tokens each at least (512 rows of a stream of 8192 tokens, the same heads: 284 us unsplit, 96 us;
-        // 64 rows of 2048: 81, 32 with 512 tokens at least, 23)
+        // two workgroups to a compute unit, with 256 tokens each at least (512 rows of a stream of 8192 tokens, the same heads: 278 us unsplit, 96 us;
+        // 64 rows of 2048: 78, 31 with 512 tokens at least, 24)
         const int64_t units = cdiv(rows * group, 128) * heads, wanted = cdiv(512, units < 1 ? 1 : units), most = cdiv(length, 256);
         p.splits = (int)(wanted < most ? wanted : most);
         // A few more tiles than are resident at a time leave most of the card to the last ones: halves or thirds fill it better, up to where the join
-        // costs as much (2080 rows of 32 heads on 8 of 128, 8192 tokens: 398, 365 and 349 us whole, in halves, in thirds; 3000 rows 394, 389, 405; 4000
-        // rows 436, 476, 500; of heads of 64 the sums of parts are small: 20000 rows of 8, 4096 tokens, 254, 233, 231; 26240 rows 261, 255, 253)
+        // costs as much (2080 rows of 32 heads on 8 of 128, 8192 tokens: 376, 349 and 342 us whole, in halves, in thirds; 3000 rows 380, 388, 400, but
+        // of 2048 tokens 165, 150, 155; 4000 rows 439, 475, 493; of heads of 64 the sums of parts are small: 20000 rows of 8, 4096 tokens, 242, 224, 226)
         const int waves = tile_waves(dim / 32, dtype_size == 4 ? 3 : 1);
         const int64_t slots = 256 * waves;
         if (units > slots && length >= 2048) p.splits = units * 10 <= slots * 13 ? 3 : units * 2 <= slots * (waves > 2 ? 5 : 3) ? 2 : p.splits;

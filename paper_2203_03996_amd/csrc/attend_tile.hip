@@ -10,10 +10,11 @@
 //   * V^T: values lie in LDS as rows of tokens and are read transposed, four tokens of a channel at a time, in that same order.
 // Rows of several streams in a tile of rows are taken one stream after the other ("segments": columns outside of it see nothing).
 // Instruction issue bounds it: eight vector instructions for each product of a query and a key that a lane has, an exponential among them, stand
-// between the matrix products, and the two or three workgroups of a compute unit overlap them in part.  Measured: 14348 rows of 32 heads on 8 of 128 (bf16, causal, three
-// prompts of up to 6000 tokens) 665 us, 0.88 PFLOP/s, matrix cores 35 % busy; 26240 flagged pixels of 8 heads of 64 (fp16, 4096 tokens each) 491 us
-// with the join of halves (34).  A wave with 32 columns and a workgroup with 128 leave room for two waves to a SIMD at heads of 128; 256 vectors to a
-// workgroup, with the products of one tile between the exponentials of the one before, took 770 us and more.
+// between the matrix products, and the two or three workgroups of a compute unit overlap them in part.  Measured: 14348 rows of 32 heads on 8 of
+// 128 (bf16, causal, three prompts of up to 6000 tokens) 654 us, 0.90 PFLOP/s, matrix cores 37 % busy; 26240 flagged pixels of 8 heads of 64 (fp16,
+// 4096 tokens each) 453 us with the join of halves (34).  A wave with 32 columns and a workgroup with 128 leave room for two waves to a SIMD at
+// heads of 128.  With 256 vectors to a workgroup the prompts took 770 us and more with the products of one tile between the exponentials of the one
+// before, 818 with two groups of four waves, one at the matrix cores while the other weighs and stages.
 #include "attend_device.h"
 
 namespace dcnn {
@@ -153,7 +154,8 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                 const uint64_t tile_slot = (uint64_t)(uint32_t)(page < 0 ? 0 : page) * (2 * page_tokens) + ((start + t * kTokens) & page_mask);
 #pragma unroll
                 for (int n = 0; n < CHUNKS; ++n) {
-                    const int within = (tid + 256 * n) % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB, which = which_of(n), t_at = start + t * kTokens + token_in;
+                    const int within = (tid + 256 * n) % (kTokens * NB), token_in = staged_token<NB>(within / NB), b = within % NB;
+                    const int which = which_of(n), t_at = start + t * kTokens + token_in;
                     if (NB % 2 != 0 && which > 1) break;
                     bool counts = (uint32_t)(t_at - first) < (uint32_t)(last - first);
                     if constexpr (WHOLE) {

@@ -23,20 +23,16 @@ __device__ __forceinline__ int page_of(const CacheArgs& c, int stream, int block
     const int page = c.pages != nullptr ? c.pages[at] : (int)at;
     return (uint32_t)page < (uint32_t)c.num_pages ? page : -1;
 }
-// The same where stream and block are one for all lanes, in two steps: the table's entry through the scalar cache, so that it waits for no other
-// load, and what it says, where it is needed.  (No branches: what is loaded in one is waited for at its end.  Without a table, or past its end, a word
-// of the table or of the codes is read and not looked at.)
-__device__ __forceinline__ int entry_of_all(const CacheArgs& c, int stream, int block) {
+// The same where stream and block are one for all lanes: through the scalar cache, so that it waits for no other load.  (No branches: what is loaded is
+// waited for where it is used.  Without a table, or past its end, a word of the codes or of the table is read, and not looked at.)
+__device__ __forceinline__ int page_of_all(const CacheArgs& c, int stream, int block) {
     typedef __attribute__((address_space(4))) const int32_t ConstInt;
-    const uint32_t in = (uint32_t)block < (uint32_t)c.per_stream ? block : 0;
-    const uintptr_t at = c.pages != nullptr ? (uintptr_t)(c.pages + (int64_t)stream * c.per_stream + in) : (uintptr_t)c.codes;
-    return *((ConstInt*)at);
+    const bool in = (uint32_t)block < (uint32_t)c.per_stream;
+    const int64_t at = (int64_t)stream * c.per_stream + (in ? block : 0);
+    const int entry = *((ConstInt*)(c.pages != nullptr ? (uintptr_t)(c.pages + at) : (uintptr_t)c.codes));
+    const int page = c.pages != nullptr ? entry : (int)at;
+    return in && (uint32_t)page < (uint32_t)c.num_pages ? page : -1;
 }
-__device__ __forceinline__ int page_of_entry(const CacheArgs& c, int stream, int block, int entry) {
-    const int page = c.pages != nullptr ? entry : (int)((uint32_t)stream * (uint32_t)c.per_stream + (uint32_t)block);
-    return (uint32_t)block < (uint32_t)c.per_stream && (uint32_t)page < (uint32_t)c.num_pages ? page : -1;
-}
-__device__ __forceinline__ int page_of_all(const CacheArgs& c, int stream, int block) { return page_of_entry(c, stream, block, entry_of_all(c, stream, block)); }
 // Tokens before the first one of a page's head; `which`: 0 keys, 1 values.
 __device__ __forceinline__ int64_t head_of_page(const CacheArgs& c, int page, int which, int head) {
     return (((int64_t)page * 2 + which) * c.heads + head) << c.page_shift;
