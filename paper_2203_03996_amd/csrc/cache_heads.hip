@@ -114,7 +114,7 @@ __device__ __forceinline__ void turn_of(Turn<A>& f, const RotationArgs& rot, int
         const T* p = static_cast<const T*>(params);
 #pragma unroll
         for (int e = 0; e < 8; ++e) own[e] = none, other[e] = none;
-        if (p == nullptr || !at.in) return;
+        if (p == nullptr || !at.in || !at.here) return;        // (a row without a token: zeros times one, and no bias)
         load8<T>(p + at.at, own);
 #pragma unroll
         for (int e = 0; e < 8; ++e) other[e] = own[e ^ 1];

@@ -1,0 +1,39 @@
+"""Heads, the cache in 4 bits and attention at the edges of what their calls allow, against the plain forms in 64 bits (tolerances as in test_gpu_cache.py)."""
+import pytest
+import torch
+
+import paper_2203_03996_amd as pkg
+from tests import cache_plain as plain
+from tests.test_gpu_cache import TYPES, U32, check_append, close, ctx, ints, new_cache, norm_of, rand, seeded  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- rows without a token -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+def test_heads_of_rows_without_a_token_are_zeros_behind_any_norm(ctx, dt, kind, style):  # noqa: F811
+    """Entries outside of the map and positions outside of the rotation's table; norms with weight and bias, an infinity and a NaN among the weights."""
+    gen = seeded(31)
+    dim, rows = 64, 9
+    q, k = rand(gen, rows, 5 * dim, dt=dt), rand(gen, rows, 2 * dim, dt=dt)
+    w, b = rand(gen, dim, dt=dt, scale=0.3, mean=1.0), rand(gen, dim, dt=dt, scale=0.3, mean=1.0)
+    rotation = pkg.Rotation.of_positions(50, 32, style=style)
+    idx = ints(3, -1, 0, 40, 7, 1 << 30, 8, 2, 5)                      # (of a map of 9 rows)
+    pos = ints(4, 50, 6, -1, 8, 9, 2 ** 31 - 1, 11, 49)
+    has = torch.tensor([i in range(9) and 0 <= int(pos[i]) < 50 for i in idx.tolist()], device="cuda")
+    assert 2 < has.sum() < 7
+    for broken in (False, True):
+        if broken:
+            w[3], w[40], w[41] = float("inf"), float("nan"), -float("inf")
+        norm = pkg.RowNorm(kind, w, b, 1e-5)
+        got = ctx.rows_heads(q, k, dim=dim, q_norm=norm, k_norm=norm, rotation=rotation, positions=pos, idx=idx)
+        alone = ctx.rows_heads(q, dim=dim, q_norm=norm, idx=idx, count=ints(rows))         # (a list without a rotation: entries below zero alone)
+        ctx.sync()
+        for y, x in ((got[0], q), (got[1], k)):
+            assert (y[~has] == 0).all(), f"{dt} {kind} {style}: rows without a token are {y[~has].abs().amax(1).tolist()}"
+            if not broken:
+                want, mag = plain.heads64(x[has], dim, kind, w, b, 1e-5, rotation.table, style, pos[idx.long()[has]])
+                close(y[has], want, dt, 32 * U32 * mag, f"{dt} {kind} {style}")
+        assert (alone[1] == 0).all() and (alone[3] != 0).any()
