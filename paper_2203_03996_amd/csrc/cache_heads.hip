@@ -116,6 +116,7 @@ __device__ __forceinline__ void turn_of(Turn<A>& f, const RotationArgs& rot, int
         for (int e = 0; e < 8; ++e) own[e] = none, other[e] = none;
         if (p == nullptr || !at.in || !at.here) return;        // (a row without a token: zeros times one, and no bias)
         load8<T>(p + at.at, own);
+        if (!at.turned) return;                                // (an infinity times the sine of no turn, zero, is none)
 #pragma unroll
         for (int e = 0; e < 8; ++e) other[e] = own[e ^ 1];
         if (at.halves) load8<T>(p + at.partner, other);

@@ -37,3 +37,26 @@ def test_heads_of_rows_without_a_token_are_zeros_behind_any_norm(ctx, dt, kind, 
                 want, mag = plain.heads64(x[has], dim, kind, w, b, 1e-5, rotation.table, style, pos[idx.long()[has]])
                 close(y[has], want, dt, 32 * U32 * mag, f"{dt} {kind} {style}")
         assert (alone[1] == 0).all() and (alone[3] != 0).any()
+
+
+# ---- norms' weights that are no numbers -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+@pytest.mark.parametrize("rot", [0, 32])
+def test_an_infinite_weight_stays_in_its_channel_where_nothing_turns(ctx, dt, style, rot):  # noqa: F811
+    gen = seeded(33)
+    dim, rows = 64, 5
+    q = rand(gen, rows, 2 * dim, dt=dt) + 3.0
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    rotation = pkg.Rotation.of_positions(rows, rot, style=style) if rot else None
+    for kind in ("rms", "layer"):
+        w, b = rand(gen, dim, dt=dt, scale=0.3, mean=1.0), rand(gen, dim, dt=dt, scale=0.3)
+        w[40], w[55], b[50] = float("inf"), float("nan"), -float("inf")
+        got = ctx.rows_heads(q, dim=dim, q_norm=pkg.RowNorm(kind, w, b, 1e-5), rotation=rotation, positions=pos)
+        ctx.sync()
+        want, mag = plain.heads64(q, dim, kind, w, b, 1e-5, rotation and rotation.table, style, pos)
+        got = got.double().view(want.shape)
+        assert torch.isinf(want[..., 40]).all() and torch.equal(torch.isinf(got), torch.isinf(want)) and torch.equal(got.sign().nan_to_num(7.0), want.sign().nan_to_num(7.0))
+        sane = torch.ones(dim, dtype=torch.bool, device="cuda")
+        sane[[40, 50, 55]] = False
+        close(got[..., sane].contiguous(), want[..., sane], dt, 32 * U32 * mag[..., sane], f"{dt} {kind} {style}")
