@@ -60,3 +60,34 @@ def test_an_infinite_weight_stays_in_its_channel_where_nothing_turns(ctx, dt, st
         sane = torch.ones(dim, dtype=torch.bool, device="cuda")
         sane[[40, 50, 55]] = False
         close(got[..., sane].contiguous(), want[..., sane], dt, 32 * U32 * mag[..., sane], f"{dt} {kind} {style}")
+
+
+# ---- keys of any size -----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_codes_of_keys_below_the_normal_range(ctx, dt):  # noqa: F811
+    """Every border of two codes at the smallest scale and the one above it, the numbers next to them, and, by a rotation, numbers that only 64 bits tell from a border."""
+    t, _, step = TYPES[dt]
+    border = torch.tensor([0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0, 0.125, 0.375], dtype=torch.float64)
+    rows = []
+    for e in (-126, -125, -124):
+        for nudge in (-1, 0, 1):
+            for top in (0.0, 1.0, 6.0):
+                block = torch.cat([border, -border]) * 2.0 ** e + nudge * step
+                block = block * (block.abs() <= max(top, 1.0) * 2.0 ** e)                  # (blocks whose largest magnitude asks for less, and for this scale)
+                rows.append(block)
+    x = torch.stack(rows).to(t).cuda()
+    n = len(x)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    cache = new_cache(ctx, 1, n, 1, 32, dt)
+    check_append(ctx, cache, x, x.flip(0).contiguous(), torch.zeros_like(pos), pos, dt, "none", streams=torch.zeros_like(pos), positions=pos)
+    # a - b sin, b + a sin: b a few steps, the sine so small that b sin and a sin are far below a step
+    table = torch.ones(n, 16, 2, device="cuda")
+    table[..., 1] = torch.where(torch.arange(n, device="cuda") % 2 == 0, 2.0 ** -20, -2.0 ** -20)[:, None]
+    y = x.clone()
+    y[:, 16:] = (torch.arange(16, device="cuda") - 8).to(t) * step
+    rotation = pkg.Rotation(table)
+    cache.append(y, x, rotation=rotation, streams=torch.zeros_like(pos), positions=pos)
+    ctx.sync()
+    c, s = plain.quantised(plain.heads64(y, 32, table=table, pos=pos)[0])
+    at = (cache.pages[0, pos.long() // 16].long(), 0, slice(None), pos.long() % 16)
+    assert torch.equal(cache.scales[at], s) and torch.equal(cache.codes[at], plain.pack(c))
