@@ -187,19 +187,20 @@ template <typename T, int D, int L> __device__ __forceinline__ double centre64(c
 }
 
 // An fp64 value as the fp32 one next to zero of it, with the last bit set where something was cut off ("to odd"): rounding that to a code, and
-// comparing it with a border, is rounding and comparing the fp64 value.  Magnitudes from 2^128 on become infinity; those below 2^-126 zero, or with
-// SMALL steps of 2^-149, as fp32 has them.
-template <bool SMALL> __device__ __forceinline__ float to_odd(double v) {
+// comparing it with a border, is rounding and comparing the fp64 value.  Magnitudes from 2^128 on become infinity, those below 2^-126 zero.  At the EDGE
+// they are told apart: the former are the largest number if they are finite, and the latter have steps of 2^-149, as fp32 has them.
+template <bool EDGE> __device__ __forceinline__ float to_odd(double v) {
     const uint64_t bits = __builtin_bit_cast(uint64_t, v);
     const uint32_t hi = (uint32_t)(bits >> 32), lo = (uint32_t)bits, rest = lo & 0x1fffffffu;
     const uint32_t f = ((hi << 3 | lo >> 29) - (896u << 23)) & 0x7fffffffu;    // exponent with the bias of fp32
     const uint32_t odd = f | (rest < 1u ? rest : 1u) | (hi & 0x80000000u);
     const uint32_t size = hi & 0x7fffffffu;
-    if (SMALL && size < 0x38100000u) {
+    if (EDGE && size < 0x38100000u) {
         const double steps = __builtin_fabs(v) * 0x1p149;
         const uint32_t n = (uint32_t)steps;
         return __builtin_bit_cast(float, n | ((double)n != steps ? 1u : 0u) | (hi & 0x80000000u));
     }
+    if (EDGE && size >= 0x47f00000u && size < 0x7ff00000u) return __builtin_bit_cast(float, 0x7f7fffffu | (hi & 0x80000000u));
     return size < 0x38100000u ? 0.0f : __builtin_bit_cast(float, size < 0x47f00000u ? odd : 0x7f800000u);
 }
 // (a zero is code 0, whatever its sign was)
@@ -337,9 +338,10 @@ __global__ __launch_bounds__(256, OP == kAppendHeads && !BIAS ? 4 : 1) void head
                 for (int e = 0; e < 8; ++e) o[e] = to_odd<false>(key(e));
                 uint32_t byte;
                 uint32_t words = encode<kMaxScale<T>>(o, &byte);
-                // Scales up to 2^-125: magnitudes below 2^-126 have codes too.  (Blocks of zeros alone are among them.  Looked at for each value where it
-                // was made, it took 35 us in place of 30, 16275 rows of 8 x 128; the values are fetched again, or they take registers.)
-                if (__any(here && in && byte <= 2)) {
+                // Scales up to 2^-125: magnitudes below 2^-126 have codes too.  An infinity: it may be a number that fp32 lacks, held as the largest.  (Blocks
+                // of zeros alone are among the first.  Looked at for each value where it was made, it took 35 us in place of 30, 16275 rows of 8 x 128; the
+                // values are fetched again, or they take registers.)
+                if (__any(here && in && (byte <= 2 || byte == 255))) {
                     fetch(h);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = to_odd<true>(key(e));

@@ -91,3 +91,25 @@ def test_codes_of_keys_below_the_normal_range(ctx, dt):  # noqa: F811
     c, s = plain.quantised(plain.heads64(y, 32, table=table, pos=pos)[0])
     at = (cache.pages[0, pos.long() // 16].long(), 0, slice(None), pos.long() % 16)
     assert torch.equal(cache.scales[at], s) and torch.equal(cache.codes[at], plain.pack(c))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_keys_that_are_finite_beyond_fp32_are_held_as_the_largest(ctx, dt):  # noqa: F811
+    info = torch.finfo(TYPES[dt][0])
+    gen = seeded(32)
+    x = rand(gen, 6, 64, dt=dt)
+    x = (x.double() * (info.max / x.double().abs().amax(1, keepdim=True))).clamp(-info.max, info.max).to(TYPES[dt][0])
+    x[3], x[4, 40] = info.max, float("inf")
+    pos = torch.arange(6, dtype=torch.int32, device="cuda")
+    cache = new_cache(ctx, 1, 6, 1, 64, dt)
+    zero = torch.zeros_like(pos)
+    table = torch.full((6, 16, 2), 0.5 ** 0.5, device="cuda")
+    w = torch.full((64,), info.max, dtype=TYPES[dt][0], device="cuda")
+    for norm, p, turn in ((None, {}, table), (pkg.RowNorm("rms", w, None, 0.0), dict(kind="rms", w=w), None), (pkg.RowNorm("layer", w, w, 0.0), dict(kind="layer", w=w, b=w), table)):
+        cache.append(x, x, norm=norm, rotation=None if turn is None else pkg.Rotation(turn), streams=zero, positions=pos)
+        ctx.sync()
+        want = plain.heads64(x, 64, table=turn, pos=pos, **p)[0]
+        c, s = plain.quantised(want)
+        at = (cache.pages[0, pos.long() // 16].long(), 0, slice(None), pos.long())
+        assert torch.equal(cache.scales[at], s), f"{cache.scales[at].tolist()} and {s.tolist()}"
+        assert torch.equal(cache.codes[at], plain.pack(c))
