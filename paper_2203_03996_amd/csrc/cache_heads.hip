@@ -239,13 +239,13 @@ __global__ __launch_bounds__(256, OP == kAppendHeads && !BIAS ? 4 : 1) void head
     const int lane = threadIdx.x % L, sub = threadIdx.x / L;
     const bool in = lane * 8 < D;
     const int at = in ? lane * 8 : 0;
-    const int count = row_count(a.tokens.count, a.tokens.rows);
+    const uint32_t count = (uint32_t)row_count(a.tokens.count, a.tokens.rows);         // (up to 2^31 - 1: with a tile's rows on top it needs the last bit)
     const RotationArgs& rot = a.rotation;
     // 2^shift heads of a row side by side: two, so that what belongs to the row serves many, and as many as there are where workgroups are left
     int shift = a.shift;
-    while (shift > 1 && (int64_t)((count + (R >> shift) - 1) / (R >> shift)) * a.jobs > (int)gridDim.x) --shift;
+    while (shift > 1 && (int64_t)((count + (R >> shift) - 1) / (uint32_t)(R >> shift)) * a.jobs > (int)gridDim.x) --shift;
     const int rows = R >> shift, stride = 1 << shift, h0 = sub & (stride - 1);
-    const int tiles = (count + rows - 1) / rows;
+    const int tiles = (int)((count + rows - 1) / (uint32_t)rows);
     // one job before the other: what one costs is not what the other does, and workgroups that follow each other go to different L2 caches
     for (int64_t item = blockIdx.x; item < (int64_t)tiles * a.jobs; item += gridDim.x) {
         const int which = item >= tiles, tile = (int)(which ? item - tiles : item);

@@ -113,3 +113,30 @@ def test_keys_that_are_finite_beyond_fp32_are_held_as_the_largest(ctx, dt):  # n
         at = (cache.pages[0, pos.long() // 16].long(), 0, slice(None), pos.long())
         assert torch.equal(cache.scales[at], s), f"{cache.scales[at].tolist()} and {s.tolist()}"
         assert torch.equal(cache.codes[at], plain.pack(c))
+
+
+# ---- many rows ------------------------------------------------------------------------------------------------------
+def test_heads_of_as_many_rows_as_there_may_be(ctx):  # noqa: F811
+    """2^31 - 1 rows of one head, in place (128 GiB): numbers of rows next to the largest integer."""
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    rows, dim = 2 ** 31 - 1, 32
+    if torch.cuda.mem_get_info()[0] < rows * dim * 2 + (4 << 30):
+        pytest.skip("not enough memory for 2^31 - 1 rows")
+    x = torch.empty(rows, dim, dtype=torch.float16, device="cuda")
+    places = [slice(0, 200), slice(2 ** 30 - 100, 2 ** 30 + 100), slice(rows - 200, rows)]
+    gen = seeded(36)
+    before = []
+    for p in places:
+        x[p] = rand(gen, 200, dim, dt="f16", scale=2.0)
+        before.append(x[p].clone())
+    w = rand(gen, dim, dt="f16", scale=0.3, mean=1.0)
+    try:
+        ctx.rows_heads(x, dim=dim, q_norm=pkg.RowNorm("rms", w, None, 1e-5), q_out=x)
+        ctx.sync()
+        for p, was in zip(places, before):
+            want, mag = plain.heads64(was, dim, "rms", w, None, 1e-5)
+            close(x[p], want, "f16", 32 * U32 * mag, f"rows {p.start} on")
+    finally:
+        del x
+        torch.cuda.empty_cache()
