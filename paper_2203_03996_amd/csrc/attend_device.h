@@ -14,6 +14,7 @@ typedef bf16 bf16x8v __attribute__((ext_vector_type(8)));
 template <typename T> struct Operand {
     typedef f16x8v type;
     static constexpr int TERMS = 1;
+    static constexpr float RAISE = 15.0f;      // weights are 2^15 at most: below 2^-14 fp16 has fewer digits, below 2^-25 none
     static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[0][e] = (f16)v[e];
@@ -25,6 +26,7 @@ template <typename T> struct Operand {
 template <> struct Operand<bf16> {
     typedef bf16x8v type;
     static constexpr int TERMS = 1;
+    static constexpr float RAISE = 0.0f;
     static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[0][e] = (bf16)v[e];

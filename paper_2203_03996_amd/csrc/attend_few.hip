@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256, NB * Operand<T>::TERMS <= 6 ? 2 : 1) void atte
 #pragma unroll
                 for (int d = 0; d < 2 * NB; ++d) o[d] *= factor;
             }
-            const float base = top == -INFINITY ? 0.0f : top;
+            const float base = top == -INFINITY ? 0.0f : top - O::RAISE;       // (sums of weights and of values are raised alike)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], a.factor, -base));

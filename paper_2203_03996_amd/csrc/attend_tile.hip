@@ -23,6 +23,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int kVectors = 128, kTokens = 64;
+constexpr float kSlack = 8.0f;                  // how far a column's maximum may lie above the one that its sums are relative to, as a power of two
 
 // 16-byte columns of a row of LDS (4 NB of them), permuted so that sixteen lanes meet sixteen different ones of the 256 bytes that the banks span: the same
 // column of sixteen rows in a row (keys), four columns of four rows (values, read transposed).
@@ -284,8 +285,8 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
                     for (int e = 0; e < 16; ++e) m = fmaxf(m, s[kb][e]);
                 m = max_of_halves(m);
                 m *= a.factor;                                         // (the factor is above zero)
-                // (weights up to 2^8 do as well as those up to one: sums are scaled anew where a column's maximum has grown by more than that)
-                if (__any(m > top + 8.0f)) {
+                // (weights up to 2^kSlack do as well as those up to one: sums are scaled anew where a column's maximum has grown by more than that)
+                if (__any(m > top + kSlack)) {
                     m = fmaxf(m, top);
                     const float factor = m > top ? __builtin_amdgcn_exp2f(top - m) : 1.0f;
                     top = m;
@@ -293,7 +294,8 @@ __global__ __launch_bounds__(256, (TileShape<T, NB>::waves)) void attend_tile_ke
 #pragma unroll
                     for (int b = 0; b < NB; ++b) o[b] *= factor;
                 }
-                const float base = top == -INFINITY ? 0.0f : top;
+                constexpr float RAISE = O::RAISE > 0.0f ? O::RAISE - kSlack : 0.0f;
+                const float base = top == -INFINITY ? 0.0f : top - RAISE;      // (sums of weights and of values are raised alike)
                 Op p[2][2][TERMS];
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)

@@ -140,3 +140,28 @@ def test_heads_of_as_many_rows_as_there_may_be(ctx):  # noqa: F811
     finally:
         del x
         torch.cuda.empty_cache()
+
+
+# ---- many weak tokens -----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("gap", [8.0, 14.0, 17.5, 19.0])
+def test_many_weak_tokens_behind_a_strong_one_count(ctx, rows, gap):  # noqa: F811
+    """fp16: one token's weight is exp(gap) times each of 6000 others', whose sum matters.  A weight of 2^-39 of the largest is as good as zero for a row alone,
+    one of 2^-32 for rows in tiles (the largest of these is 2^7 at least): half a step below fp16's normal range, for each token."""
+    n, dim = 6001, 32
+    cache = pkg.TokenCache(ctx, 1, n, 1, dim, dtype=torch.float16)
+    v = torch.full((n, 1, dim), 6.0, dtype=torch.float64, device="cuda")
+    k = torch.zeros((n, 1, dim), dtype=torch.float64, device="cuda")
+    strong = 4500
+    k[strong, 0, 0], v[strong] = 1.5, 0.0
+    at, slot = torch.arange(n, device="cuda") // 64, torch.arange(n, device="cuda") % 64
+    for which, x in ((0, k), (1, v)):
+        c, s = plain.quantised(x, 13)
+        cache.codes[at, which, :, slot], cache.scales[at, which, :, slot] = plain.pack(c), s
+    q = torch.zeros(rows, dim, dtype=torch.float16, device="cuda")
+    q[:, 0] = torch.linspace(gap, gap + 0.5, rows, device="cuda") / 1.5
+    got = cache.attend(q, scale=1.0, streams=torch.zeros(rows, dtype=torch.int32, device="cuda"), positions=torch.zeros(rows, dtype=torch.int32, device="cuda"))
+    ctx.sync()
+    pages = torch.arange(cache.num_pages, device="cuda").view(1, -1)
+    want, slack = plain.attend64(q, cache.codes, cache.scales, pages, 64, [0] * rows, [0] * rows, [n], 1.0, weight_u=2.0 ** -11, tiny=2.0 ** (-39 if rows == 1 else -32))
+    close(got, want, "f16", slack, f"gap {gap}")
