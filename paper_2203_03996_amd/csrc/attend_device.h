@@ -35,18 +35,23 @@ template <> struct Operand<bf16> {
     static __device__ __forceinline__ f32x4 mfma16(type a, type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x16 mfma32(type a, type b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
+// (cut, not rounded: eight bits of the 24 to a term are exact too, and the largest numbers do not become infinity)
 template <> struct Operand<float> : Operand<bf16> {
     static constexpr int TERMS = 3;
     static __device__ __forceinline__ void split(const float (&v)[8], type (&o)[TERMS]) {
+        u32x4 w[TERMS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float rest = v[e];
+        for (int e = 0; e < 8; e += 2) {
+            float a = v[e], b = v[e + 1];
 #pragma unroll
             for (int t = 0; t < TERMS; ++t) {
-                o[t][e] = (bf16)rest;
-                rest -= (float)o[t][e];
+                const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+                w[t][e / 2] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                a -= __builtin_bit_cast(float, x & 0xffff0000u), b -= __builtin_bit_cast(float, y & 0xffff0000u);
             }
         }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) o[t] = __builtin_bit_cast(type, w[t]);
     }
 };
 // Eight codes of a word, one scale.

@@ -165,3 +165,44 @@ def test_many_weak_tokens_behind_a_strong_one_count(ctx, rows, gap):  # noqa: F8
     pages = torch.arange(cache.num_pages, device="cuda").view(1, -1)
     want, slack = plain.attend64(q, cache.codes, cache.scales, pages, 64, [0] * rows, [0] * rows, [n], 1.0, weight_u=2.0 ** -11, tiny=2.0 ** (-39 if rows == 1 else -32))
     close(got, want, "f16", slack, f"gap {gap}")
+
+
+# ---- the largest numbers --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_largest_queries(ctx, rows):  # noqa: F811
+    """fp32 queries up to the largest number meet keys as small: what is cut off them to 16 bits must not round up to infinity."""
+    n, dim = 70, 32
+    cache = pkg.TokenCache(ctx, 1, n, 1, dim, dtype=torch.float32)
+    gen = seeded(34)
+    k, v = rand(gen, n, dim) * 2.0 ** -126, rand(gen, n, dim)
+    zero = torch.zeros(n, dtype=torch.int32, device="cuda")
+    cache.append(k, v, streams=zero, positions=torch.arange(n, dtype=torch.int32, device="cuda"))
+    q = rand(gen, rows, dim)
+    q[:, 0] = torch.finfo(torch.float32).max
+    q[:, 1:3] *= 2.0 ** 100
+    zero = zero[:1].expand(rows).contiguous()
+    got = cache.attend(q, scale=0.5, streams=zero, positions=zero)
+    ctx.sync()
+    want, slack = plain.attend64(q, cache.codes, cache.scales, torch.arange(2, device="cuda").view(1, 2), 64, [0] * rows, [0] * rows, [n], 0.5, terms=3, weight_u=2.0 ** -24)
+    close(got, want, "f32", slack, "largest queries")
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attend_of_one_token_is_what_the_cache_holds(ctx, dt, rows):  # noqa: F811
+    """All codes at all scales whose numbers are in the type's normal range; each row sees one token."""
+    first, last = {"f32": (4, 250), "f16": (127 - 13, 127 + 13), "bf16": (4, 250)}[dt]
+    n, dim = last - first + 1, 32
+    cache = pkg.TokenCache(ctx, 1, n, 1, dim, dtype=TYPES[dt][0], page=16)
+    at, slot = torch.arange(n, device="cuda") // 16, torch.arange(n, device="cuda") % 16
+    cache.codes[at, 1, 0, slot] = plain.pack(torch.arange(32, device="cuda") % 16).to(torch.uint8)
+    cache.scales[at, 1, 0, slot, 0] = torch.arange(first, last + 1, dtype=torch.uint8, device="cuda")
+    cache.scales[at, 0] = 127
+    held = cache.read(streams=torch.zeros(n, dtype=torch.int32, device="cuda"), positions=torch.arange(n, dtype=torch.int32, device="cuda"))[1]
+    q = rand(seeded(35), rows, dim, dt=dt)
+    zero = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    for start in range(0, n, rows):
+        pos = torch.arange(start, start + rows, dtype=torch.int32, device="cuda").clamp(max=n - 1)
+        got = cache.attend(q, streams=zero, positions=pos, causal=True, window=1)
+        ctx.sync()
+        assert torch.equal(got, held[pos.long()]), f"{dt} tokens {start} on"
