@@ -778,9 +778,10 @@ class TokenCache:
     the maps are pixels, `length` to a stream: stream i / length, position i % length; with positions alone row i is the
     token of stream i.  Matrices are compact; without a count every row that idx names is wanted.
 
-    The object holds scratch that its attend calls share.  They follow each other on the context's stream, and threads take
-    turns.  Graphs hold the scratch too: two that were captured from one object must not run at the same time, and the object
-    has to outlive them."""
+    The object holds scratch that its attend calls share, as large as the largest of them needs or up to half as large again.
+    Calls follow each other on the context's stream, and threads take turns.  Graphs hold the scratch too (one that has grown
+    since stays for them): two that were captured from one object must not run at the same time, and the object has to
+    outlive them."""
 
     def __init__(self, ctx: Context, streams: int, length: int, heads: int, dim: int, *, dtype=torch.float16, page: int = 64, pages=None,
                  num_pages: int | None = None, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None):
@@ -806,8 +807,8 @@ class TokenCache:
         if pages is None and self.num_pages < streams * per_stream:
             raise ValueError(f"{self.num_pages} pages for {streams} streams of {per_stream}")
         self.codes, self.scales, self.pages = codes, scales, pages
-        # (scratch that a larger one has taken the place of is kept: a graph may hold its address)
-        self._scratch, self._scratch_at, self._kept, self._needs, self._one_call = None, (0, 0), [], {}, threading.Lock()
+        # (_captured: scratch that graphs hold the address of, kept when a larger one takes its place; _in_graph: whether what is there now is among it)
+        self._scratch, self._scratch_at, self._in_graph, self._captured, self._needs, self._one_call = None, (0, 0), False, [], {}, threading.Lock()
 
     def _args(self, a, n, streams, positions, idx, count):
         """Fills in the cache and the tokens of a call with an n-row matrix; returns its rows."""
@@ -889,20 +890,28 @@ class TokenCache:
             if len(self._needs) < 4096:
                 self._needs[rows, q_heads] = need
         with self._one_call:                                      # (a call's kernels follow each other: both use the scratch)
-            a.scratch, a.scratch_bytes = self._scratch_at if need <= self._scratch_at[1] else self._larger_scratch(need)
+            scratch = None
+            if need > self._scratch_at[1]:
+                scratch = self._larger_scratch(need)              # (a graph's own is held until the call is recorded)
+                a.scratch, a.scratch_bytes = scratch.data_ptr(), scratch.numel()
+            else:
+                a.scratch, a.scratch_bytes = self._scratch_at
+                if not self._in_graph and ctx.capturing():        # (once: a graph holds it from now on)
+                    self._in_graph = True
+                    self._captured.append(self._scratch)
             st = ctx.lib.dcnn_cache_attend(ctx.handle, a)
             if st:
                 ctx.check(st)
         return out
 
     def _larger_scratch(self, need):
-        """(address, bytes) of new scratch, which takes the place of the one before it, unless a graph is being captured: then it is the graph's."""
-        scratch = self.ctx.empty(max(need, 256), torch.uint8)
-        at = scratch.data_ptr(), scratch.numel()
-        self._kept.append(scratch)
-        if not self.ctx.capturing():
-            self._scratch, self._scratch_at = scratch, at
-        return at
+        """New scratch: it takes the place of the one before it, half as large again at least, so that sizes that rise by a little are made anew now and
+        then only.  While a graph is being captured it is the graph's alone, out of the graph's memory."""
+        if self.ctx.capturing():
+            return self.ctx.empty(need, torch.uint8)
+        scratch = self.ctx.empty(max(need, self._scratch_at[1] * 3 // 2), torch.uint8)
+        self._scratch, self._scratch_at, self._in_graph = scratch, (scratch.data_ptr(), scratch.numel()), False
+        return scratch
 
 
 _KIND = {"deltagen": DELTAGEN, "act": ACT, "add": ACT, "maxpool": MAXPOOL, "upsample": UPSAMPLE, "accum": ACCUM}

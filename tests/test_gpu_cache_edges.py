@@ -206,3 +206,58 @@ def test_attend_of_one_token_is_what_the_cache_holds(ctx, dt, rows):  # noqa: F8
         got = cache.attend(q, streams=zero, positions=pos, causal=True, window=1)
         ctx.sync()
         assert torch.equal(got, held[pos.long()]), f"{dt} tokens {start} on"
+
+
+# ---- scratch --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("before", [0, 20, 300])
+def test_graphs_keep_the_scratch_of_attention(before):
+    """Captured without a call before it, behind a small one, behind one as large; then larger calls without the graph, whose scratch takes the place of the first."""
+    stream = torch.cuda.Stream()
+    heads, dim, n, rows = 2, 64, 3000, 40                              # (tokens of tiles are split: sums of parts in the scratch)
+    gen = seeded(37)
+    with torch.cuda.stream(stream):
+        own = pkg.Context(0)
+        cache = pkg.TokenCache(own, 1, n, heads, dim, dtype=torch.float16)
+        zero = torch.zeros(n, dtype=torch.int32, device="cuda")
+        pos = torch.arange(n, dtype=torch.int32, device="cuda")
+        cache.append(*(rand(gen, n, heads * dim, dt="f16") for _ in range(2)), streams=zero, positions=pos)
+        q = rand(gen, rows, 4 * dim, dt="f16")
+
+        def call(rows, x=None):
+            return cache.attend(rand(gen, rows, 4 * dim, dt="f16") if x is None else x, streams=zero[:rows], positions=pos[n - rows:], causal=True)
+        if before:
+            call(before)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            captured = [call(rows, q), call(rows, q)]
+        for i in range(4):
+            call(1000 if i == 0 else 2000 + 100 * i)
+            stream.synchronize()
+            torch.cuda.empty_cache()
+            others = [torch.full((size,), 0x7f, dtype=torch.uint8, device="cuda") for size in (1 << 21, 1 << 22, 1 << 23)]      # (in the place of scratch that was let go)
+            q.copy_(rand(gen, rows, 4 * dim, dt="f16"))
+            graph.replay()
+            stream.synchronize()
+            got = [c.clone() for c in captured]
+            assert all((o == 0x7f).all() for o in others), f"replay {i} has written where others' tensors lie"
+            want = call(rows, q)
+            stream.synchronize()
+            assert all(torch.equal(g, want) for g in got), f"replay {i}"
+            del others
+
+
+def test_eager_attention_of_rising_sizes_holds_one_scratch(ctx):  # noqa: F811
+    heads, dim, n = 2, 64, 3000
+    cache = pkg.TokenCache(ctx, 1, n, heads, dim, dtype=torch.float16)
+    gen = seeded(38)
+    q = rand(gen, 600, 4 * dim, dt="f16")
+    zero, pos = torch.zeros(600, dtype=torch.int32, device="cuda"), torch.arange(600, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    before, most = torch.cuda.memory_allocated(), 0
+    for rows in range(7, 600):
+        cache.attend(q[:rows], streams=zero[:rows], positions=pos[:rows], causal=True, out=out[:rows])
+        most = max(most, ctx.lib.dcnn_cache_scratch_bytes(pkg.F16, rows, 4, heads, dim, 1, n))
+    ctx.sync()
+    assert torch.cuda.memory_allocated() - before <= most * 3 // 2 + (1 << 20)
