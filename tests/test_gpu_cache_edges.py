@@ -4,7 +4,7 @@ import torch
 
 import paper_2203_03996_amd as pkg
 from tests import cache_plain as plain
-from tests.test_gpu_cache import TYPES, U32, check_append, close, ctx, ints, new_cache, norm_of, rand, seeded  # noqa: F401
+from tests.test_gpu_cache import TYPES, U32, attention_block, check_append, close, ctx, ints, new_cache, norm_of, rand, seeded  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -261,3 +261,40 @@ def test_eager_attention_of_rising_sizes_holds_one_scratch(ctx):  # noqa: F811
         most = max(most, ctx.lib.dcnn_cache_scratch_bytes(pkg.F16, rows, 4, heads, dim, 1, n))
     ctx.sync()
     assert torch.cuda.memory_allocated() - before <= most * 3 // 2 + (1 << 20)
+
+
+# ---- together -------------------------------------------------------------------------------------------------------
+def test_a_captured_block_replayed_with_other_numbers_of_pixels():
+    """A block's step as a graph: replayed with other flagged pixels, from none to all, and eager steps between, it leaves the tokens and the cache that the eager step does."""
+    streams, side, c = 3, 9, 96
+    n = streams * side * side
+    stream = torch.cuda.Stream()
+    gen = seeded(39)
+    with torch.cuda.stream(stream):
+        own = pkg.Context(0)
+        block = attention_block(own, gen, "f16", c, streams, side, 4, 2, 32)
+        x, y = rand(gen, n, c, dt="f16"), torch.zeros(n, c, dtype=torch.float16, device="cuda")
+        idx, count = torch.arange(n, dtype=torch.int32, device="cuda"), ints(n)
+        block.step(x, y, idx, count)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            block.step(x, y, idx, count)
+        for m in (40, 0, 1, n, 7, 200):
+            at = torch.randperm(n, device="cuda", generator=gen)[:m].sort().values
+            idx.fill_(1 << 30)
+            idx[:m] = at.to(torch.int32)
+            count.fill_(m)
+            x[at] = rand(gen, m, c, dt="f16")
+            before = y.clone(), block.cache.codes.clone(), block.cache.scales.clone()
+            graph.replay()
+            stream.synchronize()
+            got = y.clone(), block.cache.codes.clone(), block.cache.scales.clone()
+            for t, was in zip((y, block.cache.codes, block.cache.scales), before):
+                t.copy_(was)
+            block.step(x, y, idx, count)
+            stream.synchronize()
+            assert all(torch.equal(g, w) for g, w in zip(got, (y, block.cache.codes, block.cache.scales))), f"{m} pixels"
+            rest = torch.ones(n, dtype=torch.bool, device="cuda")
+            rest[at] = False
+            assert torch.equal(y[rest], before[0][rest]) and (m == 0 or not torch.equal(y[at], before[0][at]))
