@@ -466,8 +466,9 @@ dcnn_status dcnn_cache_read(dcnn_ctx* ctx, const dcnn_cache_read_args* args);
  * over the tokens t of the row's stream with t < len (lens_dev[stream], cut to 0 .. length; NULL: length), t <= position if
  * `causal`, and |position - t| < window if window > 0.  Rows that see no token, or have none, become zeros.  Queries and
  * keys meet exactly, sums and the softmax's statistics are fp32; the weights of a row are rounded to the dtype's digits before
- * they meet the values (F32: kept; F16: small ones to 2^-32 of the row's largest at most), and the result once more.  Keys and values are what
- * dcnn_cache_read gives.
+ * they meet the values (F32: kept; F16: small ones to 2^-32 of the row's largest at most), and the result once more.  (The
+ * memory of a cache is the same in all dtypes: described as an F32 one, it serves calls that want weights kept.)  Keys and
+ * values are what dcnn_cache_read gives.
  * scratch_dev: dcnn_cache_scratch_bytes(...) bytes of the cache's and the call's sizes, 256-byte aligned, whatever it holds;
  * calls may share it one after the other.  rows * q_heads at most 2^30. */
 typedef struct {

@@ -11,6 +11,9 @@ typedef bf16 bf16x8v __attribute__((ext_vector_type(8)));
 
 // What a type's queries, weights, keys and values are on the matrix cores: TERMS operands whose sum is the number.  Codes times a power of two are
 // exact in bf16 (and, from 2^-24 to 2^16, in fp16), fp32 numbers are three bf16 ones.
+// Weights of 16-bit types are one operand, rounded by half a step of each at most.  Another one for what that leaves over (weights as good as fp32's) was
+// measured: one row of 262143 tokens 54 us in place of 50, 64 rows of up to 8192 70 in place of 64, prompts in tiles 820 in place of 655, flagged pixels 657
+// in place of 442.  A call that wants them kept takes the cache's memory, which is the same in all types, as fp32's.
 template <typename T> struct Operand {
     typedef f16x8v type;
     static constexpr int TERMS = 1;

@@ -5,9 +5,9 @@
 //
 // A head's D values lie in the registers of D / 8 lanes (eight to a lane), its statistics and a block's largest magnitude are lane
 // permutations, and a value's partner in a rotation by halves is read again (from the L1) rather than passed between lanes.  A workgroup
-// takes some rows and up to eight heads of each side by side.
+// takes some rows and heads of each side by side: two where rows are many, and up to all the places that it has (2048 / D, D a power of two) where they are few.
 // Keys are fp64 from the norm to the code: a code is the same whatever the order of a sum.
-// Heads move 344 MB (16384 rows of 40 x 128, bf16) in 75 us, 4.6 TB/s.  Appending 16275 rows of 8 x 128 (bf16, pages of 16) takes 33 us, 11 of them for
+// Heads move 344 MB (16384 rows of 40 x 128, bf16) in 76 us, 4.5 TB/s.  Appending 16275 rows of 8 x 128 (bf16, pages of 16) takes 33 us, 11 of them for
 // the values, where all of its 84 MB could take 17: a key's chain of norm, fp64 and rounding is latency and instructions.  Reading them back takes 16.
 #include "cache_device.h"
 
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(256, OP == kAppendHeads && !BIAS ? 4 : 1) void head
     const int at = in ? lane * 8 : 0;
     const uint32_t count = (uint32_t)row_count(a.tokens.count, a.tokens.rows);         // (up to 2^31 - 1: with a tile's rows on top it needs the last bit)
     const RotationArgs& rot = a.rotation;
-    // 2^shift heads of a row side by side: two, so that what belongs to the row serves many, and as many as there are where workgroups are left
+    // 2^shift heads of a row side by side: two, so that what belongs to the row serves many, and as many as have a place where workgroups are left
     int shift = a.shift;
     while (shift > 1 && (int64_t)((count + (R >> shift) - 1) / (uint32_t)(R >> shift)) * a.jobs > (int)gridDim.x) --shift;
     const int rows = R >> shift, stride = 1 << shift, h0 = sub & (stride - 1);

@@ -298,3 +298,23 @@ def test_a_captured_block_replayed_with_other_numbers_of_pixels():
             rest = torch.ones(n, dtype=torch.bool, device="cuda")
             rest[at] = False
             assert torch.equal(y[rest], before[0][rest]) and (m == 0 or not torch.equal(y[at], before[0][at]))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("rows", [2, 90])
+def test_a_cache_in_16_bits_serves_calls_in_fp32(ctx, dt, rows):  # noqa: F811
+    """The memory is the same: appended in 16 bits, read and attended to in fp32, with weights kept."""
+    n, heads, dim = 700, 2, 64
+    gen = seeded(40)
+    cache = pkg.TokenCache(ctx, 2, n, heads, dim, dtype=TYPES[dt][0])
+    stream, pos = torch.arange(2, dtype=torch.int32, device="cuda").repeat_interleave(n), torch.arange(n, dtype=torch.int32, device="cuda").repeat(2)
+    cache.append(*(rand(gen, 2 * n, heads * dim, dt=dt) for _ in range(2)), streams=stream, positions=pos)
+    wide = pkg.TokenCache(ctx, 2, n, heads, dim, dtype=torch.float32, codes=cache.codes, scales=cache.scales)
+    q = rand(gen, rows, 4 * dim, dt=dt).float()
+    at = torch.randint(0, n, (rows,), dtype=torch.int32, device="cuda", generator=gen)
+    of = torch.arange(rows, dtype=torch.int32, device="cuda") % 2
+    got, held = wide.attend(q, streams=of, positions=at, causal=True), (cache.read(), wide.read())
+    ctx.sync()
+    assert all(torch.equal(a.float(), b) for a, b in zip(*held))
+    want, slack = plain.attend64(q, cache.codes, cache.scales, torch.arange(22, device="cuda").view(2, 11), 64, of, at, [n, n], dim ** -0.5, True, 0, 3, 2.0 ** -24)
+    close(got, want, "f32", slack, f"{dt} cache in fp32")
