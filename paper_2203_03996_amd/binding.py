@@ -770,7 +770,7 @@ class TokenCache:
     """Keys and values of the tokens of `streams` streams, up to `length` each, in 4 bits (dcnn_cache), and attention over them.
 
     heads, dim: of keys and values; dtype: of queries, keys, values and outputs.  page: tokens of a page.  pages: int32
-    [streams, ceil(length / page)], the number of each page, read at every call (the caller may hand pages out anew), or
+    [streams, ceil(length / page)], the number of each page, read at every call (to hand pages out anew, write into it), or
     None where every stream has its own, one behind the other.  codes, scales: the memory (see dcnn_cache), or None for
     new, zeroed memory of `num_pages` pages (as many as all streams need where it is not given).
 
