@@ -100,6 +100,7 @@ AttendPlan attend_plan(int dtype_size, int64_t rows, int q_heads, int heads, int
     AttendPlan p;
     // A tile of 128 query vectors reads its tokens once, a row alone reads them for itself: some rows of a stream find them in the caches.
     // (16 streams of 4096 tokens, 32 heads on 8 of 128: four rows each take 48 us alone and 57 in tiles, six 72 and 79, eight 87 and 56.)
+    // `rows` are those that the call has room for, taken as spread over all streams: fewer, or those of a few streams, are known on the GPU alone.
     p.tiles = rows > 6 * streams;
     if (p.tiles) {
         // two workgroups to a compute unit, with 256 tokens each at least (512 rows of a stream of 8192 tokens, the same heads: 278 us unsplit, 96 us;
